@@ -422,6 +422,34 @@ SPEC_API spec_status spec_sample_draft(int32_t n, const float* logits, int32_t V
                                        const int32_t* pos, uint64_t seed, int32_t* tokens,
                                        void* workspace, size_t workspace_bytes, void* stream);
 
+/* Log probabilities, entropy and top alternatives of logits rows: what a
+ * caller reports or ranks candidates by beside the tokens of the decision
+ * pass, or expands candidates with (the target's logits of a verify are at
+ * spec_last_logits).  Row r is the V floats at logits + r * row_stride (device
+ * fp32, row_stride >= V) under softmax(z / T), T = temperature[r] (device fp32
+ * [rows]; NULL: 1).  T = 0 is the point mass on the first maximum.
+ *   logprobs[r]  log p(tokens[r]) (natural logarithm; tokens device int32
+ *                [rows]; -inf for an id outside the vocabulary); NULL: not
+ *                wanted, tokens may be NULL then
+ *   entropy[r]   -sum p log p; NULL: not wanted
+ *   top_ids, top_logprobs [rows, n_top]: the n_top <= min(64, V) tokens of the
+ *                largest logits, in descending order, equal logits by ascending
+ *                id, masked tokens (-inf) last; may be NULL for n_top = 0
+ * A row that defines no distribution (every logit -inf; a logit +inf or NaN; a
+ * temperature negative or NaN) gives NaN and ids -1.  Outputs are device
+ * buffers that overlap no input.  Sums and statistics are fp32; results do not
+ * depend on the other rows of a call.  workspace: device, 16-byte aligned, >=
+ * spec_token_logprobs_workspace_bytes, not shared by calls that overlap in time.
+ * Nothing is read from the host, so the call can be captured into a graph and
+ * replayed on new contents.  Rows that are 16-byte aligned (row_stride % 4 ==
+ * 0) are read fastest.  Asynchronous. */
+SPEC_API size_t spec_token_logprobs_workspace_bytes(int32_t rows, int32_t V, int32_t n_top);
+SPEC_API spec_status spec_token_logprobs(int32_t rows, int32_t V, const float* logits, int64_t row_stride,
+                                         const float* temperature, const int32_t* tokens, int32_t n_top,
+                                         float* logprobs, float* entropy, int32_t* top_ids,
+                                         float* top_logprobs, void* workspace, size_t workspace_bytes,
+                                         void* stream);
+
 /* The generator itself: out (device fp32 [n]) <- uniforms of stream
  * (seed, seq_id, pos, purpose), words 0..n-1. */
 SPEC_API spec_status spec_philox_uniform(uint64_t seed, int64_t seq_id, int32_t pos, int32_t purpose,

@@ -68,6 +68,69 @@ SPEC_API spec_status spec_op_attention(int32_t dtype, int32_t n_seqs, const int3
                                        const void* v_pages, void* out, void* workspace,
                                        size_t workspace_bytes, void* stream);
 
+/* Copies of cache pages in every plane of a pool: page dst_pages[i] of each of
+ * the n_planes planes <- page src_pages[i] of that plane (host int32 [n]).
+ * pool: device, 16-byte aligned, [n_planes][num_pages][page_bytes] (a context's
+ * pool is one: K and V pages of every layer; page_bytes % 16 == 0, whatever the
+ * pages hold).  One source may have several copies; a page that is a
+ * destination twice, or a destination and a source, is refused
+ * (SPEC_E_INVALID), as is one outside the pool.  workspace: device, 16-byte
+ * aligned, >= spec_op_kv_copy_pages_workspace_bytes(n), not shared by calls that
+ * overlap in time.  A captured call takes at most 384 pairs
+ * (SPEC_E_UNSUPPORTED beyond).  Asynchronous; host arrays are consumed before
+ * return. */
+SPEC_API size_t spec_op_kv_copy_pages_workspace_bytes(int32_t n);
+SPEC_API spec_status spec_op_kv_copy_pages(int32_t n_planes, int32_t num_pages, size_t page_bytes, void* pool,
+                                           int32_t n, const int32_t* src_pages, const int32_t* dst_pages,
+                                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* The KV cache in 4 bits, for one layer: 17/64 of the bytes of a bf16 cache.
+ * k_pages and v_pages (device, 16-byte aligned): [num_pages][Hkv] blocks of 16
+ * tokens x hd dims, spec_kv4_page_bytes(Hkv, hd) bytes a page, hd 64 or 128 (0
+ * bytes, and SPEC_E_UNSUPPORTED from the calls, for another).  A token's head
+ * vector is held in blocks of 32 consecutive dims: a scale 2^E, E the smallest
+ * integer >= -126 with max |x| <= 6 2^E, and for every x the nearest of 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6 times 2^E with its sign (ties to the one of even code 0, 2,
+ * 4, 6 in that order).  A block with an infinity or a NaN reads back as NaN.
+ * Every value held is a bf16 number.  The library alone writes the pages
+ * (kv4_layout.h has the byte order). */
+SPEC_API size_t spec_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim);
+
+/* spec_op_rope_kv into a 4-bit cache: q_out <- the rotated q (dtype), the
+ * rotated k and the v of row r into slot[r].  A row with a slot outside 0 ..
+ * 16 num_pages - 1 (padding: -1) has its q written and no K / V.  Two rows of
+ * one call must not have one slot.  qkv and q_out 16-byte aligned. */
+SPEC_API spec_status spec_op_rope_kv4(int32_t dtype, int32_t R, int32_t n_heads, int32_t n_kv_heads,
+                                      int32_t head_dim, float theta, const float* qkv, const int32_t* pos,
+                                      const int32_t* slot, int32_t num_pages, void* q_out, void* k_pages,
+                                      void* v_pages, void* stream);
+
+/* The values held in the slots of a 4-bit cache: k_out, v_out (device, dtype,
+ * [R, Hkv, hd], 16-byte aligned) row r <- slot[r] (device int32); rows with a
+ * slot outside the pool are left as they were. */
+SPEC_API spec_status spec_op_kv4_read(int32_t dtype, int32_t R, int32_t n_kv_heads, int32_t head_dim,
+                                      const int32_t* slot, int32_t num_pages, const void* k_pages,
+                                      const void* v_pages, void* k_out, void* v_out, void* stream);
+
+/* spec_op_attention over a 4-bit cache.  rows[i] may be 0 (a sequence without
+ * rows in this call).  num_pages: pages of the pool; a page id outside it is
+ * refused (SPEC_E_INVALID).  q, out: dtype, 16-byte aligned.  n_heads /
+ * n_kv_heads <= 64 (bf16) or 32 (fp32), else SPEC_E_UNSUPPORTED.  fp32 keeps q
+ * and the probabilities to 24 bits.  workspace: device, 256-byte aligned, >=
+ * spec_op_attention_kv4_workspace_bytes of the same rows and positions (0 for
+ * arguments the call refuses), not shared by calls that overlap in time.  A
+ * captured call takes tables of at most 3 KB (SPEC_E_UNSUPPORTED beyond).
+ * Asynchronous; host arrays are consumed before return. */
+SPEC_API size_t spec_op_attention_kv4_workspace_bytes(int32_t dtype, int32_t n_seqs, const int32_t* rows,
+                                                      const int32_t* pos0, int32_t max_pages, int32_t n_heads,
+                                                      int32_t n_kv_heads, int32_t head_dim);
+SPEC_API spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const int32_t* rows,
+                                           const int32_t* pos0, const int32_t* page_table, int32_t max_pages,
+                                           int32_t num_pages, int32_t n_heads, int32_t n_kv_heads,
+                                           int32_t head_dim, const void* q, const void* k_pages,
+                                           const void* v_pages, void* out, void* workspace,
+                                           size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

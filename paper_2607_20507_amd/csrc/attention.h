@@ -45,13 +45,19 @@ struct AttnArgs {
 hipError_t launch_attention_bf16(const AttnArgs& a, const AttnItem* d_items, int n_items,
                                  const AttnGroup* d_groups, int n_groups, int nt, int w, hipStream_t st);
 
+// Merges the partials of split items into the output (element type a.dtype),
+// parts in index order; nt as the items' launch.
+hipError_t launch_attention_combine(const AttnArgs& a, const AttnGroup* d_groups, int n_groups, int nt,
+                                    hipStream_t st);
+
 // bf16 causal prefill: items from plan_attention's prefill form (blocks of
 // 256 / G consecutive rows of one sequence against keys 0 .. t1 - 1, t0 = 0,
 // part < 0), heaviest first; grid n_items x Hkv (kv head = block % Hkv).
-// few_keys: every item has at most kPrefillShortKeys keys.
+// few_keys: every item has at most kPrefillShortKeys keys.  far: scores may be
+// of any size.
 constexpr int kPrefillShortKeys = 384;
 hipError_t launch_attention_prefill_bf16(const AttnArgs& a, const AttnItem* d_items, int n_items, bool few_keys,
-                                         hipStream_t st);
+                                         hipStream_t st, bool far = false);
 const char* attn_prefill_kernel_name(int hd, bool few_keys);
 
 // fp32: one workgroup of 256 threads per (row, head); row r of sequence slot row_seq[r] at

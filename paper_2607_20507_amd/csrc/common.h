@@ -39,6 +39,8 @@ typedef f32x4 f32x4_any __attribute__((aligned(4)));  // 16 bytes of global memo
 
 constexpr int kWave = 64;
 constexpr int kPage = 16;
+// most workgroups of 256 threads in a launch (a launch counts its threads in 32 bits)
+constexpr size_t kMaxGrid256 = (size_t{1} << 24) - 1;
 
 __device__ __forceinline__ float bf16_to_f32(bf16_t x) {
   return __uint_as_float(static_cast<uint32_t>(x) << 16);

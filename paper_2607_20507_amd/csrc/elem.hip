@@ -429,7 +429,38 @@ __global__ __launch_bounds__(256) void kv_move_kernel(KvMoveJob j) {
   }
 }
 
+// Copies of whole pages: workgroup (pair, span of the page, plane) moves a span
+// of kCopySpan 16-byte units, all of a thread's loads in flight together.
+constexpr int kCopySpan = 1024;
+__global__ __launch_bounds__(256) void kv_copy_kernel(const int2* __restrict__ pairs, uint4* __restrict__ pool,
+                                                      int spans, uint32_t page_units, size_t plane_units) {
+  const int2 p = pairs[blockIdx.x / spans];
+  uint4* plane = pool + blockIdx.y * plane_units;
+  const uint4* src = plane + static_cast<size_t>(p.x) * page_units;
+  uint4* dst = plane + static_cast<size_t>(p.y) * page_units;
+  const uint32_t u0 = blockIdx.x % spans * kCopySpan + threadIdx.x;
+  constexpr int N = kCopySpan / 256;
+  uint4 v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (u0 + 256 * i < page_units) v[i] = ld_stream(src + u0 + 256 * i);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (u0 + 256 * i < page_units) dst[u0 + 256 * i] = v[i];
+}
+
 }  // namespace
+
+hipError_t launch_kv_copy_pages(const int2* d_pairs, int n, void* pool, int n_planes, int64_t num_pages,
+                                size_t page_bytes, hipStream_t st) {
+  if (n <= 0 || n_planes <= 0) return hipSuccess;
+  const size_t units = page_bytes / 16;
+  const size_t spans = (units + kCopySpan - 1) / kCopySpan;
+  if (page_bytes % 16 || units == 0 || spans * n > kMaxGrid256 || n_planes > 65535) return hipErrorInvalidValue;
+  kv_copy_kernel<<<dim3(static_cast<uint32_t>(spans * n), n_planes), 256, 0, st>>>(
+      d_pairs, static_cast<uint4*>(pool), static_cast<int>(spans), static_cast<uint32_t>(units), num_pages * units);
+  return hipGetLastError();
+}
 
 hipError_t launch_kv_move(int dtype, const KvMoveJob& j, hipStream_t st) {
   if (j.n_groups <= 0 || j.n_layers <= 0) return hipSuccess;

@@ -1,0 +1,570 @@
+// The 4-bit KV cache (kv4_layout.h): append, read back, attention.
+
+#include <algorithm>
+#include <type_traits>
+
+#include "attn_finish.h"
+#include "common.h"
+#include "kv4.h"
+#include "kv4_layout.h"
+
+namespace spec {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---------------------------------------------------------------------------
+// values <-> codes
+
+__device__ __forceinline__ float scale_of_byte(uint32_t b) { return __uint_as_float(b << 23); }
+
+// Codes of two values (a in the low nibble) with the scale s = 2^E.  The
+// instruction rounds to the nearest level, ties to the even code.
+template <int SEL>
+__device__ __forceinline__ uint32_t put_codes(uint32_t w, float a, float b, float s) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, a, b, s, SEL);
+}
+
+// The two values of byte SEL of w as bf16 (low nibble in the low half).  Only
+// the exponent field of s counts, so callers pass a scale byte shifted there
+// with whatever bits surround it.
+template <int SEL>
+__device__ __forceinline__ uint32_t get_codes(uint32_t w, uint32_t s) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, __uint_as_float(s), SEL));
+}
+// Scale byte B of a word, moved to the exponent field of a float.
+template <int B>
+__device__ __forceinline__ uint32_t scale_bits(uint32_t w) {
+  return B == 0 ? w << 23 : B == 1 ? w << 15 : B == 2 ? w << 7 : w >> 1;
+}
+
+// One 4-byte unit: 8 values of one token as bf16.
+__device__ __forceinline__ uint4 get8(uint32_t w, uint32_t s) {
+  return make_uint4(get_codes<0>(w, s), get_codes<1>(w, s), get_codes<2>(w, s), get_codes<3>(w, s));
+}
+
+// 8 tokens of one V byte column (w0: tokens 0..3, w1: 4..7; s0, s1 their scale
+// bytes): the low nibbles' dim and the high nibbles' dim, 8 tokens each.
+__device__ __forceinline__ void get8_tokens(uint32_t w0, uint32_t w1, uint32_t s0, uint32_t s1, uint4& lo, uint4& hi) {
+  const uint32_t t0 = get_codes<0>(w0, scale_bits<0>(s0)), t1 = get_codes<1>(w0, scale_bits<1>(s0));
+  const uint32_t t2 = get_codes<2>(w0, scale_bits<2>(s0)), t3 = get_codes<3>(w0, scale_bits<3>(s0));
+  const uint32_t t4 = get_codes<0>(w1, scale_bits<0>(s1)), t5 = get_codes<1>(w1, scale_bits<1>(s1));
+  const uint32_t t6 = get_codes<2>(w1, scale_bits<2>(s1)), t7 = get_codes<3>(w1, scale_bits<3>(s1));
+  auto low = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); };
+  auto high = [](uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); };
+  lo = make_uint4(low(t0, t1), low(t2, t3), low(t4, t5), low(t6, t7));
+  hi = make_uint4(high(t0, t1), high(t2, t3), high(t4, t5), high(t6, t7));
+}
+
+template <typename T>
+__device__ __forceinline__ void put8(T* dst, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+  } else {
+    reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+// 8 bf16 values to T, exact
+template <typename T>
+__device__ __forceinline__ void put8_bf16(T* dst, const uint4& u) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(dst) = u;
+  } else {
+    reinterpret_cast<uint4*>(dst)[0] = make_uint4(u.x << 16, u.x & 0xFFFF0000u, u.y << 16, u.y & 0xFFFF0000u);
+    reinterpret_cast<uint4*>(dst)[1] = make_uint4(u.z << 16, u.z & 0xFFFF0000u, u.w << 16, u.w & 0xFFFF0000u);
+  }
+}
+
+// Bits of the larger magnitude of a and b (as integers: an infinity or a NaN
+// is above every finite magnitude, and the largest survives).
+__device__ __forceinline__ uint32_t mag_max(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// ---------------------------------------------------------------------------
+// RoPE + append.  One workgroup per row.  Thread (head, t) rotates pairs
+// 8 t .. 8 t + 7 of a q or k head: dims 8 t .. and hd / 2 + 8 t .., which are
+// one 4-byte unit each of two blocks of the key, whose other units are held by
+// the 3 neighbouring lanes.  Angles, sines and the keys' rotation are in fp64,
+// so that a key's code depends on its exact value and not on the order of the
+// roundings before it; q is rotated in fp32.
+template <typename T>
+__global__ __launch_bounds__(256) void rope_kv4_kernel(int Hq, int Hkv, int hd, float theta,
+                                                       const float* __restrict__ qkv, const int32_t* __restrict__ pos,
+                                                       const int32_t* __restrict__ slot, int num_pages,
+                                                       T* __restrict__ q, uint8_t* __restrict__ kpool,
+                                                       uint8_t* __restrict__ vpool) {
+  const int r = blockIdx.x;
+  const int half = hd / 2, groups = half / 8;
+  const float* x = qkv + static_cast<size_t>(r) * (Hq + 2 * Hkv) * hd;
+  __shared__ double s_cos[64], s_sin[64];
+  if (static_cast<int>(threadIdx.x) < half) {
+    double sn, cs;
+    sincos(static_cast<double>(pos[r]) * exp(-(2.0 * threadIdx.x / hd) * log(static_cast<double>(theta))), &sn, &cs);
+    s_cos[threadIdx.x] = cs;
+    s_sin[threadIdx.x] = sn;
+  }
+  __syncthreads();
+  const int sl = slot[r];
+  const bool keep = sl >= 0 && sl < 16 * num_pages;
+  const int page = keep ? sl >> 4 : 0, off = sl & 15;
+  const int bb = kv4_block_bytes(hd);
+  // (head, t) pairs in steps of the workgroup: the 4 lanes of a block run the
+  // same iterations (groups % 4 == 0)
+  for (int e = threadIdx.x; e < (Hq + Hkv) * groups; e += blockDim.x) {
+    const int h = e / groups, t = e % groups, i0 = 8 * t;
+    const float4* pa = reinterpret_cast<const float4*>(x + h * hd + i0);
+    const float4* pb = reinterpret_cast<const float4*>(x + h * hd + i0 + half);
+    const float4 a0 = pa[0], a1 = pa[1], b0 = pb[0], b1 = pb[1];
+    const float av[8] = {a0.x, a0.y, a0.z, a0.w, a1.x, a1.y, a1.z, a1.w};
+    const float bv[8] = {b0.x, b0.y, b0.z, b0.w, b1.x, b1.y, b1.z, b1.w};
+    float ra[8], rb[8];
+    if (h < Hq) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float c = static_cast<float>(s_cos[i0 + j]), sn = static_cast<float>(s_sin[i0 + j]);
+        ra[j] = av[j] * c - bv[j] * sn;
+        rb[j] = bv[j] * c + av[j] * sn;
+      }
+      T* o = q + (static_cast<size_t>(r) * Hq + h) * hd;
+      put8(o + i0, ra);
+      put8(o + i0 + half, rb);
+      continue;
+    }
+    uint32_t ma = 0, mb = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const double c = s_cos[i0 + j], sn = s_sin[i0 + j];
+      const double a = av[j], b = bv[j];
+      ra[j] = static_cast<float>(a * c - b * sn);
+      rb[j] = static_cast<float>(b * c + a * sn);
+      ma = mag_max(ma, mag(ra[j]));
+      mb = mag_max(mb, mag(rb[j]));
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      ma = mag_max(ma, __shfl_xor(ma, o, kWave));
+      mb = mag_max(mb, __shfl_xor(mb, o, kWave));
+    }
+    if (!keep) continue;
+    uint8_t* blk = kpool + (static_cast<size_t>(page) * Hkv + (h - Hq)) * bb;
+    auto put = [&](const float (&v)[8], uint32_t m, int d0) {
+      const int s = d0 / 32, g = d0 / 8 % 4;
+      const uint32_t sb = kv4_scale_of(m);
+      const float sc = scale_of_byte(sb);
+      uint32_t w = put_codes<0>(0u, v[0], v[1], sc);
+      w = put_codes<1>(w, v[2], v[3], sc);
+      w = put_codes<2>(w, v[4], v[5], sc);
+      w = put_codes<3>(w, v[6], v[7], sc);
+      *reinterpret_cast<uint32_t*>(blk + kv4_k_unit(off, s, g, hd)) = w;
+      if (g == 0) blk[kv4_k_scale(off, s, hd)] = static_cast<uint8_t>(sb);
+    };
+    put(ra, ma, i0);
+    put(rb, mb, i0 + half);
+  }
+  if (!keep) return;
+  // values: thread (head, block, i) holds dims 32 b + i and 32 b + 16 + i
+  for (int e = threadIdx.x; e < Hkv * half; e += blockDim.x) {
+    const int h = e / half, b = e % half / 16, i = e % 16;
+    const float* v = x + (Hq + Hkv + h) * hd + 32 * b + i;
+    const float lo = v[0], hi = v[16];
+    uint32_t m = mag_max(mag(lo), mag(hi));
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) m = mag_max(m, __shfl_xor(m, o, kWave));
+    const uint32_t sb = kv4_scale_of(m);
+    uint8_t* blk = vpool + (static_cast<size_t>(page) * Hkv + h) * bb;
+    blk[kv4_v_byte(off, b, i)] = static_cast<uint8_t>(put_codes<0>(0u, lo, hi, scale_of_byte(sb)));
+    if (i == 0) blk[kv4_v_scale(off, b, hd)] = static_cast<uint8_t>(sb);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Read back: one workgroup per (16 rows, kv head).
+template <typename T>
+__global__ __launch_bounds__(256) void kv4_read_kernel(int R, int Hkv, int hd, const int32_t* __restrict__ slot,
+                                                       int num_pages, const uint8_t* __restrict__ kpool,
+                                                       const uint8_t* __restrict__ vpool, T* __restrict__ k,
+                                                       T* __restrict__ v) {
+  const int r0 = blockIdx.x / Hkv * 16, h = blockIdx.x % Hkv;
+  const int bb = kv4_block_bytes(hd);
+  const int units = hd / 8;
+  for (int e = threadIdx.x; e < 16 * units; e += blockDim.x) {
+    const int r = r0 + e / units, u = e % units;
+    if (r >= R) break;
+    const int sl = slot[r];
+    if (sl < 0 || sl >= 16 * num_pages) continue;
+    const uint8_t* blk = kpool + (static_cast<size_t>(sl >> 4) * Hkv + h) * bb;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(blk + kv4_k_unit(sl & 15, u / 4, u % 4, hd));
+    const uint32_t s = blk[kv4_k_scale(sl & 15, u / 4, hd)];
+    put8_bf16(k + (static_cast<size_t>(r) * Hkv + h) * hd + 8 * u, get8(w, s << 23));
+  }
+  // values: thread (row, block, half) takes 8 byte columns, dims 32 b + 8 o .. and 32 b + 16 + 8 o ..
+  for (int e = threadIdx.x; e < 16 * (hd / 16); e += blockDim.x) {
+    const int r = r0 + e / (hd / 16), b = e % (hd / 16) / 2, o = e % 2;
+    if (r >= R) break;
+    const int sl = slot[r];
+    if (sl < 0 || sl >= 16 * num_pages) continue;
+    const uint8_t* blk = vpool + (static_cast<size_t>(sl >> 4) * Hkv + h) * bb;
+    const uint32_t s = static_cast<uint32_t>(blk[kv4_v_scale(sl & 15, b, hd)]) << 23;
+    uint32_t t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = get_codes<0>(blk[kv4_v_byte(sl & 15, b, 8 * o + i)], s);
+    auto low = [&](int i) { return __builtin_amdgcn_perm(t[i + 1], t[i], 0x05040100u); };
+    auto high = [&](int i) { return __builtin_amdgcn_perm(t[i + 1], t[i], 0x07060302u); };
+    T* dst = v + (static_cast<size_t>(r) * Hkv + h) * hd + 32 * b + 8 * o;
+    put8_bf16(dst, make_uint4(low(0), low(2), low(4), low(6)));
+    put8_bf16(dst + 16, make_uint4(high(0), high(2), high(4), high(6)));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Expansion to bf16 pages: one workgroup per (page, kv head).
+template <int HD>
+__global__ __launch_bounds__(256) void kv4_expand_kernel(const int32_t* __restrict__ src, int Hkv,
+                                                         const uint8_t* __restrict__ kpool,
+                                                         const uint8_t* __restrict__ vpool, bf16_t* __restrict__ kdst,
+                                                         bf16_t* __restrict__ vdst) {
+  constexpr int DS = HD / 32, BB = kv4_block_bytes(HD);
+  const int p = blockIdx.x / Hkv, h = blockIdx.x % Hkv;
+  const size_t from = (static_cast<size_t>(src[p]) * Hkv + h) * BB;
+  const size_t to = (static_cast<size_t>(p) * Hkv + h) * 16 * HD;
+  // K: destination unit ((s 2 + hh) 4 + g) 8 + j is source unit s of lane unit (hh, g, j)
+  for (int u = threadIdx.x; u < 2 * HD; u += blockDim.x) {
+    const int j = u % 8, g = u / 8 % 4, hh = u / 32 % 2, s = u / 64;
+    const uint8_t* blk = kpool + from;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(
+        blk + (HD == 128 ? ((hh * 4 + g) * 8 + j) * 16 : ((g * 8 + j) * 2 + hh) * 8) + 4 * s);
+    const uint32_t sb = blk[kv4_code_bytes(HD) + (j * 2 + hh) * DS + s];
+    reinterpret_cast<uint4*>(kdst + to)[u] = get8(w, sb << 23);
+  }
+  // V: 8 tokens of a byte column are two destination units
+  for (int e = threadIdx.x; e < HD; e += blockDim.x) {
+    const int i = e % 16, th = e / 16 % 2, b = e / 32;
+    const uint8_t* blk = vpool + from;
+    const uint2 w = *reinterpret_cast<const uint2*>(blk + kv4_v_byte(8 * th, b, i));
+    const uint2 s = *reinterpret_cast<const uint2*>(blk + kv4_v_scale(8 * th, b, HD));
+    uint4 lo, hi;
+    get8_tokens(w.x, w.y, s.x, s.y, lo, hi);
+    uint4* o = reinterpret_cast<uint4*>(vdst + to);
+    o[(2 * b * 2 + th) * 16 + i] = lo;
+    o[((2 * b + 1) * 2 + th) * 16 + i] = hi;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention over the 4-bit cache: items, lanes and softmax as the bf16 verify
+// attention (attention.hip): S^T = K Q^T and O^T = V^T P^T on the matrix cores,
+// 32 keys at a time, a query vector's statistics in the lanes of its column.
+// The operands come from the 4-bit pages: a lane's K operand is 4 bytes of one
+// key and one scale, its V^T operand 8 bytes (8 tokens, two dims) with 8
+// scales, converted in registers to bf16, which holds every value exactly.
+// T = float: q and the probabilities are split into three bf16 parts (24 bits
+// of fraction), whose products with the cache's values are exact in fp32.
+
+template <typename T>
+struct Parts;
+template <>
+struct Parts<bf16_t> { static constexpr int n = 1; };
+template <>
+struct Parts<float> { static constexpr int n = 3; };
+
+// Two fp32 -> N pairs of bf16 whose sums are the values (N = 1: rounded once).
+template <int N>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&w)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    w[i] = cvt_pk_bf16(a, b);
+    if (i + 1 < N) {
+      a -= __uint_as_float(w[i] << 16);
+      b -= __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+}
+
+constexpr int kStagedPages = 256;  // page ids of one work item kept in LDS (4096 keys)
+
+template <typename T, int HD, int NT, int W>
+__global__ __launch_bounds__(64 * W, NT <= 2 ? 2 : 1) void attn_kv4_kernel(AttnArgs a,
+                                                                           const AttnItem* __restrict__ items) {
+  constexpr int DS = HD / 32, DT = HD / 16, BB = kv4_block_bytes(HD), CB = kv4_code_bytes(HD);
+  constexpr int NP = Parts<T>::n;
+  const int gkv = blockIdx.x % a.Hkv;
+  const AttnItem it = items[blockIdx.x / a.Hkv];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int g = lane >> 4, l16 = lane & 15;
+  const int G = a.Hq / a.Hkv;
+  const int M = it.nrows * G;
+  const uint8_t* kp = static_cast<const uint8_t*>(a.kpool);
+  const uint8_t* vp = static_cast<const uint8_t*>(a.vpool);
+  const int32_t* pt = a.page_table + static_cast<size_t>(it.seq) * a.max_pages;
+  __shared__ int32_t s_pt[kStagedPages];
+  const int p0 = it.t0 >> 4;
+  const int np = it.t1 > it.t0 ? ((it.t1 - 1) >> 4) - p0 + 1 : 0;
+  const bool staged = np <= kStagedPages;
+  if (staged)
+    for (int i = threadIdx.x; i < np; i += kWave * W) s_pt[i] = pt[p0 + i];
+  __syncthreads();
+
+  uint4 qf[NT][DS][NP];
+  int vpos[NT];
+  bool vval[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int m = 16 * nt + l16;
+    vval[nt] = m < M;
+    const int mm = vval[nt] ? m : 0;
+    vpos[nt] = it.pos0 + mm / G;
+    const T* base = static_cast<const T*>(a.q) + (static_cast<size_t>(it.row0 + mm / G) * a.Hq + gkv * G + mm % G) * HD + g * 8;
+#pragma unroll
+    for (int s = 0; s < DS; ++s) {
+      if constexpr (NP == 1) {
+        qf[nt][s][0] = vval[nt] ? reinterpret_cast<const uint4*>(base)[4 * s] : make_uint4(0, 0, 0, 0);
+      } else {
+        uint32_t w[4][NP];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 v = reinterpret_cast<const float2*>(base + 32 * s)[j];
+          split_pair<NP>(vval[nt] ? v.x : 0.f, vval[nt] ? v.y : 0.f, w[j]);
+        }
+#pragma unroll
+        for (int i = 0; i < NP; ++i) qf[nt][s][i] = make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]);
+      }
+    }
+  }
+  const float scale = kLog2e / sqrtf(static_cast<float>(HD));
+  const int pos_lo = it.pos0;  // every row of the item sees the keys up to here
+  // the running maximum of the raw scores: subtracted before the scale, so that
+  // the largest score's exponent is 0 whatever its size
+  float mrun[NT], lrun[NT];
+  f32x4 acc[DT][NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    mrun[nt] = -INFINITY;
+    lrun[nt] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  auto walk = [&](auto from_lds) {
+    auto page = [&](int t) -> size_t {
+      if constexpr (decltype(from_lds)::value) return s_pt[(t >> 4) - p0];
+      else return pt[t >> 4];
+    };
+    // codes and scales of one 32-key chunk's operands (keys past t1 clamped to
+    // a valid page; their scores are masked and their V entries zeroed)
+    uint32_t kc[2 * DS], ks[DS / 2];     // [hh][s] (hd 64 too: a lane's 16 bytes hold both key tiles)
+    uint32_t vc[2 * DS], vs[2 * DS];     // [block b][token half]
+    auto load_k = [&](int c0) {
+      const uint8_t* blk = kp + (page(min(c0 + 16 * (l16 >> 3), it.t1 - 1)) * a.Hkv + gkv) * BB;
+      const int j = l16 & 7;
+#pragma unroll
+      for (int i = 0; i < HD / 64; ++i) {
+        const uint4 u = ld_stream(reinterpret_cast<const uint4*>(blk) + (HD == 128 ? (i * 4 + g) * 8 + j : g * 8 + j));
+        kc[4 * i] = u.x; kc[4 * i + 1] = u.y; kc[4 * i + 2] = u.z; kc[4 * i + 3] = u.w;
+      }
+      const uint32_t* sp = reinterpret_cast<const uint32_t*>(blk + CB) + j * (DS / 2);
+#pragma unroll
+      for (int i = 0; i < DS / 2; ++i) ks[i] = sp[i];
+    };
+    auto load_v = [&](int c0) {
+      const uint8_t* blk = vp + (page(min(c0 + 8 * g, it.t1 - 1)) * a.Hkv + gkv) * BB;
+      const int th = g & 1;
+#pragma unroll
+      for (int i = 0; i < HD / 64; ++i) {
+        const uint4 u = ld_stream(reinterpret_cast<const uint4*>(blk) + (i * 2 + th) * 16 + l16);
+        vc[4 * i] = u.x; vc[4 * i + 1] = u.y; vc[4 * i + 2] = u.z; vc[4 * i + 3] = u.w;
+        const uint4 s = *(reinterpret_cast<const uint4*>(blk + CB) + th * (DS / 2) + i);
+        vs[4 * i] = s.x; vs[4 * i + 1] = s.y; vs[4 * i + 2] = s.z; vs[4 * i + 3] = s.w;
+      }
+    };
+    // K operand of key tile hh, step s
+    auto k_op = [&](auto hh_, auto s_) -> uint4 {
+      constexpr int hh = decltype(hh_)::value, s = decltype(s_)::value, n = hh * DS + s;
+      return get8(kc[n], scale_bits<n % 4>(ks[n / 4]));
+    };
+    const int cfirst = it.t0 + 32 * wave;
+    if (cfirst < it.t1) {
+      load_k(cfirst);
+      load_v(cfirst);
+    }
+    for (int c0 = cfirst; c0 < it.t1; c0 += 32 * W) {
+      const int cn = min(c0 + 32 * W, it.t1 - 1);
+      const bool full = c0 + 32 <= it.t1 && c0 + 31 <= pos_lo;  // no masks
+      f32x4 sc[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      auto step = [&](auto s_) {
+        constexpr int s = decltype(s_)::value;
+        if constexpr (s < DS) {
+          const uint4 k0 = k_op(std::integral_constant<int, 0>{}, s_), k1 = k_op(std::integral_constant<int, 1>{}, s_);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+              sc[nt][0] = mfma16x16x32(k0, qf[nt][s][i], sc[nt][0]);
+              sc[nt][1] = mfma16x16x32(k1, qf[nt][s][i], sc[nt][1]);
+            }
+        }
+      };
+      step(std::integral_constant<int, 0>{});
+      step(std::integral_constant<int, 1>{});
+      step(std::integral_constant<int, 2>{});
+      step(std::integral_constant<int, 3>{});
+      load_k(cn);
+      float raw[NT][8], msub[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) raw[nt][j] = (j < 4) ? sc[nt][0][j] : sc[nt][1][j - 4];
+        if (!full) {
+          asm volatile("");  // keeps the masks a branch
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int t = c0 + 8 * g + j;
+            const bool ok = vval[nt] & (t < it.t1) & (t <= vpos[nt]);
+            raw[nt][j] = ok ? raw[nt][j] : -INFINITY;
+          }
+        }
+        float mx = raw[nt][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) mx = fmaxf(mx, raw[nt][j]);
+        if (__any(mx > mrun[nt])) {  // a new maximum: the same in every lane of a query vector
+          mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+          const bool grow = mx > mrun[nt];
+          const float alpha = grow ? ((mrun[nt] == -INFINITY) ? 0.f : exp2f((mrun[nt] - mx) * scale)) : 1.f;
+          if (grow) mrun[nt] = mx;
+          lrun[nt] *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= alpha;
+        }
+        msub[nt] = (mrun[nt] == -INFINITY) ? 0.f : mrun[nt];
+      }
+      uint4 pf[NT][NP];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p[8], ps = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = exp2f((raw[nt][j] - msub[nt]) * scale);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ps += p[j];
+        lrun[nt] += ps;
+        uint32_t w[4][NP];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) split_pair<NP>(p[2 * j], p[2 * j + 1], w[j]);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) pf[nt][i] = make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]);
+      }
+      const bool tail = c0 + 32 > it.t1;
+      const int nvalid = min(max(it.t1 - (c0 + 8 * g), 0), 8);
+#pragma unroll
+      for (int b = 0; b < DS; ++b) {
+        uint4 v[2];
+        get8_tokens(vc[2 * b], vc[2 * b + 1], vs[2 * b], vs[2 * b + 1], v[0], v[1]);
+        if (tail) {  // keys past the end hold anything, and 0 x NaN is not 0
+          asm volatile("");
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            v[i].x = mask_pair(v[i].x, nvalid);
+            v[i].y = mask_pair(v[i].y, nvalid - 2);
+            v[i].z = mask_pair(v[i].z, nvalid - 4);
+            v[i].w = mask_pair(v[i].w, nvalid - 6);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int n = 0; n < NP; ++n) acc[2 * b + i][nt] = mfma16x16x32(v[i], pf[nt][n], acc[2 * b + i][nt]);
+      }
+      load_v(cn);
+    }
+  };
+  if (staged) walk(std::true_type{});
+  else walk(std::false_type{});
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) mrun[nt] *= scale;  // base-2 logits
+  attn_finish<T, HD, NT, W>(a, it, gkv, M, lane, wave, mrun, lrun, acc);
+}
+
+template <typename T, int HD, int NT>
+void launch_items(const AttnArgs& a, const AttnItem* items, int n_items, int w, hipStream_t st) {
+  const dim3 grid(n_items * a.Hkv);
+  if (w >= 4) launch_kernel(attn_kv4_kernel<T, HD, NT, 4>, grid, dim3(4 * kWave), 0, st, a, items);
+  else launch_kernel(attn_kv4_kernel<T, HD, NT, 2>, grid, dim3(2 * kWave), 0, st, a, items);
+}
+
+template <typename T, int HD>
+hipError_t launch_attn(const AttnArgs& a, const AttnItem* items, int n_items, int nt, int w, hipStream_t st) {
+  if (nt <= 1) launch_items<T, HD, 1>(a, items, n_items, w, st);
+  else if (nt == 2) launch_items<T, HD, 2>(a, items, n_items, w, st);
+  else if constexpr (Parts<T>::n == 1)
+    launch_kernel(attn_kv4_kernel<T, HD, 4, 2>, dim3(n_items * a.Hkv), dim3(2 * kWave), 0, st, a, items);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rope_kv4(int dtype, int R, int Hq, int Hkv, int hd, float theta, const float* qkv,
+                           const int32_t* pos, const int32_t* slot, int num_pages, void* q, void* kpool, void* vpool,
+                           hipStream_t st) {
+  if (hd != 64 && hd != 128) return hipErrorInvalidValue;
+  if (R <= 0) return hipSuccess;
+  if (static_cast<size_t>(R) > kMaxGrid256) return hipErrorInvalidValue;
+  auto go = [&](auto* qp) {
+    using T = std::remove_pointer_t<decltype(qp)>;
+    launch_kernel(rope_kv4_kernel<T>, dim3(R), dim3(256), 0, st, Hq, Hkv, hd, theta, qkv, pos, slot, num_pages, qp,
+                  static_cast<uint8_t*>(kpool), static_cast<uint8_t*>(vpool));
+  };
+  if (dtype == 0) go(static_cast<float*>(q));
+  else go(static_cast<bf16_t*>(q));
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_read(int dtype, int R, int Hkv, int hd, const int32_t* slot, int num_pages, const void* kpool,
+                           const void* vpool, void* k, void* v, hipStream_t st) {
+  if (hd != 64 && hd != 128) return hipErrorInvalidValue;
+  if (R <= 0) return hipSuccess;
+  const size_t blocks = (static_cast<size_t>(R) + 15) / 16 * Hkv;
+  if (blocks > kMaxGrid256) return hipErrorInvalidValue;
+  const dim3 grid(static_cast<uint32_t>(blocks));
+  auto go = [&](auto* kd, auto* vd) {
+    using T = std::remove_pointer_t<decltype(kd)>;
+    launch_kernel(kv4_read_kernel<T>, grid, dim3(256), 0, st, R, Hkv, hd, slot, num_pages,
+                  static_cast<const uint8_t*>(kpool), static_cast<const uint8_t*>(vpool), kd, vd);
+  };
+  if (dtype == 0) go(static_cast<float*>(k), static_cast<float*>(v));
+  else go(static_cast<bf16_t*>(k), static_cast<bf16_t*>(v));
+  return hipGetLastError();
+}
+
+hipError_t launch_kv4_expand(int n, const int32_t* src, int Hkv, int hd, const void* kpool, const void* vpool,
+                             void* kdst, void* vdst, hipStream_t st) {
+  if (hd != 64 && hd != 128) return hipErrorInvalidValue;
+  if (n <= 0) return hipSuccess;
+  if (static_cast<size_t>(n) * Hkv > kMaxGrid256) return hipErrorInvalidValue;
+  const auto kernel = hd == 128 ? kv4_expand_kernel<128> : kv4_expand_kernel<64>;
+  launch_kernel(kernel, dim3(n * Hkv), dim3(256), 0, st, src, Hkv, static_cast<const uint8_t*>(kpool),
+                static_cast<const uint8_t*>(vpool), static_cast<bf16_t*>(kdst), static_cast<bf16_t*>(vdst));
+  return hipGetLastError();
+}
+
+hipError_t launch_attention_kv4(const AttnArgs& a, const AttnItem* d_items, int n_items, const AttnGroup* d_groups,
+                                int n_groups, int nt, int w, hipStream_t st) {
+  if (n_items <= 0) return hipSuccess;
+  if (static_cast<size_t>(n_items) * a.Hkv > kMaxGrid256) return hipErrorInvalidValue;
+  if ((a.hd != 64 && a.hd != 128) || nt > kv4_max_nt(a.dtype)) return hipErrorInvalidValue;
+  hipError_t e;
+  if (a.dtype == 0)
+    e = a.hd == 128 ? launch_attn<float, 128>(a, d_items, n_items, nt, w, st)
+                    : launch_attn<float, 64>(a, d_items, n_items, nt, w, st);
+  else
+    e = a.hd == 128 ? launch_attn<bf16_t, 128>(a, d_items, n_items, nt, w, st)
+                    : launch_attn<bf16_t, 64>(a, d_items, n_items, nt, w, st);
+  return e == hipSuccess ? launch_attention_combine(a, d_groups, n_groups, nt, st) : e;
+}
+
+}  // namespace spec

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <exception>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -14,6 +15,9 @@
 #include "elem.h"
 #include "gemm.h"
 #include "host_util.h"
+#include "kv4.h"
+#include "kv4_layout.h"
+#include "logprob.h"
 #include "vocab.h"
 
 using namespace spec;
@@ -21,6 +25,7 @@ using namespace spec;
 namespace {
 
 constexpr int kOpMaxParts = 4096;
+constexpr int kMaxSlotPages = INT32_MAX / kPage;  // a slot (page * 16 + offset) is an int32
 
 std::mutex g_mu;
 Stager& stager() {
@@ -32,6 +37,27 @@ spec_status hip_status(hipError_t e) {
   if (e == hipSuccess) return SPEC_OK;
   if (e == hipErrorInvalidValue) return SPEC_E_UNSUPPORTED;
   return SPEC_E_HIP;
+}
+
+// Refusal of a context-free call, explained by spec_last_error(NULL).
+spec_status refuse(spec_status s, const char* msg) {
+  set_global_error(msg);
+  return s;
+}
+
+bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
+
+// Tables of a call to its workspace.  A stream that is being captured takes
+// only tables that travel in a kernel's arguments, so that a replay finds them.
+spec_status upload_tables(void* ws, const MetaBlock& mb, const char* what, hipStream_t st) {
+  const size_t n = mb.size();
+  if (n > kUploadInline) {
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(st, &cap) != hipSuccess) return refuse(SPEC_E_HIP, what);
+    if (cap != hipStreamCaptureStatusNone) return refuse(SPEC_E_UNSUPPORTED, what);
+  }
+  std::lock_guard<std::mutex> lk(g_mu);
+  return stager().upload(ws, mb.data(), n, st) == hipSuccess ? SPEC_OK : refuse(SPEC_E_HIP, "uploading a call's tables failed");
 }
 
 }  // namespace
@@ -311,6 +337,242 @@ spec_status spec_op_attention(int32_t dtype, int32_t n_seqs, const int32_t* rows
                                             static_cast<int>(plan.groups.size()), plan.nt, plan.w, st));
   return hip_status(launch_attention_f32(a, R, reinterpret_cast<const int32_t*>(ws + ors),
                                          reinterpret_cast<const int32_t*>(ws + orp), st));
+}
+
+// ---------------------------------------------------------------------------
+// token log probabilities
+
+size_t spec_token_logprobs_workspace_bytes(int32_t rows, int32_t V, int32_t n_top) {
+  if (rows <= 0 || V <= 0 || n_top < 0 || n_top > kLogprobMaxTop) return 0;
+  return logprob_ws_bytes(logprob_plan(rows, V, n_top));
+}
+
+spec_status spec_token_logprobs(int32_t rows, int32_t V, const float* logits, int64_t row_stride,
+                                const float* temperature, const int32_t* tokens, int32_t n_top, float* logprobs,
+                                float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  if (rows < 0 || V <= 0 || row_stride < V) return refuse(SPEC_E_INVALID, "spec_token_logprobs: need rows >= 0, V > 0, row_stride >= V");
+  if (n_top < 0 || n_top > kLogprobMaxTop || n_top > V)
+    return refuse(SPEC_E_INVALID, "spec_token_logprobs: need 0 <= n_top <= min(64, V)");
+  if (rows == 0) return SPEC_OK;
+  if (!logits || !workspace || (logprobs && !tokens) || (n_top > 0 && (!top_ids || !top_logprobs)))
+    return refuse(SPEC_E_INVALID, "spec_token_logprobs: null pointer");
+  if (misaligned(logits, 4) || misaligned(workspace, 16))
+    return refuse(SPEC_E_INVALID, "spec_token_logprobs: misaligned logits or workspace");
+  const LogprobPlan p = logprob_plan(rows, V, n_top);
+  if (workspace_bytes < logprob_ws_bytes(p)) return refuse(SPEC_E_INVALID, "spec_token_logprobs: workspace too small");
+  return hip_status(launch_logprobs(p, logits, row_stride, temperature, tokens, logprobs, entropy, top_ids,
+                                    top_logprobs, workspace, static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------------------------------------
+// cache pages
+
+size_t spec_op_kv_copy_pages_workspace_bytes(int32_t n) { return n <= 0 ? 0 : align_up(sizeof(int2) * n); }
+
+spec_status spec_op_kv_copy_pages(int32_t n_planes, int32_t num_pages, size_t page_bytes, void* pool, int32_t n,
+                                  const int32_t* src_pages, const int32_t* dst_pages, void* workspace,
+                                  size_t workspace_bytes, void* stream) try {
+  if (n_planes < 0 || num_pages < 0 || n < 0) return refuse(SPEC_E_INVALID, "spec_op_kv_copy_pages: negative size");
+  if (n == 0 || n_planes == 0) return SPEC_OK;
+  if (!pool || !src_pages || !dst_pages || !workspace) return refuse(SPEC_E_INVALID, "spec_op_kv_copy_pages: null pointer");
+  if (page_bytes == 0 || page_bytes % 16 || n_planes > 65535)
+    return refuse(SPEC_E_UNSUPPORTED, "spec_op_kv_copy_pages: page_bytes must be a multiple of 16, n_planes at most 65535");
+  if (misaligned(pool, 16) || misaligned(workspace, 16) || workspace_bytes < spec_op_kv_copy_pages_workspace_bytes(n))
+    return refuse(SPEC_E_INVALID, "spec_op_kv_copy_pages: misaligned pool or workspace, or workspace too small");
+  std::vector<uint64_t> is_dst((static_cast<size_t>(num_pages) + 63) / 64, 0);
+  std::vector<int2> pairs(n);
+  for (int i = 0; i < n; ++i) {
+    const int32_t s = src_pages[i], d = dst_pages[i];
+    if (s < 0 || s >= num_pages || d < 0 || d >= num_pages)
+      return refuse(SPEC_E_INVALID, "spec_op_kv_copy_pages: page outside the pool");
+    if (is_dst[d / 64] >> (d % 64) & 1) return refuse(SPEC_E_INVALID, "spec_op_kv_copy_pages: a page is a destination twice");
+    is_dst[d / 64] |= uint64_t{1} << (d % 64);
+    pairs[i] = make_int2(s, d);
+  }
+  for (int i = 0; i < n; ++i)
+    if (is_dst[src_pages[i] / 64] >> (src_pages[i] % 64) & 1)
+      return refuse(SPEC_E_INVALID, "spec_op_kv_copy_pages: a destination is also a source");
+  MetaBlock mb;
+  mb.add(pairs);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const spec_status s = upload_tables(workspace, mb, "spec_op_kv_copy_pages: more pairs than a captured call takes", st);
+  if (s != SPEC_OK) return s;
+  return hip_status(launch_kv_copy_pages(static_cast<const int2*>(workspace), n, pool, n_planes, num_pages, page_bytes, st));
+} catch (const std::exception&) {
+  return refuse(SPEC_E_UNSUPPORTED, "spec_op_kv_copy_pages: out of host memory");
+}
+
+// ---------------------------------------------------------------------------
+// the 4-bit cache
+
+size_t spec_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim) {
+  if (n_kv_heads <= 0 || (head_dim != 64 && head_dim != 128)) return 0;
+  return static_cast<size_t>(n_kv_heads) * kv4_block_bytes(head_dim);
+}
+
+spec_status spec_op_rope_kv4(int32_t dtype, int32_t R, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                             float theta, const float* qkv, const int32_t* pos, const int32_t* slot,
+                             int32_t num_pages, void* q_out, void* k_pages, void* v_pages, void* stream) {
+  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || R < 0 || n_heads <= 0 || n_kv_heads <= 0 || !(theta > 0.f) ||
+      num_pages < 0 || num_pages > kMaxSlotPages)
+    return refuse(SPEC_E_INVALID, "spec_op_rope_kv4: bad dtype or size");
+  if (head_dim != 64 && head_dim != 128) return refuse(SPEC_E_UNSUPPORTED, "spec_op_rope_kv4: head_dim must be 64 or 128");
+  if (R == 0) return SPEC_OK;
+  if (!qkv || !pos || !slot || !q_out || (num_pages > 0 && (!k_pages || !v_pages)))
+    return refuse(SPEC_E_INVALID, "spec_op_rope_kv4: null pointer");
+  if (misaligned(qkv, 16) || misaligned(q_out, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16))
+    return refuse(SPEC_E_INVALID, "spec_op_rope_kv4: qkv, q_out and the pages must be 16-byte aligned");
+  return hip_status(launch_rope_kv4(dtype == SPEC_F32 ? 0 : 1, R, n_heads, n_kv_heads, head_dim, theta, qkv, pos, slot,
+                                    num_pages, q_out, k_pages, v_pages, static_cast<hipStream_t>(stream)));
+}
+
+spec_status spec_op_kv4_read(int32_t dtype, int32_t R, int32_t n_kv_heads, int32_t head_dim, const int32_t* slot,
+                             int32_t num_pages, const void* k_pages, const void* v_pages, void* k_out, void* v_out,
+                             void* stream) {
+  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || R < 0 || n_kv_heads <= 0 || num_pages < 0 ||
+      num_pages > kMaxSlotPages)
+    return refuse(SPEC_E_INVALID, "spec_op_kv4_read: bad dtype or size");
+  if (head_dim != 64 && head_dim != 128) return refuse(SPEC_E_UNSUPPORTED, "spec_op_kv4_read: head_dim must be 64 or 128");
+  if (R == 0 || num_pages == 0) return SPEC_OK;
+  if (!slot || !k_pages || !v_pages || !k_out || !v_out) return refuse(SPEC_E_INVALID, "spec_op_kv4_read: null pointer");
+  if (misaligned(k_pages, 16) || misaligned(v_pages, 16) || misaligned(k_out, 16) || misaligned(v_out, 16))
+    return refuse(SPEC_E_INVALID, "spec_op_kv4_read: the pages and outputs must be 16-byte aligned");
+  return hip_status(launch_kv4_read(dtype == SPEC_F32 ? 0 : 1, R, n_kv_heads, head_dim, slot, num_pages, k_pages,
+                                    v_pages, k_out, v_out, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+// One spec_op_attention_kv4 call: its work and the layout of its workspace.
+struct Kv4Call {
+  spec_status status = SPEC_E_INVALID;
+  const char* why = "";
+  int R = 0;
+  int64_t pages = 0;  // of all sequences (expanded form)
+  AttnPlan plan;
+  size_t tables = 0, o_part = 0, o_ml = 0, o_k = 0, o_v = 0, bytes = 0;
+};
+
+Kv4Call kv4_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32_t* pos0, int32_t max_pages,
+                 int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
+  Kv4Call c;
+  auto fail = [&](spec_status s, const char* why) {
+    c.status = s;
+    c.why = why;
+    return c;
+  };
+  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || n_seqs < 0 || max_pages <= 0 || n_heads <= 0 || n_kv_heads <= 0 ||
+      n_heads % n_kv_heads)
+    return fail(SPEC_E_INVALID, "spec_op_attention_kv4: bad dtype or size");
+  const int G = n_heads / n_kv_heads, dt = dtype == SPEC_F32 ? 0 : 1;
+  if (head_dim != 64 && head_dim != 128) return fail(SPEC_E_UNSUPPORTED, "spec_op_attention_kv4: head_dim must be 64 or 128");
+  if (G > 16 * kv4_max_nt(dt))
+    return fail(SPEC_E_UNSUPPORTED, "spec_op_attention_kv4: more query heads per kv head than a tile holds (64 for bf16, 32 for fp32)");
+  if (n_seqs > 0 && (!rows || !pos0)) return fail(SPEC_E_INVALID, "spec_op_attention_kv4: null pointer");
+  std::vector<AttnSegment> segs;
+  int64_t R = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    const int64_t len = static_cast<int64_t>(pos0[i]) + rows[i];
+    if (rows[i] < 0 || pos0[i] < 0 || len > INT32_MAX || (len + 15) / 16 > max_pages)
+      return fail(SPEC_E_INVALID, "spec_op_attention_kv4: rows beyond the page table, or a negative length");
+    if (R + rows[i] > INT32_MAX) return fail(SPEC_E_INVALID, "spec_op_attention_kv4: too many rows");
+    if (rows[i] > 0) segs.push_back(AttnSegment{i, static_cast<int32_t>(R), rows[i], pos0[i]});
+    if (rows[i] > 0) c.pages += (len + 15) / 16;
+    R += rows[i];
+  }
+  c.R = static_cast<int>(R);
+  c.status = SPEC_OK;
+  if (R == 0) return c;
+  c.plan = plan_attention(segs, G, n_kv_heads, kOpMaxParts, kAttnTargetWgs, dt == 1, kv4_max_nt(dt));
+  c.tables = align_up(sizeof(int32_t) * static_cast<size_t>(n_seqs) * max_pages) +
+             align_up(sizeof(AttnItem) * c.plan.items.size()) + align_up(sizeof(AttnGroup) * c.plan.groups.size()) +
+             (c.plan.prefill ? align_up(sizeof(int32_t) * c.pages) : 0);
+  c.o_part = c.tables;
+  c.o_ml = c.o_part + align_up(sizeof(float) * static_cast<size_t>(c.plan.n_parts) * n_kv_heads * 64 * head_dim);
+  c.o_k = c.o_ml + align_up(sizeof(float) * static_cast<size_t>(c.plan.n_parts) * n_kv_heads * 64 * 2);
+  const size_t pool = c.plan.prefill ? align_up(size_t{2} * c.pages * n_kv_heads * 16 * head_dim) : 0;
+  c.o_v = c.o_k + pool;
+  c.bytes = c.o_v + pool;
+  return c;
+}
+
+}  // namespace
+
+size_t spec_op_attention_kv4_workspace_bytes(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32_t* pos0,
+                                             int32_t max_pages, int32_t n_heads, int32_t n_kv_heads,
+                                             int32_t head_dim) try {
+  const Kv4Call c = kv4_call(dtype, n_seqs, rows, pos0, max_pages, n_heads, n_kv_heads, head_dim);
+  if (c.status != SPEC_OK) set_global_error(c.why);
+  return c.status == SPEC_OK ? c.bytes : 0;
+} catch (const std::exception&) {
+  set_global_error("spec_op_attention_kv4: out of host memory");
+  return 0;
+}
+
+spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32_t* pos0,
+                                  const int32_t* page_table, int32_t max_pages, int32_t num_pages, int32_t n_heads,
+                                  int32_t n_kv_heads, int32_t head_dim, const void* q, const void* k_pages,
+                                  const void* v_pages, void* out, void* workspace, size_t workspace_bytes,
+                                  void* stream) try {
+  Kv4Call c = kv4_call(dtype, n_seqs, rows, pos0, max_pages, n_heads, n_kv_heads, head_dim);
+  if (c.status != SPEC_OK) return refuse(c.status, c.why);
+  if (c.R == 0) return SPEC_OK;
+  if (!page_table || !q || !k_pages || !v_pages || !out || !workspace)
+    return refuse(SPEC_E_INVALID, "spec_op_attention_kv4: null pointer");
+  if (misaligned(q, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16) || misaligned(out, 16) ||
+      misaligned(workspace, 256) || workspace_bytes < c.bytes)
+    return refuse(SPEC_E_INVALID,
+                  "spec_op_attention_kv4: buffers must be 16-byte aligned, the workspace 256-byte aligned and large enough");
+  // the pages that the call reads, compact where they are expanded
+  std::vector<int32_t> table(static_cast<size_t>(n_seqs) * max_pages, 0), src;
+  for (int i = 0; i < n_seqs; ++i) {
+    const int n = rows[i] > 0 ? static_cast<int>((static_cast<int64_t>(pos0[i]) + rows[i] + 15) / 16) : 0;
+    for (int j = 0; j < n; ++j) {
+      const size_t e = static_cast<size_t>(i) * max_pages + j;
+      const int32_t p = page_table[e];
+      if (p < 0 || p >= num_pages) return refuse(SPEC_E_INVALID, "spec_op_attention_kv4: page outside the pool");
+      if (c.plan.prefill) {
+        table[e] = static_cast<int32_t>(src.size());
+        src.push_back(p);
+      } else {
+        table[e] = p;
+      }
+    }
+  }
+  MetaBlock mb;
+  const size_t opt = mb.add(table), oit = mb.add(c.plan.items), ogr = mb.add(c.plan.groups), osr = mb.add(src);
+  char* ws = static_cast<char*>(workspace);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const spec_status s = upload_tables(ws, mb, "spec_op_attention_kv4: larger tables than a captured call takes", st);
+  if (s != SPEC_OK) return s;
+  AttnArgs a;
+  a.dtype = dtype == SPEC_F32 ? 0 : 1;
+  a.Hq = n_heads;
+  a.Hkv = n_kv_heads;
+  a.hd = head_dim;
+  a.q = q;
+  a.kpool = k_pages;
+  a.vpool = v_pages;
+  a.page_table = reinterpret_cast<const int32_t*>(ws + opt);
+  a.max_pages = max_pages;
+  a.out = out;
+  a.part_o = reinterpret_cast<float*>(ws + c.o_part);
+  a.part_ml = reinterpret_cast<float*>(ws + c.o_ml);
+  const AttnItem* items = reinterpret_cast<const AttnItem*>(ws + oit);
+  const int n_items = static_cast<int>(c.plan.items.size());
+  if (c.plan.prefill) {
+    const hipError_t e = launch_kv4_expand(static_cast<int>(src.size()), reinterpret_cast<const int32_t*>(ws + osr),
+                                           n_kv_heads, head_dim, k_pages, v_pages, ws + c.o_k, ws + c.o_v, st);
+    if (e != hipSuccess) return hip_status(e);
+    a.kpool = ws + c.o_k;
+    a.vpool = ws + c.o_v;
+    return hip_status(launch_attention_prefill_bf16(a, items, n_items, c.plan.few_keys, st, true));
+  }
+  return hip_status(launch_attention_kv4(a, items, n_items, reinterpret_cast<const AttnGroup*>(ws + ogr),
+                                         static_cast<int>(c.plan.groups.size()), c.plan.nt, c.plan.w, st));
+} catch (const std::exception&) {
+  return refuse(SPEC_E_UNSUPPORTED, "spec_op_attention_kv4: out of host memory");
 }
 
 }  // extern "C"

@@ -7,7 +7,7 @@
 namespace spec {
 
 AttnPlan plan_attention(const std::vector<AttnSegment>& segs, int G, int Hkv, int max_parts,
-                        int target_wgs, bool allow_prefill) {
+                        int target_wgs, bool allow_prefill, int max_nt) {
   AttnPlan p;
   int max_rows = 1, min_rows = 1 << 30;
   for (const auto& s : segs) {
@@ -33,7 +33,7 @@ AttnPlan plan_attention(const std::vector<AttnSegment>& segs, int G, int Hkv, in
     return p;
   }
   // query vectors per tile: rows * G <= 16 * nt, nt in {1, 2, 4}
-  const int want = std::min(max_rows * G, 64);
+  const int want = std::min(max_rows * G, 16 * max_nt);
   p.nt = want <= 16 ? 1 : (want <= 32 ? 2 : 4);
   // One sequence (a batch-1 verify, draft step or tree verify: a few MB of
   // keys and values, latency-bound): twice the items with half the query
