@@ -143,6 +143,8 @@ def lib():
 # marshalling helpers
 
 def _i32(a) -> np.ndarray:
+    if type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous:
+        return a
     return np.ascontiguousarray(np.asarray(a, dtype=np.int32))
 
 
@@ -169,8 +171,10 @@ def dptr(t) -> Optional[int]:
 
 def stream_ptr(stream=None) -> Optional[int]:
     import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # 0.1 us; the Stream object takes 2.7
+    return raw(torch.cuda.current_device()) if raw else torch.cuda.current_stream().cuda_stream
 
 
 def check(status: int, ctx=None):
@@ -441,14 +445,13 @@ def spec_op_attention(dtype: int, rows, pos0, page_table, n_heads: int, n_kv_hea
 # Calls that take their sizes from tensors: each checks the tensors' device,
 # type, layout and element count against what the library will touch.
 
-def _dev(t, dtypes, numel: int, what: str) -> Optional[int]:
-    """Address of a contiguous tensor on the current device with at least numel elements of one of dtypes."""
-    import torch
+def _dev(t, dtype, numel: int, what: str, gpu: int) -> Optional[int]:
+    """Address of a contiguous tensor on GPU `gpu` with at least numel elements of dtype (None: of any)."""
     if t is None:
         return None
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    if t.get_device() != gpu:
         raise ValueError(f"{what}: not on the current GPU")
-    if dtypes is not None and t.dtype not in dtypes:
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{what}: type {t.dtype}")
     if not t.is_contiguous() or t.numel() < numel:
         raise ValueError(f"{what}: needs {numel} contiguous elements")
@@ -457,7 +460,11 @@ def _dev(t, dtypes, numel: int, what: str) -> Optional[int]:
 
 def _elem(dtype: int):
     import torch
-    return (torch.float32,) if dtype == SPEC_F32 else (torch.bfloat16,)
+    return torch.float32 if dtype == SPEC_F32 else torch.bfloat16
+
+
+def _host(a: np.ndarray) -> int:
+    return a.__array_interface__["data"][0]
 
 
 def spec_token_logprobs_workspace_bytes(rows: int, V: int, n_top: int) -> int:
@@ -468,22 +475,24 @@ def spec_token_logprobs(logits, temperature, tokens, logprobs, entropy, top_ids,
     """logits fp32 [rows, V] (rows may be strided), temperature fp32 [rows] or None, tokens int32 [rows] or
     None; logprobs, entropy fp32 [rows] or None; top_ids int32, top_logprobs fp32 [rows, n_top] or None."""
     import torch
-    f32, i32 = (torch.float32,), (torch.int32,)
-    if logits.dim() != 2 or logits.stride(1) != 1 or logits.dtype != torch.float32:
+    f32, i32 = torch.float32, torch.int32
+    if logits.dim() != 2 or logits.stride(1) != 1 or logits.dtype is not f32:
         raise ValueError("logits: fp32 [rows, V] with unit stride along the vocabulary")
-    if not logits.is_cuda or logits.device.index != torch.cuda.current_device():
+    if not logits.is_cuda or logits.get_device() != torch.cuda.current_device():
         raise ValueError("logits: not on the current GPU")
+    gpu = logits.get_device()
     R, V = logits.shape
+    ld = logits.stride(0) if R > 1 else V
+    if ld < V:
+        raise ValueError("logits: rows overlap")
     n = 0 if top_ids is None else top_ids.shape[1]
     if (top_ids is None) != (top_logprobs is None) or (n and top_logprobs.shape[1] != n):
         raise ValueError("top_ids and top_logprobs go together, [rows, n_top] both")
-    ld = max(logits.stride(0), V) if R > 1 else V
-    if R > 1 and logits.stride(0) < V:
-        raise ValueError("logits: rows overlap")
     check(lib().spec_token_logprobs(
-        R, V, logits.data_ptr(), ld, _dev(temperature, f32, R, "temperature"), _dev(tokens, i32, R, "tokens"), n,
-        _dev(logprobs, f32, R, "logprobs"), _dev(entropy, f32, R, "entropy"), _dev(top_ids, i32, R * n, "top_ids"),
-        _dev(top_logprobs, f32, R * n, "top_logprobs"), _dev(workspace, None, 0, "workspace"),
+        R, V, logits.data_ptr(), ld, _dev(temperature, f32, R, "temperature", gpu),
+        _dev(tokens, i32, R, "tokens", gpu), n, _dev(logprobs, f32, R, "logprobs", gpu),
+        _dev(entropy, f32, R, "entropy", gpu), _dev(top_ids, i32, R * n, "top_ids", gpu),
+        _dev(top_logprobs, f32, R * n, "top_logprobs", gpu), _dev(workspace, None, 0, "workspace", gpu),
         workspace.numel() * workspace.element_size(), stream_ptr(stream)))
 
 
@@ -493,15 +502,16 @@ def spec_op_kv_copy_pages_workspace_bytes(n: int) -> int:
 
 def spec_op_kv_copy_pages(pool, src_pages, dst_pages, workspace, stream=None):
     """pool [n_planes, num_pages, ...]: page dst_pages[i] of every plane <- page src_pages[i]."""
+    import torch
     src, dst = _i32(src_pages), _i32(dst_pages)
     if src.ndim != 1 or src.shape != dst.shape:
         raise ValueError("src_pages and dst_pages: one list each, of one length")
     if pool.dim() < 3:
         raise ValueError("pool: [n_planes, num_pages, page]")
     planes, pages = pool.shape[:2]
-    page_bytes = pool[0, 0].numel() * pool.element_size() if planes and pages else 0
-    check(lib().spec_op_kv_copy_pages(planes, pages, page_bytes, _dev(pool, None, 0, "pool"), len(src),
-                                      src.ctypes.data, dst.ctypes.data, _dev(workspace, None, 0, "workspace"),
+    page_bytes, gpu = pool.stride(1) * pool.element_size(), torch.cuda.current_device()
+    check(lib().spec_op_kv_copy_pages(planes, pages, page_bytes, _dev(pool, None, 0, "pool", gpu), len(src),
+                                      _host(src), _host(dst), _dev(workspace, None, 0, "workspace", gpu),
                                       workspace.numel() * workspace.element_size(), stream_ptr(stream)))
 
 
@@ -509,32 +519,29 @@ def spec_kv4_page_bytes(n_kv_heads: int, head_dim: int) -> int:
     return lib().spec_kv4_page_bytes(n_kv_heads, head_dim)
 
 
-def _kv4_pages(t, num_pages: int, n_kv_heads: int, head_dim: int, what: str) -> Optional[int]:
-    import torch
-    return _dev(t, (torch.uint8,), num_pages * spec_kv4_page_bytes(n_kv_heads, head_dim), what)
-
-
 def spec_op_rope_kv4(dtype: int, R: int, n_heads: int, n_kv_heads: int, head_dim: int, theta: float, qkv, pos, slot,
                      num_pages: int, q_out, k_pages, v_pages, stream=None):
     import torch
-    check(lib().spec_op_rope_kv4(
+    gpu, L = torch.cuda.current_device(), lib()
+    pool = num_pages * L.spec_kv4_page_bytes(n_kv_heads, head_dim)
+    check(L.spec_op_rope_kv4(
         dtype, R, n_heads, n_kv_heads, head_dim, theta,
-        _dev(qkv, (torch.float32,), R * (n_heads + 2 * n_kv_heads) * head_dim, "qkv"),
-        _dev(pos, (torch.int32,), R, "pos"), _dev(slot, (torch.int32,), R, "slot"), num_pages,
-        _dev(q_out, _elem(dtype), R * n_heads * head_dim, "q_out"),
-        _kv4_pages(k_pages, num_pages, n_kv_heads, head_dim, "k_pages"),
-        _kv4_pages(v_pages, num_pages, n_kv_heads, head_dim, "v_pages"), stream_ptr(stream)))
+        _dev(qkv, torch.float32, R * (n_heads + 2 * n_kv_heads) * head_dim, "qkv", gpu),
+        _dev(pos, torch.int32, R, "pos", gpu), _dev(slot, torch.int32, R, "slot", gpu), num_pages,
+        _dev(q_out, _elem(dtype), R * n_heads * head_dim, "q_out", gpu),
+        _dev(k_pages, torch.uint8, pool, "k_pages", gpu), _dev(v_pages, torch.uint8, pool, "v_pages", gpu),
+        stream_ptr(stream)))
 
 
 def spec_op_kv4_read(dtype: int, R: int, n_kv_heads: int, head_dim: int, slot, num_pages: int, k_pages, v_pages,
                      k_out, v_out, stream=None):
     import torch
-    n = R * n_kv_heads * head_dim
-    check(lib().spec_op_kv4_read(
-        dtype, R, n_kv_heads, head_dim, _dev(slot, (torch.int32,), R, "slot"), num_pages,
-        _kv4_pages(k_pages, num_pages, n_kv_heads, head_dim, "k_pages"),
-        _kv4_pages(v_pages, num_pages, n_kv_heads, head_dim, "v_pages"), _dev(k_out, _elem(dtype), n, "k_out"),
-        _dev(v_out, _elem(dtype), n, "v_out"), stream_ptr(stream)))
+    gpu, L = torch.cuda.current_device(), lib()
+    n, pool, el = R * n_kv_heads * head_dim, num_pages * L.spec_kv4_page_bytes(n_kv_heads, head_dim), _elem(dtype)
+    check(L.spec_op_kv4_read(
+        dtype, R, n_kv_heads, head_dim, _dev(slot, torch.int32, R, "slot", gpu), num_pages,
+        _dev(k_pages, torch.uint8, pool, "k_pages", gpu), _dev(v_pages, torch.uint8, pool, "v_pages", gpu),
+        _dev(k_out, el, n, "k_out", gpu), _dev(v_out, el, n, "v_out", gpu), stream_ptr(stream)))
 
 
 def spec_op_attention_kv4_workspace_bytes(dtype: int, rows, pos0, max_pages: int, n_heads: int, n_kv_heads: int,
@@ -542,18 +549,20 @@ def spec_op_attention_kv4_workspace_bytes(dtype: int, rows, pos0, max_pages: int
     r, p = _i32(rows), _i32(pos0)
     if r.ndim != 1 or r.shape != p.shape:
         raise ValueError("rows and pos0: one list each, of one length")
-    return lib().spec_op_attention_kv4_workspace_bytes(dtype, len(r), r.ctypes.data, p.ctypes.data, max_pages,
-                                                       n_heads, n_kv_heads, head_dim)
+    return lib().spec_op_attention_kv4_workspace_bytes(dtype, len(r), _host(r), _host(p), max_pages, n_heads,
+                                                       n_kv_heads, head_dim)
 
 
 def spec_op_attention_kv4(dtype: int, rows, pos0, page_table, num_pages: int, n_heads: int, n_kv_heads: int,
                           head_dim: int, q, k_pages, v_pages, out, workspace, stream=None):
+    import torch
     r, p, pt = _i32(rows), _i32(pos0), _i32(page_table)
     if r.ndim != 1 or r.shape != p.shape or pt.ndim != 2 or len(pt) != len(r):
         raise ValueError("rows and pos0: one list each, page_table: one row of page ids for each sequence")
-    n = int(r.sum()) * n_heads * head_dim
-    check(lib().spec_op_attention_kv4(
-        dtype, len(r), r.ctypes.data, p.ctypes.data, pt.ctypes.data, pt.shape[1], num_pages, n_heads, n_kv_heads,
-        head_dim, _dev(q, _elem(dtype), n, "q"), _kv4_pages(k_pages, num_pages, n_kv_heads, head_dim, "k_pages"),
-        _kv4_pages(v_pages, num_pages, n_kv_heads, head_dim, "v_pages"), _dev(out, _elem(dtype), n, "out"),
-        _dev(workspace, None, 0, "workspace"), workspace.numel() * workspace.element_size(), stream_ptr(stream)))
+    gpu, L = torch.cuda.current_device(), lib()
+    n, pool, el = sum(r.tolist()) * n_heads * head_dim, num_pages * L.spec_kv4_page_bytes(n_kv_heads, head_dim), _elem(dtype)
+    check(L.spec_op_attention_kv4(
+        dtype, len(r), _host(r), _host(p), _host(pt), pt.shape[1], num_pages, n_heads, n_kv_heads, head_dim,
+        _dev(q, el, n, "q", gpu), _dev(k_pages, torch.uint8, pool, "k_pages", gpu),
+        _dev(v_pages, torch.uint8, pool, "v_pages", gpu), _dev(out, el, n, "out", gpu),
+        _dev(workspace, None, 0, "workspace", gpu), workspace.numel() * workspace.element_size(), stream_ptr(stream)))

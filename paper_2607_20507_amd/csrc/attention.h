@@ -45,11 +45,6 @@ struct AttnArgs {
 hipError_t launch_attention_bf16(const AttnArgs& a, const AttnItem* d_items, int n_items,
                                  const AttnGroup* d_groups, int n_groups, int nt, int w, hipStream_t st);
 
-// Merges the partials of split items into the output (element type a.dtype),
-// parts in index order; nt as the items' launch.
-hipError_t launch_attention_combine(const AttnArgs& a, const AttnGroup* d_groups, int n_groups, int nt,
-                                    hipStream_t st);
-
 // bf16 causal prefill: items from plan_attention's prefill form (blocks of
 // 256 / G consecutive rows of one sequence against keys 0 .. t1 - 1, t0 = 0,
 // part < 0), heaviest first; grid n_items x Hkv (kv head = block % Hkv).

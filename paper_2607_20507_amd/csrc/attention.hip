@@ -27,7 +27,6 @@
 #include <type_traits>
 
 #include "attention.h"
-#include "attn_finish.h"
 #include "common.h"
 
 namespace spec {
@@ -35,6 +34,11 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kAttnStagedPages = 256;  // page ids of one work item kept in LDS (4096 keys)
+
+__device__ __forceinline__ uint32_t mask_pair(uint32_t w, int valid) {
+  // keep the first `valid` (0, 1, 2) bf16 halves of a 32-bit word
+  return valid >= 2 ? w : (valid == 1 ? (w & 0xFFFFu) : 0u);
+}
 
 // W waves per workgroup share one work item: wave w takes the 32-key chunks
 // w, w + W, ... of the item's key range, and the waves' softmax states are
@@ -247,7 +251,81 @@ __device__ __forceinline__ void attn_bf16_body(const AttnArgs& a, const AttnItem
   if (staged) walk(std::true_type{});
   else walk(std::false_type{});
 
-  attn_finish<bf16_t, HD, NT, W>(a, it, gkv, M, lane, wave, mrun, lrun, acc);
+  float ltot[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float lt = lrun[nt];
+    lt += __shfl_xor(lt, 16, kWave);
+    lt += __shfl_xor(lt, 32, kWave);
+    ltot[nt] = lt;
+  }
+  if (W > 1) {
+    // waves 1..W-1 hand their state to wave 0 (same lane layout in every wave)
+    __shared__ float s_acc[W > 1 ? W - 1 : 1][NT][DT][4][kWave];
+    __shared__ float s_ml[W > 1 ? W - 1 : 1][NT][2][kWave];
+    if (wave > 0) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        s_ml[wave - 1][nt][0][lane] = mrun[nt];
+        s_ml[wave - 1][nt][1][lane] = ltot[nt];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s_acc[wave - 1][nt][dt][r][lane] = acc[dt][nt][r];
+      }
+    }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float mm = mrun[nt];
+      for (int w = 0; w < W - 1; ++w) mm = fmaxf(mm, s_ml[w][nt][0][lane]);
+      if (mm == -INFINITY) continue;  // no key of the item for this query vector
+      const float e0 = (mrun[nt] == -INFINITY) ? 0.f : exp2f(mrun[nt] - mm);
+      float lt = ltot[nt] * e0;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= e0;
+      for (int w = 0; w < W - 1; ++w) {
+        const float mw = s_ml[w][nt][0][lane];
+        const float ew = (mw == -INFINITY) ? 0.f : exp2f(mw - mm);
+        lt += ew * s_ml[w][nt][1][lane];
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[dt][nt][r] += ew * s_acc[w][nt][dt][r][lane];
+      }
+      mrun[nt] = mm;
+      ltot[nt] = lt;
+    }
+  }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const float lt = ltot[nt];
+    const int m = 16 * nt + l16;
+    if (m >= M) continue;
+    if (it.part < 0) {
+      const float inv = (lt > 0.f) ? 1.f / lt : 0.f;
+      bf16_t* o = static_cast<bf16_t*>(a.out) +
+                  (static_cast<size_t>(it.row0 + m / G) * a.Hq + gkv * G + m % G) * HD;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const f32x4 v = acc[dt][nt];
+        *reinterpret_cast<uint2*>(o + 16 * dt + 4 * g) =
+            make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
+      }
+    } else {
+      const size_t pm = static_cast<size_t>(it.part * a.Hkv + gkv) * 64 + m;
+      float* po = a.part_o + pm * HD;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        *reinterpret_cast<float4*>(po + 16 * dt + 4 * g) =
+            make_float4(acc[dt][nt][0], acc[dt][nt][1], acc[dt][nt][2], acc[dt][nt][3]);
+      if (g == 0) {
+        a.part_ml[pm * 2] = mrun[nt];
+        a.part_ml[pm * 2 + 1] = lt;
+      }
+    }
+  }
 }
 
 // One workgroup per (group, kv head, 4 query vectors), one thread per (query
@@ -623,7 +701,7 @@ __global__ __launch_bounds__(512, 1) void attn_prefill_far_bf16_kernel(AttnArgs 
   attn_prefill_body<HD, SHORT, true>(a, items);
 }
 
-template <typename T, int HD, int DPT>
+template <int HD, int DPT>
 __global__ __launch_bounds__(HD / DPT * kCombineQv) void attn_combine_kernel(AttnArgs a,
                                                                               const AttnGroup* __restrict__ groups) {
   constexpr int TQ = HD / DPT;  // threads per query vector
@@ -693,12 +771,12 @@ __global__ __launch_bounds__(HD / DPT * kCombineQv) void attn_combine_kernel(Att
   }
   const size_t o = (static_cast<size_t>(gr.row0 + m / G) * a.Hq + gkv * G + m % G) * HD + d0;
   const bool ok = den > 0.f;
-  T* out = static_cast<T*>(a.out) + o;
+  bf16_t* out = static_cast<bf16_t*>(a.out) + o;
   if constexpr (DPT == 4) {
-    attn_store4(out, f32x4{ok ? num[0] / den : 0.f, ok ? num[1] / den : 0.f, ok ? num[2] / den : 0.f,
-                           ok ? num[3] / den : 0.f});
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(ok ? num[0] / den : 0.f, ok ? num[1] / den : 0.f),
+                                                pack_bf16x2(ok ? num[2] / den : 0.f, ok ? num[3] / den : 0.f));
   } else {
-    out[0] = Elem<T>::from_f32(ok ? num[0] / den : 0.f);
+    out[0] = f32_to_bf16(ok ? num[0] / den : 0.f);
   }
 }
 
@@ -818,32 +896,15 @@ hipError_t launch_bf16_hd(const AttnArgs& a, const AttnItem* items, int n_items,
     else if (nt == 2) launch_item_kernel<HD, 2>(a, items, grid, w, st);
     else launch_item_kernel<HD, 4>(a, items, grid, std::min(w, 2), st);
   }
-  if (n_groups > 0) return launch_attention_combine(a, groups, n_groups, nt, st);
-  return hipGetLastError();
-}
-
-template <typename T, int HD>
-void launch_combine_hd(const AttnArgs& a, const AttnGroup* groups, int n_groups, int nt, hipStream_t st) {
-  constexpr int DPT = HD == 128 ? 4 : 1;
-  attn_combine_kernel<T, HD, DPT><<<dim3(n_groups, a.Hkv, 16 * nt / kCombineQv), HD / DPT * kCombineQv, 0, st>>>(
-      a, groups);
-}
-
-}  // namespace
-
-hipError_t launch_attention_combine(const AttnArgs& a, const AttnGroup* d_groups, int n_groups, int nt,
-                                    hipStream_t st) {
-  if (n_groups <= 0) return hipSuccess;
-  if (a.hd != 64 && a.hd != 128) return hipErrorInvalidValue;
-  if (a.dtype == 0) {
-    if (a.hd == 128) launch_combine_hd<float, 128>(a, d_groups, n_groups, nt, st);
-    else launch_combine_hd<float, 64>(a, d_groups, n_groups, nt, st);
-  } else {
-    if (a.hd == 128) launch_combine_hd<bf16_t, 128>(a, d_groups, n_groups, nt, st);
-    else launch_combine_hd<bf16_t, 64>(a, d_groups, n_groups, nt, st);
+  if (n_groups > 0) {
+    constexpr int DPT = HD == 128 ? 4 : 1;
+    attn_combine_kernel<HD, DPT><<<dim3(n_groups, a.Hkv, 16 * nt / kCombineQv), HD / DPT * kCombineQv, 0, st>>>(
+        a, groups);
   }
   return hipGetLastError();
 }
+
+}  // namespace
 
 const char* attn_kernel_name(int hd, int nt, int w, bool tree) {
   if (tree) {

@@ -79,9 +79,10 @@ struct KvMoveJob {
 hipError_t launch_kv_move(int dtype, const KvMoveJob& j, hipStream_t st);
 
 // Page .y of every plane of pool [n_planes][num_pages][page_bytes] <- page .x,
-// for n pairs (device).  No page is a destination twice or a destination and a
-// source (page_bytes % 16 == 0).
-hipError_t launch_kv_copy_pages(const int2* d_pairs, int n, void* pool, int n_planes, int64_t num_pages,
+// for n pairs (device memory; in_args: host memory, n * 8 <= kUploadInline bytes
+// that travel in the kernel's arguments).  No page is a destination twice or a
+// destination and a source (page_bytes % 16 == 0).
+hipError_t launch_kv_copy_pages(const int2* pairs, int n, bool in_args, void* pool, int n_planes, int64_t num_pages,
                                 size_t page_bytes, hipStream_t st);
 
 }  // namespace spec

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "common.h"
 #include "elem.h"
@@ -430,11 +431,21 @@ __global__ __launch_bounds__(256) void kv_move_kernel(KvMoveJob j) {
 }
 
 // Copies of whole pages: workgroup (pair, span of the page, plane) moves a span
-// of kCopySpan 16-byte units, all of a thread's loads in flight together.
+// of kCopySpan 16-byte units, all of a thread's loads in flight together.  The
+// pairs lie in device memory, or, up to kCopyInline of them, in the arguments
+// (8 pages of 24 planes 15.5 -> 9 us: one launch instead of two).
 constexpr int kCopySpan = 1024;
-__global__ __launch_bounds__(256) void kv_copy_kernel(const int2* __restrict__ pairs, uint4* __restrict__ pool,
-                                                      int spans, uint32_t page_units, size_t plane_units) {
-  const int2 p = pairs[blockIdx.x / spans];
+constexpr int kCopyInline = kUploadInline / sizeof(int2);
+struct CopyMem {
+  const int2* p;
+};
+struct CopyArgs {
+  int2 p[kCopyInline];
+};
+template <typename Pairs>
+__global__ __launch_bounds__(256) void kv_copy_kernel(const Pairs pairs, uint4* __restrict__ pool, int spans,
+                                                      uint32_t page_units, size_t plane_units) {
+  const int2 p = pairs.p[blockIdx.x / spans];
   uint4* plane = pool + blockIdx.y * plane_units;
   const uint4* src = plane + static_cast<size_t>(p.x) * page_units;
   uint4* dst = plane + static_cast<size_t>(p.y) * page_units;
@@ -451,14 +462,26 @@ __global__ __launch_bounds__(256) void kv_copy_kernel(const int2* __restrict__ p
 
 }  // namespace
 
-hipError_t launch_kv_copy_pages(const int2* d_pairs, int n, void* pool, int n_planes, int64_t num_pages,
+hipError_t launch_kv_copy_pages(const int2* pairs, int n, bool in_args, void* pool, int n_planes, int64_t num_pages,
                                 size_t page_bytes, hipStream_t st) {
   if (n <= 0 || n_planes <= 0) return hipSuccess;
   const size_t units = page_bytes / 16;
   const size_t spans = (units + kCopySpan - 1) / kCopySpan;
-  if (page_bytes % 16 || units == 0 || spans * n > kMaxGrid256 || n_planes > 65535) return hipErrorInvalidValue;
-  kv_copy_kernel<<<dim3(static_cast<uint32_t>(spans * n), n_planes), 256, 0, st>>>(
-      d_pairs, static_cast<uint4*>(pool), static_cast<int>(spans), static_cast<uint32_t>(units), num_pages * units);
+  if (page_bytes % 16 || units == 0 || units > UINT32_MAX || spans > INT32_MAX || spans * n > kMaxGrid256 ||
+      n_planes > 65535 || (in_args && n > kCopyInline))
+    return hipErrorInvalidValue;
+  const dim3 grid(static_cast<uint32_t>(spans * n), n_planes);
+  auto go = [&](const auto& p) {
+    launch_kernel(kv_copy_kernel<std::decay_t<decltype(p)>>, grid, dim3(256), 0, st, p, static_cast<uint4*>(pool),
+                  static_cast<int>(spans), static_cast<uint32_t>(units), static_cast<size_t>(num_pages) * units);
+  };
+  if (in_args) {
+    CopyArgs a;
+    std::copy(pairs, pairs + n, a.p);
+    go(a);
+  } else {
+    go(CopyMem{pairs});
+  }
   return hipGetLastError();
 }
 

@@ -231,10 +231,14 @@ struct AttnPlan {
 // Runs of at least kPrefillMinRows rows in every segment (prefill chunks) with
 // 256 % G == 0 and at most kPrefillMaxKeys keys take the prefill form instead: blocks of 256 / G rows against
 // all their keys, heaviest first (allow_prefill = false keeps the tiled form).
-// max_nt: the widest query tile (in 16 vectors) that the kernel has (G <= 16 max_nt).
 constexpr int kPrefillMinRows = 64;
 constexpr int kPrefillMaxKeys = 16384;  // the prefill kernel stages at most 1024 page ids
 AttnPlan plan_attention(const std::vector<AttnSegment>& segs, int G, int Hkv, int max_parts,
-                        int target_wgs = kAttnTargetWgs, bool allow_prefill = true, int max_nt = 4);
+                        int target_wgs = kAttnTargetWgs, bool allow_prefill = true);
+
+// The same for the attention over a 4-bit cache (w = 4 or 8): fewer, longer items,
+// since a cache a quarter as large leaves less to gain by sharing it.
+constexpr int kKv4MaxNt = 4, kKv4MaxNtF32 = 2;
+AttnPlan plan_kv4(const std::vector<AttnSegment>& segs, int G, int Hkv, int max_parts, bool fp32);
 
 }  // namespace spec

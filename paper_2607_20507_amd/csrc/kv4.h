@@ -25,12 +25,18 @@ hipError_t launch_kv4_read(int dtype, int R, int Hkv, int hd, const int32_t* slo
 hipError_t launch_kv4_expand(int n, const int32_t* src, int Hkv, int hd, const void* kpool, const void* vpool,
                              void* kdst, void* vdst, hipStream_t st);
 
-// Widest query tile (in 16 vectors) of the attention kernel.
-constexpr int kv4_max_nt(int dtype) { return dtype == 0 ? 2 : 4; }
-
 // As launch_attention_bf16 (items, groups and partials), kpool / vpool 4-bit
-// pages; q and out are fp32 or bf16 (a.dtype).
-hipError_t launch_attention_kv4(const AttnArgs& a, const AttnItem* d_items, int n_items, const AttnGroup* d_groups,
-                                int n_groups, int nt, int w, hipStream_t st);
+// pages; q and out are fp32 or bf16 (a.dtype).  The page table, items and groups
+// are at byte offsets o_pt, o_it and o_gr of `tables`: device memory, or, with
+// `inline_bytes` > 0 (at most kUploadInline), host memory that travels in the
+// kernel's arguments (no groups then, and items of at most kKv4StagedPages
+// pages).
+constexpr int kKv4StagedPages = 512;
+struct Kv4Tables {
+  const char* tables = nullptr;
+  size_t inline_bytes = 0, o_pt = 0, o_it = 0, o_gr = 0;
+};
+hipError_t launch_attention_kv4(const AttnArgs& a, const Kv4Tables& t, int n_items, int n_groups, int max_parts,
+                                int nt, int w, hipStream_t st);
 
 }  // namespace spec

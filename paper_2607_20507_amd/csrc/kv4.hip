@@ -3,8 +3,8 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "attn_finish.h"
 #include "common.h"
+#include "host_util.h"
 #include "kv4.h"
 #include "kv4_layout.h"
 
@@ -282,29 +282,129 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&w)[N]) {
   }
 }
 
-constexpr int kStagedPages = 256;  // page ids of one work item kept in LDS (4096 keys)
+// Exponents are one FMA, p = 2^(raw scale - M), with M the rounded base-2 logit of
+// the maximum: exact as long as M is used for the sums too, but off by up to
+// M 2^-24 from the largest exponent, 0.  Above this M a wave takes the difference of
+// the raw scores first (one instruction more per score), which a 4-bit cache, whose
+// blocks have any scale, may need.
+constexpr float kFarLog2 = 16777216.f;
+// A maximum is raised only by a score more than 2^8 times as probable: fewer
+// rescalings, and probabilities stay below 2^8.
+constexpr float kRescaleLog2 = 8.f;
 
+// The call's tables: in device memory, or in the kernel's arguments, which saves
+// the launch that would bring them there.
+struct TabMem {
+  const AttnItem* items;
+  const int32_t* pt;
+};
+struct TabArgs {
+  uint32_t n, o_it, o_pt;  // 4-byte words: all, the first item, the page table
+  int32_t w[kUploadInline / 4];
+};
+__device__ __forceinline__ int32_t global_page(const TabMem& t, size_t i) { return t.pt[i]; }
+__device__ __forceinline__ int32_t global_page(const TabArgs&, size_t) { return 0; }  // (always in LDS)
+static_assert(sizeof(AttnItem) == 32, "eight words an item");
+
+__device__ __forceinline__ void store4(bf16_t* o, const f32x4& v) {
+  *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+}
+__device__ __forceinline__ void store4(float* o, const f32x4& v) {
+  *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+}
+
+// The waves' states are merged through LDS, each wave taking some of the output
+// tiles, and the output or the partial is written.  m: base-2 logit that a lane's
+// sums are relative to (-inf: no key), l: its share of the sum.
 template <typename T, int HD, int NT, int W>
-__global__ __launch_bounds__(64 * W, NT <= 2 ? 2 : 1) void attn_kv4_kernel(AttnArgs a,
-                                                                           const AttnItem* __restrict__ items) {
+__device__ __forceinline__ void finish(const AttnArgs& a, const AttnItem& it, int gkv, int M, int lane, int wave,
+                                       const float (&m)[NT], const float (&l)[NT], const f32x4 (&acc)[HD / 16][NT]) {
+  constexpr int DT = HD / 16;
+  const int g = lane >> 4, l16 = lane & 15;
+  const int G = a.Hq / a.Hkv;
+  // one query tile after the other: the buffer of all would leave room for fewer
+  // workgroups on a CU
+  __shared__ f32x4 s_acc[W][DT][kWave];
+  __shared__ float s_m[W][16], s_l[W][16];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    if (16 * nt >= M) break;
+    float lt = l[nt];
+    lt += __shfl_xor(lt, 16, kWave);
+    lt += __shfl_xor(lt, 32, kWave);
+    if (nt > 0) __syncthreads();
+    if (g == 0) {
+      s_m[wave][l16] = m[nt];
+      s_l[wave][l16] = lt;
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) s_acc[wave][dt][lane] = acc[dt][nt];
+    __syncthreads();
+    const int v = 16 * nt + l16;
+    float mm = -INFINITY, e[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_m[w][l16]);
+    lt = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      e[w] = s_m[w][l16] == -INFINITY ? 0.f : exp2f(s_m[w][l16] - mm);
+      lt += e[w] * s_l[w][l16];
+    }
+    if (v < M)
+    for (int dt = wave; dt < DT; dt += W) {
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < W; ++w) o += e[w] * s_acc[w][dt][lane];
+      if (it.part < 0) {
+        store4(static_cast<T*>(a.out) + (static_cast<size_t>(it.row0 + v / G) * a.Hq + gkv * G + v % G) * HD + 16 * dt + 4 * g,
+               o * (1.f / lt));
+      } else {
+        const size_t pm = (static_cast<size_t>(it.part) * a.Hkv + gkv) * 64 + v;
+        store4(a.part_o + pm * HD + 16 * dt + 4 * g, o);
+        if (dt == 0 && g == 0) reinterpret_cast<float2*>(a.part_ml)[pm] = make_float2(mm, lt);
+      }
+    }
+  }
+}
+
+template <typename T, int HD, int NT, int W, typename Tab>
+__global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv4_kernel(AttnArgs a, const Tab tab) {
   constexpr int DS = HD / 32, DT = HD / 16, BB = kv4_block_bytes(HD), CB = kv4_code_bytes(HD);
   constexpr int NP = Parts<T>::n;
   const int gkv = blockIdx.x % a.Hkv;
-  const AttnItem it = items[blockIdx.x / a.Hkv];
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int g = lane >> 4, l16 = lane & 15;
+  constexpr bool kInArgs = std::is_same_v<Tab, TabArgs>;
+  // page ids of the item, in LDS unless it has more than fit
+  __shared__ int32_t s_tab[kInArgs ? kUploadInline / 4 : kKv4StagedPages];
+  AttnItem it;
+  const int32_t* s_pt = s_tab;
+  size_t pt = 0;  // the sequence's page ids in tab.pt
+  int p0 = 0;     // first page of s_pt
+  bool staged = true;
+  if constexpr (kInArgs) {
+    // arguments lie in host memory: one round trip for all of the tables instead
+    // of one for the item and one for its pages
+    for (uint32_t i = threadIdx.x; i < tab.n; i += kWave * W) s_tab[i] = tab.w[i];
+    __syncthreads();
+    const int32_t* p = s_tab + tab.o_it + blockIdx.x / a.Hkv * 8;
+    auto word = [&](int i) { return __builtin_amdgcn_readfirstlane(p[i]); };
+    it = AttnItem{word(0), word(1), word(2), word(3), word(4), word(5), word(6), word(7)};
+    s_pt = s_tab + tab.o_pt + it.seq * a.max_pages;
+  } else {
+    it = tab.items[blockIdx.x / a.Hkv];
+    pt = static_cast<size_t>(it.seq) * a.max_pages;
+    p0 = it.t0 >> 4;
+    const int np = it.t1 > it.t0 ? ((it.t1 - 1) >> 4) - p0 + 1 : 0;
+    staged = np <= kKv4StagedPages;
+    if (staged)
+      for (int i = threadIdx.x; i < np; i += kWave * W) s_tab[i] = tab.pt[pt + p0 + i];
+    __syncthreads();
+  }
   const int G = a.Hq / a.Hkv;
   const int M = it.nrows * G;
   const uint8_t* kp = static_cast<const uint8_t*>(a.kpool);
   const uint8_t* vp = static_cast<const uint8_t*>(a.vpool);
-  const int32_t* pt = a.page_table + static_cast<size_t>(it.seq) * a.max_pages;
-  __shared__ int32_t s_pt[kStagedPages];
-  const int p0 = it.t0 >> 4;
-  const int np = it.t1 > it.t0 ? ((it.t1 - 1) >> 4) - p0 + 1 : 0;
-  const bool staged = np <= kStagedPages;
-  if (staged)
-    for (int i = threadIdx.x; i < np; i += kWave * W) s_pt[i] = pt[p0 + i];
-  __syncthreads();
 
   uint4 qf[NT][DS][NP];
   int vpos[NT];
@@ -334,62 +434,58 @@ __global__ __launch_bounds__(64 * W, NT <= 2 ? 2 : 1) void attn_kv4_kernel(AttnA
   }
   const float scale = kLog2e / sqrtf(static_cast<float>(HD));
   const int pos_lo = it.pos0;  // every row of the item sees the keys up to here
-  // the running maximum of the raw scores: subtracted before the scale, so that
-  // the largest score's exponent is 0 whatever its size
-  float mrun[NT], lrun[NT];
+  int klim[NT];                // the last key a query vector sees (-1: none, a padding vector)
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) klim[nt] = vval[nt] ? min(vpos[nt], it.t1 - 1) : -1;
+  // the running maximum of the raw scores, the score above which it is raised,
+  // minus its base-2 logit
+  float mrun[NT], mlim[NT], mneg[NT], lrun[NT];
+  bool far = false;
   f32x4 acc[DT][NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    mrun[nt] = -INFINITY;
-    lrun[nt] = 0.f;
+    mrun[nt] = mlim[nt] = -INFINITY;
+    mneg[nt] = lrun[nt] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
   auto walk = [&](auto from_lds) {
     auto page = [&](int t) -> size_t {
-      if constexpr (decltype(from_lds)::value) return s_pt[(t >> 4) - p0];
-      else return pt[t >> 4];
+      if constexpr (kInArgs || decltype(from_lds)::value) return s_pt[(t >> 4) - p0];
+      else return global_page(tab, pt + (t >> 4));
     };
     // codes and scales of one 32-key chunk's operands (keys past t1 clamped to
     // a valid page; their scores are masked and their V entries zeroed)
-    uint32_t kc[2 * DS], ks[DS / 2];     // [hh][s] (hd 64 too: a lane's 16 bytes hold both key tiles)
-    uint32_t vc[2 * DS], vs[2 * DS];     // [block b][token half]
-    auto load_k = [&](int c0) {
+    struct Raw {
+      uint32_t kc[2 * DS], ks[DS / 2];  // [key tile][step] (hd 64 too: a lane's 16 bytes hold both tiles)
+      uint32_t vc[2 * DS], vs[2 * DS];  // [block][token half]
+    };
+    auto load_k = [&](Raw& w, int c0) {
       const uint8_t* blk = kp + (page(min(c0 + 16 * (l16 >> 3), it.t1 - 1)) * a.Hkv + gkv) * BB;
       const int j = l16 & 7;
 #pragma unroll
       for (int i = 0; i < HD / 64; ++i) {
         const uint4 u = ld_stream(reinterpret_cast<const uint4*>(blk) + (HD == 128 ? (i * 4 + g) * 8 + j : g * 8 + j));
-        kc[4 * i] = u.x; kc[4 * i + 1] = u.y; kc[4 * i + 2] = u.z; kc[4 * i + 3] = u.w;
+        w.kc[4 * i] = u.x; w.kc[4 * i + 1] = u.y; w.kc[4 * i + 2] = u.z; w.kc[4 * i + 3] = u.w;
       }
       const uint32_t* sp = reinterpret_cast<const uint32_t*>(blk + CB) + j * (DS / 2);
 #pragma unroll
-      for (int i = 0; i < DS / 2; ++i) ks[i] = sp[i];
+      for (int i = 0; i < DS / 2; ++i) w.ks[i] = sp[i];
     };
-    auto load_v = [&](int c0) {
+    auto load_v = [&](Raw& w, int c0) {
       const uint8_t* blk = vp + (page(min(c0 + 8 * g, it.t1 - 1)) * a.Hkv + gkv) * BB;
       const int th = g & 1;
 #pragma unroll
       for (int i = 0; i < HD / 64; ++i) {
         const uint4 u = ld_stream(reinterpret_cast<const uint4*>(blk) + (i * 2 + th) * 16 + l16);
-        vc[4 * i] = u.x; vc[4 * i + 1] = u.y; vc[4 * i + 2] = u.z; vc[4 * i + 3] = u.w;
+        w.vc[4 * i] = u.x; w.vc[4 * i + 1] = u.y; w.vc[4 * i + 2] = u.z; w.vc[4 * i + 3] = u.w;
         const uint4 s = *(reinterpret_cast<const uint4*>(blk + CB) + th * (DS / 2) + i);
-        vs[4 * i] = s.x; vs[4 * i + 1] = s.y; vs[4 * i + 2] = s.z; vs[4 * i + 3] = s.w;
+        w.vs[4 * i] = s.x; w.vs[4 * i + 1] = s.y; w.vs[4 * i + 2] = s.z; w.vs[4 * i + 3] = s.w;
       }
     };
-    // K operand of key tile hh, step s
-    auto k_op = [&](auto hh_, auto s_) -> uint4 {
-      constexpr int hh = decltype(hh_)::value, s = decltype(s_)::value, n = hh * DS + s;
-      return get8(kc[n], scale_bits<n % 4>(ks[n / 4]));
-    };
-    const int cfirst = it.t0 + 32 * wave;
-    if (cfirst < it.t1) {
-      load_k(cfirst);
-      load_v(cfirst);
-    }
-    for (int c0 = cfirst; c0 < it.t1; c0 += 32 * W) {
-      const int cn = min(c0 + 32 * W, it.t1 - 1);
+    // the chunk of keys c0 .. held in w, which then takes the wave's chunk of keys cn ..
+    auto chunk = [&](Raw& w, int c0, int cn) {
       const bool full = c0 + 32 <= it.t1 && c0 + 31 <= pos_lo;  // no masks
       f32x4 sc[NT][2];
 #pragma unroll
@@ -397,7 +493,8 @@ __global__ __launch_bounds__(64 * W, NT <= 2 ? 2 : 1) void attn_kv4_kernel(AttnA
       auto step = [&](auto s_) {
         constexpr int s = decltype(s_)::value;
         if constexpr (s < DS) {
-          const uint4 k0 = k_op(std::integral_constant<int, 0>{}, s_), k1 = k_op(std::integral_constant<int, 1>{}, s_);
+          const uint4 k0 = get8(w.kc[s], scale_bits<s % 4>(w.ks[s / 4]));
+          const uint4 k1 = get8(w.kc[DS + s], scale_bits<(DS + s) % 4>(w.ks[(DS + s) / 4]));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -411,67 +508,82 @@ __global__ __launch_bounds__(64 * W, NT <= 2 ? 2 : 1) void attn_kv4_kernel(AttnA
       step(std::integral_constant<int, 1>{});
       step(std::integral_constant<int, 2>{});
       step(std::integral_constant<int, 3>{});
-      load_k(cn);
-      float raw[NT][8], msub[NT];
+      load_k(w, cn);
+      float raw[NT][8], mx[NT];
+      bool grow = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) raw[nt][j] = (j < 4) ? sc[nt][0][j] : sc[nt][1][j - 4];
-        if (!full) {
-          asm volatile("");  // keeps the masks a branch
+      }
+      if (!full) {
+        asm volatile("");  // keeps the masks a branch
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int t = c0 + 8 * g + j;
-            const bool ok = vval[nt] & (t < it.t1) & (t <= vpos[nt]);
-            raw[nt][j] = ok ? raw[nt][j] : -INFINITY;
-          }
-        }
-        float mx = raw[nt][0];
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int j = 1; j < 8; ++j) mx = fmaxf(mx, raw[nt][j]);
-        if (__any(mx > mrun[nt])) {  // a new maximum: the same in every lane of a query vector
-          mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-          mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-          const bool grow = mx > mrun[nt];
-          const float alpha = grow ? ((mrun[nt] == -INFINITY) ? 0.f : exp2f((mrun[nt] - mx) * scale)) : 1.f;
-          if (grow) mrun[nt] = mx;
+          for (int j = 0; j < 8; ++j) raw[nt][j] = c0 + 8 * g + j <= klim[nt] ? raw[nt][j] : -INFINITY;
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        mx[nt] = raw[nt][0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) mx[nt] = fmaxf(mx[nt], raw[nt][j]);
+        grow |= mx[nt] > mlim[nt];
+      }
+      if (__any(grow)) {  // a new maximum: the same in every lane of a query vector
+        bool large = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float m = mx[nt];
+          m = fmaxf(m, __shfl_xor(m, 16, kWave));
+          m = fmaxf(m, __shfl_xor(m, 32, kWave));
+          m = m > mlim[nt] ? m : mrun[nt];
+          const float alpha = mrun[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mrun[nt] - m) * scale);
+          mrun[nt] = m;
+          mlim[nt] = m + kRescaleLog2 / scale;
+          mneg[nt] = m == -INFINITY ? 0.f : -m * scale;
+          large |= fabsf(mneg[nt]) > kFarLog2;
           lrun[nt] *= alpha;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= alpha;
         }
-        msub[nt] = (mrun[nt] == -INFINITY) ? 0.f : mrun[nt];
+        far |= __any(large) != 0;
       }
       uint4 pf[NT][NP];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float p[8], ps = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = exp2f((raw[nt][j] - msub[nt]) * scale);
+        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(raw[nt][j], scale, mneg[nt]));
+        if (far) {
+          asm volatile("");
+          const float m = mrun[nt] == -INFINITY ? 0.f : mrun[nt];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f((raw[nt][j] - m) * scale);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) ps += p[j];
         lrun[nt] += ps;
-        uint32_t w[4][NP];
+        uint32_t h[4][NP];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) split_pair<NP>(p[2 * j], p[2 * j + 1], w[j]);
+        for (int j = 0; j < 4; ++j) split_pair<NP>(p[2 * j], p[2 * j + 1], h[j]);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) pf[nt][i] = make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]);
+        for (int i = 0; i < NP; ++i) pf[nt][i] = make_uint4(h[0][i], h[1][i], h[2][i], h[3][i]);
       }
-      const bool tail = c0 + 32 > it.t1;
-      const int nvalid = min(max(it.t1 - (c0 + 8 * g), 0), 8);
+      if (c0 + 32 > it.t1) {  // keys past the end hold anything, and 0 x NaN is not 0
+        asm volatile("");
+        const int nvalid = min(max(it.t1 - (c0 + 8 * g), 0), 8);
+        const uint64_t keep = nvalid == 8 ? ~0ull : (1ull << (8 * nvalid)) - 1;
+#pragma unroll
+        for (int i = 0; i < 2 * DS; ++i) {
+          w.vc[i] &= static_cast<uint32_t>(i % 2 ? keep >> 32 : keep);
+          w.vs[i] &= static_cast<uint32_t>(i % 2 ? keep >> 32 : keep);
+        }
+      }
 #pragma unroll
       for (int b = 0; b < DS; ++b) {
         uint4 v[2];
-        get8_tokens(vc[2 * b], vc[2 * b + 1], vs[2 * b], vs[2 * b + 1], v[0], v[1]);
-        if (tail) {  // keys past the end hold anything, and 0 x NaN is not 0
-          asm volatile("");
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            v[i].x = mask_pair(v[i].x, nvalid);
-            v[i].y = mask_pair(v[i].y, nvalid - 2);
-            v[i].z = mask_pair(v[i].z, nvalid - 4);
-            v[i].w = mask_pair(v[i].w, nvalid - 6);
-          }
-        }
+        get8_tokens(w.vc[2 * b], w.vc[2 * b + 1], w.vs[2 * b], w.vs[2 * b + 1], v[0], v[1]);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -479,30 +591,143 @@ __global__ __launch_bounds__(64 * W, NT <= 2 ? 2 : 1) void attn_kv4_kernel(AttnA
 #pragma unroll
             for (int n = 0; n < NP; ++n) acc[2 * b + i][nt] = mfma16x16x32(v[i], pf[nt][n], acc[2 * b + i][nt]);
       }
-      load_v(cn);
+      load_v(w, cn);
+    };
+    // The wave's chunks: the next one's operands are loaded as soon as this one's
+    // are converted.  (Two chunks in flight took more registers and no less time:
+    // 64 sequences 42.7 .. 47.1 us against 43.7 .. 47.1, 131000 keys 37.3 and 36.4.)
+    Raw raw;
+    const int cfirst = it.t0 + 32 * wave;
+    if (cfirst < it.t1) {
+      load_k(raw, cfirst);
+      load_v(raw, cfirst);
     }
+    for (int c0 = cfirst; c0 < it.t1; c0 += 32 * W) chunk(raw, c0, min(c0 + 32 * W, it.t1 - 1));
   };
-  if (staged) walk(std::true_type{});
-  else walk(std::false_type{});
+  if constexpr (kInArgs) {
+    walk(std::true_type{});
+  } else {
+    if (staged) walk(std::true_type{});
+    else walk(std::false_type{});
+  }
+  float m[NT];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) mrun[nt] *= scale;  // base-2 logits
-  attn_finish<T, HD, NT, W>(a, it, gkv, M, lane, wave, mrun, lrun, acc);
+  for (int nt = 0; nt < NT; ++nt) m[nt] = mrun[nt] == -INFINITY ? -INFINITY : -mneg[nt];
+  finish<T, HD, NT, W>(a, it, gkv, M, lane, wave, m, lrun, acc);
 }
 
-template <typename T, int HD, int NT>
-void launch_items(const AttnArgs& a, const AttnItem* items, int n_items, int w, hipStream_t st) {
-  const dim3 grid(n_items * a.Hkv);
-  if (w >= 4) launch_kernel(attn_kv4_kernel<T, HD, NT, 4>, grid, dim3(4 * kWave), 0, st, a, items);
-  else launch_kernel(attn_kv4_kernel<T, HD, NT, 2>, grid, dim3(2 * kWave), 0, st, a, items);
+// Merges the parts of split items.  A query vector's parts are shared by P threads
+// for each 4 dims, 8 / P vectors a workgroup of 256 (head dim 64: twice as many):
+// a thread's loads of up to 8 parts are in flight together.
+template <typename T, int HD, int P>
+__global__ __launch_bounds__(256) void combine_kv4_kernel(AttnArgs a, const AttnGroup* __restrict__ groups) {
+  constexpr int TQ = HD / 4, QV = 256 / TQ / P, B = 8;
+  const AttnGroup gr = groups[blockIdx.x];
+  const int gkv = blockIdx.y, G = a.Hq / a.Hkv;
+  const int d0 = 4 * (static_cast<int>(threadIdx.x) % TQ), sl = static_cast<int>(threadIdx.x) / TQ;
+  const int pg = sl % P, v = blockIdx.z * QV + sl / P;
+  const bool in = v < gr.nrows * G;
+  const size_t base = (static_cast<size_t>(gr.part0) * a.Hkv + gkv) * 64 + (in ? v : 0);
+  const size_t stride = static_cast<size_t>(a.Hkv) * 64;
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+  float M = -INFINITY, den = 0.f;
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = pg; p0 < gr.nparts; p0 += B * P) {
+    float2 c[B];
+    f32x4 o[B];
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+      const size_t pm = base + min(p0 + i * P, gr.nparts - 1) * stride;
+      c[i] = ml[pm];
+      o[i] = *reinterpret_cast<const f32x4*>(a.part_o + pm * HD + d0);
+      if (p0 + i * P >= gr.nparts) c[i].x = -INFINITY;
+    }
+    float mx = M;
+#pragma unroll
+    for (int i = 0; i < B; ++i) mx = fmaxf(mx, c[i].x);
+    if (mx == -INFINITY) continue;
+    const float e0 = M == -INFINITY ? 0.f : exp2f(M - mx);
+    num *= e0;
+    den *= e0;
+    M = mx;
+#pragma unroll
+    for (int i = 0; i < B; ++i) {
+      const float e = c[i].x == -INFINITY ? 0.f : exp2f(c[i].x - mx);
+      num += e * o[i];
+      den += e * c[i].y;
+    }
+  }
+  if constexpr (P > 1) {
+    __shared__ f32x4 s_num[256];
+    __shared__ float s_m[256], s_den[256];
+    s_num[threadIdx.x] = num;
+    s_m[threadIdx.x] = M;
+    s_den[threadIdx.x] = den;
+    __syncthreads();
+    if (pg > 0) return;
+#pragma unroll
+    for (int i = 1; i < P; ++i) M = fmaxf(M, s_m[threadIdx.x + i * TQ]);
+    num = f32x4{0.f, 0.f, 0.f, 0.f};
+    den = 0.f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int t = threadIdx.x + i * TQ;
+      const float e = s_m[t] == -INFINITY ? 0.f : exp2f(s_m[t] - M);
+      num += e * s_num[t];
+      den += e * s_den[t];
+    }
+  }
+  if (in)
+    store4(static_cast<T*>(a.out) + (static_cast<size_t>(gr.row0 + v / G) * a.Hq + gkv * G + v % G) * HD + d0, num * (1.f / den));
 }
 
 template <typename T, int HD>
-hipError_t launch_attn(const AttnArgs& a, const AttnItem* items, int n_items, int nt, int w, hipStream_t st) {
-  if (nt <= 1) launch_items<T, HD, 1>(a, items, n_items, w, st);
-  else if (nt == 2) launch_items<T, HD, 2>(a, items, n_items, w, st);
-  else if constexpr (Parts<T>::n == 1)
-    launch_kernel(attn_kv4_kernel<T, HD, 4, 2>, dim3(n_items * a.Hkv), dim3(2 * kWave), 0, st, a, items);
-  else return hipErrorInvalidValue;
+void launch_combine(const AttnArgs& a, const AttnGroup* groups, int n_groups, int max_parts, int nt, hipStream_t st) {
+  const int per = 1024 / HD;  // vectors of a workgroup with P = 1
+  auto go = [&](auto p_) {
+    constexpr int P = decltype(p_)::value;
+    launch_kernel(combine_kv4_kernel<T, HD, P>, dim3(n_groups, a.Hkv, (16 * nt * P + per - 1) / per), dim3(256), 0, st, a,
+                  groups);
+  };
+  if (max_parts <= 8) go(std::integral_constant<int, 1>{});
+  else go(std::integral_constant<int, 8>{});
+}
+
+template <typename T, int HD, typename Tab>
+hipError_t launch_items(const AttnArgs& a, const Tab& tab, int n_items, int nt, int w, hipStream_t st) {
+  const dim3 grid(n_items * a.Hkv);
+  auto go = [&](auto nt_, auto w_) {
+    constexpr int NT = decltype(nt_)::value, W = decltype(w_)::value;
+    launch_kernel(attn_kv4_kernel<T, HD, NT, W, Tab>, grid, dim3(64 * W), 0, st, a, tab);
+    return hipGetLastError();
+  };
+  using std::integral_constant;
+  if (nt == 1 && w == 4) return go(integral_constant<int, 1>{}, integral_constant<int, 4>{});
+  if (nt == 2 && w == 4) return go(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+  if constexpr (Parts<T>::n == 1) {
+    if (nt == 4 && w == 4) return go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+    if (nt == 1 && w == 8) return go(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+    if (nt == 2 && w == 8) return go(integral_constant<int, 2>{}, integral_constant<int, 8>{});
+  }
+  return hipErrorInvalidValue;
+}
+
+template <typename T, int HD>
+hipError_t launch_attn(const AttnArgs& a, const Kv4Tables& t, int n_items, int n_groups, int max_parts, int nt, int w,
+                       hipStream_t st) {
+  if (t.inline_bytes) {
+    TabArgs tab;
+    if (t.inline_bytes > kUploadInline || n_groups > 0) return hipErrorInvalidValue;
+    tab.n = static_cast<uint32_t>(t.inline_bytes / 4);
+    tab.o_it = static_cast<uint32_t>(t.o_it / 4);
+    tab.o_pt = static_cast<uint32_t>(t.o_pt / 4);
+    std::memcpy(tab.w, t.tables, t.inline_bytes);
+    return launch_items<T, HD>(a, tab, n_items, nt, w, st);
+  }
+  const TabMem tab{reinterpret_cast<const AttnItem*>(t.tables + t.o_it), reinterpret_cast<const int32_t*>(t.tables + t.o_pt)};
+  const hipError_t e = launch_items<T, HD>(a, tab, n_items, nt, w, st);
+  if (e != hipSuccess || n_groups <= 0) return e;
+  launch_combine<T, HD>(a, reinterpret_cast<const AttnGroup*>(t.tables + t.o_gr), n_groups, max_parts, nt, st);
   return hipGetLastError();
 }
 
@@ -552,19 +777,15 @@ hipError_t launch_kv4_expand(int n, const int32_t* src, int Hkv, int hd, const v
   return hipGetLastError();
 }
 
-hipError_t launch_attention_kv4(const AttnArgs& a, const AttnItem* d_items, int n_items, const AttnGroup* d_groups,
-                                int n_groups, int nt, int w, hipStream_t st) {
+hipError_t launch_attention_kv4(const AttnArgs& a, const Kv4Tables& t, int n_items, int n_groups, int max_parts,
+                                int nt, int w, hipStream_t st) {
   if (n_items <= 0) return hipSuccess;
-  if (static_cast<size_t>(n_items) * a.Hkv > kMaxGrid256) return hipErrorInvalidValue;
-  if ((a.hd != 64 && a.hd != 128) || nt > kv4_max_nt(a.dtype)) return hipErrorInvalidValue;
-  hipError_t e;
+  if (static_cast<size_t>(n_items) * a.Hkv * w > 4 * kMaxGrid256 || (a.hd != 64 && a.hd != 128)) return hipErrorInvalidValue;
   if (a.dtype == 0)
-    e = a.hd == 128 ? launch_attn<float, 128>(a, d_items, n_items, nt, w, st)
-                    : launch_attn<float, 64>(a, d_items, n_items, nt, w, st);
-  else
-    e = a.hd == 128 ? launch_attn<bf16_t, 128>(a, d_items, n_items, nt, w, st)
-                    : launch_attn<bf16_t, 64>(a, d_items, n_items, nt, w, st);
-  return e == hipSuccess ? launch_attention_combine(a, d_groups, n_groups, nt, st) : e;
+    return a.hd == 128 ? launch_attn<float, 128>(a, t, n_items, n_groups, max_parts, nt, w, st)
+                       : launch_attn<float, 64>(a, t, n_items, n_groups, max_parts, nt, w, st);
+  return a.hd == 128 ? launch_attn<bf16_t, 128>(a, t, n_items, n_groups, max_parts, nt, w, st)
+                     : launch_attn<bf16_t, 64>(a, t, n_items, n_groups, max_parts, nt, w, st);
 }
 
 }  // namespace spec

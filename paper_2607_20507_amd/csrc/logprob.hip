@@ -14,9 +14,12 @@
 // The largest logits are ordered by a 64-bit key, the value (mapped to an
 // integer of the same order) above the complement of the id, so that equal
 // values go to the lower id and every key is different.  A workgroup keeps a
-// threshold T that at least n_top elements reach and collects what passes it
-// in LDS; the n_top-th largest of 256 disjoint subsets' maxima is such a
-// threshold, and at most n_top subsets hold anything above it.  Masked logits
+// value that at least n_top elements with lower ids reach and collects in LDS
+// what is above it.  That value first comes from the threads' maxima of the
+// first 4096 elements; where many keys were collected it is raised to the
+// n_top-th largest of 256 disjoint subsets' maxima, above which at most n_top
+// subsets hold anything.  A chunk whose logits ascend can collect more than the
+// buffer holds: it is then read once more in steps that cannot.  Masked logits
 // (-inf) are never collected: where fewer than n_top remain, the final kernel
 // appends the first masked ids.
 
@@ -32,10 +35,14 @@ namespace spec {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
 constexpr int kPerThread = 16;
-constexpr int kStep = kThreads * kPerThread;  // elements between two looks at the collected keys
-constexpr int kLimit = 512;                   // collected keys above this are thinned
-constexpr int kCap = kStep + kLimit;
+constexpr int kStep = kThreads * kPerThread;
+constexpr int kLook = 4;              // steps between two looks at the collected keys
+constexpr int kLimit = 512;           // collected keys above this are thinned
+constexpr int kCap = 2048;
+constexpr int kSafeStep = kThreads * 4;  // a step of the second reading
+static_assert(kSafeStep + kLimit <= kCap && kLogprobMaxTop * kPerThread <= kCap, "fits the buffer");
 constexpr int kTargetBlocks = 2048;
 constexpr int kMaxChunks = 64;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -47,15 +54,18 @@ struct LpStat {
   int32_t idx;    // of the first maximum
 };
 
-__device__ __forceinline__ uint64_t key_of(float v, int i) {
-  const uint32_t b = __float_as_uint(v + 0.f);  // -0 counts as 0
-  const uint32_t o = (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-  return (static_cast<uint64_t>(o) << 32) | static_cast<uint32_t>(~i);
+// Bits of v as an integer of the same order (-0 counts as 0).
+__device__ __forceinline__ uint32_t ordered(float v) {
+  const uint32_t b = __float_as_uint(v + 0.f);
+  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
-__device__ __forceinline__ float value_of(uint64_t k) {
-  const uint32_t o = static_cast<uint32_t>(k >> 32);
+__device__ __forceinline__ float unordered(uint32_t o) {
   return __uint_as_float((o & 0x80000000u) ? (o & 0x7FFFFFFFu) : ~o);
 }
+__device__ __forceinline__ uint64_t key_of(float v, int i) {
+  return (static_cast<uint64_t>(ordered(v)) << 32) | static_cast<uint32_t>(~i);
+}
+__device__ __forceinline__ float value_of(uint64_t k) { return unordered(static_cast<uint32_t>(k >> 32)); }
 __device__ __forceinline__ int id_of(uint64_t k) { return static_cast<int>(~static_cast<uint32_t>(k)); }
 
 // 1 / T in base 2, finite and above 0, so that 0 and -inf times it stay what they
@@ -92,54 +102,65 @@ struct Collect {
   alignas(16) uint64_t keys[kThreads];
   uint64_t buf[kCap];
   uint64_t t;
-  int cnt;
+  float first[kWaves];
+  int cnt, over;
 };
 
-// Number of the workgroup's keys above `mine` (every thread's key in s.keys).
-__device__ __forceinline__ int rank_of(const Collect& s, uint64_t mine) {
+__device__ __forceinline__ void collect(Collect& s, uint64_t key) {
+  const int p = atomicAdd(&s.cnt, 1);
+  if (p < kCap) s.buf[p] = key;
+  else s.over = 1;
+}
+
+// Number of the first n (even) of s.keys above `mine`.
+__device__ __forceinline__ int rank_of(const Collect& s, uint64_t mine, int n) {
   const ulonglong2* k2 = reinterpret_cast<const ulonglong2*>(s.keys);
   int r = 0;
-#pragma unroll 16
-  for (int i = 0; i < kThreads / 2; ++i) {
+#pragma unroll 4
+  for (int i = 0; i < n / 2; ++i) {
     const ulonglong2 v = k2[i];
     r += (v.x > mine) + (v.y > mine);
   }
   return r;
 }
 
-// s.t <- the n-th largest of the threads' keys (0: none), if there are n.
-// Barriers on both sides.
-__device__ __forceinline__ void raise_threshold(Collect& s, uint64_t mine, int n) {
-  __syncthreads();
-  s.keys[threadIdx.x] = mine;
-  __syncthreads();
-  if (mine != 0 && rank_of(s, mine) == n - 1) s.t = mine;
-  __syncthreads();
-}
-
-// Thins the collected keys to at most kThreads, the n largest among them.
+// Thins the collected keys to at most kThreads, the n largest among them, and
+// leaves in s.t a key that n of them reach.  Barriers on both sides.
 __device__ __forceinline__ void thin(Collect& s, int n) {
-  constexpr int PER = (kCap + kThreads - 1) / kThreads;
+  const int tid = threadIdx.x;
   __syncthreads();
-  int cnt = s.cnt;
+  int cnt = min(s.cnt, kCap);
+  __syncthreads();
   while (cnt > kThreads) {  // each turn leaves at most n ceil(cnt / 256) keys, n <= 64
-    uint64_t own[PER], mx = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int e = i * kThreads + static_cast<int>(threadIdx.x);
-      own[i] = e < cnt ? s.buf[e] : 0;
-      mx = own[i] > mx ? own[i] : mx;
-    }
-    raise_threshold(s, mx, n);
-    if (threadIdx.x == 0) s.cnt = 0;
+    uint64_t mx = 0;
+    for (int e = tid; e < cnt; e += kThreads) mx = s.buf[e] > mx ? s.buf[e] : mx;
+    s.keys[tid] = mx;
+    if (tid == 0) s.cnt = 0;
+    __syncthreads();
+    if (rank_of(s, mx, kThreads) == n - 1) s.t = mx;
     __syncthreads();
     const uint64_t t = s.t;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (own[i] != 0 && own[i] >= t) s.buf[atomicAdd(&s.cnt, 1)] = own[i];
-    __syncthreads();
+    // in place: a round's keys are read before any of them is written back, and
+    // no more are written than were read
+    for (int e0 = 0; e0 < cnt; e0 += kThreads) {
+      const uint64_t k = e0 + tid < cnt ? s.buf[e0 + tid] : 0;
+      __syncthreads();
+      if (k >= t) s.buf[atomicAdd(&s.cnt, 1)] = k;
+      __syncthreads();
+    }
     cnt = s.cnt;
+    __syncthreads();
   }
+}
+
+// The largest value to 16 leading bits that k lanes' values reach (-inf: none).
+__device__ __forceinline__ float reached_by(float v, int k) {
+  const uint32_t o = ordered(v);
+  uint32_t t = 0;
+#pragma unroll
+  for (int b = 31; b >= 16; --b)
+    if (__popcll(__ballot(o >= (t | (1u << b)))) >= k) t |= 1u << b;
+  return t > 0x007FFFFFu ? unordered(t) : -INFINITY;
 }
 
 template <bool VEC, bool TOP>
@@ -151,12 +172,12 @@ __global__ __launch_bounds__(kThreads) void logprob_chunk_kernel(int V, const fl
   const float* z = logits + static_cast<int64_t>(r) * ld;
   const float c = base2_factor(temps ? temps[r] : 1.f);
   const int beg = ch * chunk, end = min(V, beg + chunk);
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, wave = tid / kWave;
   __shared__ std::conditional_t<TOP, Collect, int> s;
   if constexpr (TOP) {
     if (tid == 0) {
       s.t = 0;
-      s.cnt = 0;
+      s.cnt = s.over = 0;
     }
     __syncthreads();
   }
@@ -164,10 +185,7 @@ __global__ __launch_bounds__(kThreads) void logprob_chunk_kernel(int V, const fl
   auto id = [&](int base, int e) {
     return VEC ? base + (e / 4) * 4 * kThreads + 4 * tid + e % 4 : base + e * kThreads + tid;
   };
-  LpStat st{-FLT_MAX, 0.f, 0.f, INT_MAX};
-  float tv = -INFINITY;
-  for (int base = beg; base < end; base += kStep) {
-    float v[kPerThread];
+  auto load = [&](int base, float (&v)[kPerThread]) {
     if (VEC && base + kStep <= end) {
 #pragma unroll
       for (int q = 0; q < kPerThread / 4; ++q) {
@@ -178,25 +196,27 @@ __global__ __launch_bounds__(kThreads) void logprob_chunk_kernel(int V, const fl
 #pragma unroll
       for (int e = 0; e < kPerThread; ++e) v[e] = id(base, e) < end ? z[id(base, e)] : -INFINITY;
     }
+  };
+  LpStat st{-FLT_MAX, 0.f, 0.f, INT_MAX};
+  float tv = -INFINITY;
+  float v[kPerThread], next[kPerThread];
+  load(beg, v);
+  int i = 0;
+  for (int base = beg; base < end; base += kStep, ++i) {
+    if (base + kStep < end) load(base + kStep, next);
     float vm = v[0];
 #pragma unroll
     for (int e = 1; e < kPerThread; ++e) vm = fmaxf(vm, v[e]);
-    int first = 0;
-    if (vm > st.m || (TOP && base == beg)) {
-#pragma unroll
-      for (int e = kPerThread - 1; e >= 0; --e)
-        if (v[e] == vm) first = e;
-    }
     if (vm > st.m || (vm == st.m && st.idx == INT_MAX)) {
       const float d = fmaxf((st.m - vm) * c, kFloor), a = exp2f(d);
       st.u = a * (st.u + d * st.s);
       st.s *= a;
       st.m = vm;
-      int fe = 0;
+      int first = 0;
 #pragma unroll
       for (int e = kPerThread - 1; e >= 0; --e)
-        if (v[e] == vm) fe = e;
-      st.idx = id(base, fe);
+        if (v[e] == vm) first = e;
+      st.idx = id(base, first);
     }
 #pragma unroll
     for (int e = 0; e < kPerThread; ++e) {
@@ -206,56 +226,84 @@ __global__ __launch_bounds__(kThreads) void logprob_chunk_kernel(int V, const fl
       st.u = fmaf(fmaxf(t, kFloor), p, st.u);
     }
     if constexpr (TOP) {
-      if (base == beg) {
-        raise_threshold(s, vm > -INFINITY ? key_of(vm, id(base, first)) : 0, n_top);
-        const uint64_t t = s.t;
-#pragma unroll
-        for (int e = 0; e < kPerThread; ++e) {
-          const uint64_t k = key_of(v[e], id(base, e));
-          if (v[e] > -INFINITY && k >= t) s.buf[atomicAdd(&s.cnt, 1)] = k;
-        }
+      if (i == 0) {
+        // each wave's share of n_top maxima reaches its value, so n_top reach the least of them
+        const float w = reached_by(vm, (n_top + kWaves - 1) / kWaves);
+        if ((tid & (kWave - 1)) == 0) s.first[wave] = w;
         __syncthreads();
-        tv = t ? value_of(t) : -INFINITY;
-      } else {
-        // n_top elements with lower ids are at least tv: an equal value here comes after them
-        if (vm > tv) {
+        tv = fminf(fminf(s.first[0], s.first[1]), fminf(s.first[2], s.first[3]));
+        static_assert(kWaves == 4, "one value a wave");
+        if (vm >= tv) {
 #pragma unroll
           for (int e = 0; e < kPerThread; ++e)
-            if (v[e] > tv) s.buf[atomicAdd(&s.cnt, 1)] = key_of(v[e], id(base, e));
+            if (v[e] >= tv && v[e] > -INFINITY) collect(s, key_of(v[e], id(base, e)));
+        }
+      } else if (vm > tv) {  // n_top elements with lower ids reach tv: an equal value here comes after them
+#pragma unroll
+        for (int e = 0; e < kPerThread; ++e)
+          if (v[e] > tv) collect(s, key_of(v[e], id(base, e)));
+      }
+      if (i % kLook == kLook - 1) {
+        __syncthreads();
+        const bool many = s.cnt > kLimit;
+        __syncthreads();  // nobody adds before everybody has looked
+        if (many) {
+          thin(s, n_top);
+          tv = fmaxf(tv, s.t ? value_of(s.t) : -INFINITY);
+          __syncthreads();
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < kPerThread; ++e) v[e] = next[e];
+  }
+  if constexpr (TOP) {
+    __syncthreads();
+    if (s.over) {
+      __syncthreads();
+      if (tid == 0) {
+        s.t = 0;
+        s.cnt = s.over = 0;
+      }
+      tv = -INFINITY;
+      __syncthreads();
+      for (int base = beg; base < end; base += kSafeStep) {
+        for (int e = 0; e < kSafeStep; e += kThreads) {
+          const int j = base + e + tid;
+          if (j < end && z[j] > tv) collect(s, key_of(z[j], j));
         }
         __syncthreads();
-      }
-      const bool many = s.cnt > kLimit;
-      __syncthreads();  // nobody adds before everybody has looked
-      if (many) {
-        thin(s, n_top);
-        tv = s.t ? value_of(s.t) : -INFINITY;
+        const bool many = s.cnt > kLimit;
         __syncthreads();
+        if (many) {
+          thin(s, n_top);
+          tv = s.t ? value_of(s.t) : -INFINITY;
+          __syncthreads();
+        }
       }
     }
   }
   st = wave_merge(st, c);
-  __shared__ LpStat s_st[kThreads / kWave];
-  if ((tid & (kWave - 1)) == 0) s_st[tid / kWave] = st;
+  __shared__ LpStat s_st[kWaves];
+  if ((tid & (kWave - 1)) == 0) s_st[wave] = st;
   if constexpr (TOP) {
     thin(s, n_top);
     const int cnt = s.cnt;
     const uint64_t mine = tid < cnt ? s.buf[tid] : 0;
-    __syncthreads();
     s.keys[tid] = mine;
     __syncthreads();
     uint64_t* out = lists + static_cast<size_t>(blockIdx.x) * n_top;
     if (mine != 0) {
-      const int k = rank_of(s, mine);
+      const int k = rank_of(s, mine, (cnt + 1) & ~1);
       if (k < n_top) out[k] = mine;
-    } else if (tid < n_top && tid >= cnt) {
-      out[tid] = 0;
+    } else if (tid < n_top) {
+      out[tid] = 0;  // (tid >= cnt)
     }
   } else {
     __syncthreads();
   }
   if (tid == 0) {
-    for (int w = 1; w < kThreads / kWave; ++w) stat_merge(st, s_st[w], c);
+    for (int w = 1; w < kWaves; ++w) stat_merge(st, s_st[w], c);
     stats[blockIdx.x] = st;
   }
 }
@@ -278,6 +326,11 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
   const int lane = tid & (kWave - 1);
   if (lane < n_chunks) st = stats[static_cast<size_t>(r) * n_chunks + lane];
   st = wave_merge(st, c);
+  // the butterfly's lanes round differently: one lane's result for all of them
+  st.m = __shfl(st.m, 0, kWave);
+  st.s = __shfl(st.s, 0, kWave);
+  st.u = __shfl(st.u, 0, kWave);
+  st.idx = __shfl(st.idx, 0, kWave);
   const bool ok = st.s > 0.f && st.m <= FLT_MAX && T >= 0.f;
   const float log_s = logf(st.s);
   auto log_p = [&](float v, int i) {
@@ -307,23 +360,29 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
     __shared__ Collect s;
     if (tid == 0) {
       s.t = 0;
-      s.cnt = 0;
+      s.cnt = s.over = 0;
     }
     __syncthreads();
     const uint64_t* in = lists + static_cast<size_t>(r) * n_chunks * n_top;
-    for (int e = tid; e < n_chunks * n_top; e += kThreads)
-      if (in[e] != 0) s.buf[atomicAdd(&s.cnt, 1)] = in[e];
+    for (int e0 = 0; e0 < n_chunks * n_top; e0 += kSafeStep) {
+      const uint64_t t = s.t;
+      for (int e = e0 + tid; e < min(e0 + kSafeStep, n_chunks * n_top); e += kThreads)
+        if (in[e] > t) collect(s, in[e]);
+      __syncthreads();
+      const bool many = s.cnt > kLimit;
+      __syncthreads();
+      if (many) thin(s, n_top);
+    }
     thin(s, n_top);
     const int cnt = s.cnt;
     const uint64_t mine = tid < cnt ? s.buf[tid] : 0;
-    __syncthreads();
     s.keys[tid] = mine;
     __syncthreads();
     if (mine != 0) {
-      const int k = rank_of(s, mine);
+      const int k = rank_of(s, mine, (cnt + 1) & ~1);
       if (k < n_top) {
         ids[k] = id_of(mine);
-        lps[k] = log_p(z[id_of(mine)], id_of(mine));
+        lps[k] = log_p(value_of(mine), id_of(mine));
       }
     }
     // fewer than n_top logits are not masked: the first masked ids follow (n_top <= V)
@@ -351,7 +410,7 @@ LogprobPlan logprob_plan(int rows, int V, int n_top) {
   p.V = V;
   p.n_top = n_top;
   int want = std::max(1, (kTargetBlocks + rows - 1) / std::max(1, rows));
-  want = std::min(want, std::max(1, V / kStep));
+  want = std::min(want, std::max(1, V / (kStep / 2)));
   // at most kMaxChunks chunks, each a multiple of 1024 elements (16-byte loads)
   const int chunk = std::max((V + want - 1) / want, (V + kMaxChunks - 1) / kMaxChunks);
   p.chunk = (chunk + 1023) / 1024 * 1024;

@@ -393,12 +393,16 @@ spec_status spec_op_kv_copy_pages(int32_t n_planes, int32_t num_pages, size_t pa
   for (int i = 0; i < n; ++i)
     if (is_dst[src_pages[i] / 64] >> (src_pages[i] % 64) & 1)
       return refuse(SPEC_E_INVALID, "spec_op_kv_copy_pages: a destination is also a source");
-  MetaBlock mb;
-  mb.add(pairs);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const spec_status s = upload_tables(workspace, mb, "spec_op_kv_copy_pages: more pairs than a captured call takes", st);
-  if (s != SPEC_OK) return s;
-  return hip_status(launch_kv_copy_pages(static_cast<const int2*>(workspace), n, pool, n_planes, num_pages, page_bytes, st));
+  const bool in_args = sizeof(int2) * n <= kUploadInline;
+  if (!in_args) {
+    MetaBlock mb;
+    mb.add(pairs);
+    const spec_status s = upload_tables(workspace, mb, "spec_op_kv_copy_pages: more pairs than a captured call takes", st);
+    if (s != SPEC_OK) return s;
+  }
+  return hip_status(launch_kv_copy_pages(in_args ? pairs.data() : static_cast<const int2*>(workspace), n, in_args, pool,
+                                         n_planes, num_pages, page_bytes, st));
 } catch (const std::exception&) {
   return refuse(SPEC_E_UNSUPPORTED, "spec_op_kv_copy_pages: out of host memory");
 }
@@ -467,7 +471,7 @@ Kv4Call kv4_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32
     return fail(SPEC_E_INVALID, "spec_op_attention_kv4: bad dtype or size");
   const int G = n_heads / n_kv_heads, dt = dtype == SPEC_F32 ? 0 : 1;
   if (head_dim != 64 && head_dim != 128) return fail(SPEC_E_UNSUPPORTED, "spec_op_attention_kv4: head_dim must be 64 or 128");
-  if (G > 16 * kv4_max_nt(dt))
+  if (G > 16 * (dt == 0 ? kKv4MaxNtF32 : kKv4MaxNt))
     return fail(SPEC_E_UNSUPPORTED, "spec_op_attention_kv4: more query heads per kv head than a tile holds (64 for bf16, 32 for fp32)");
   if (n_seqs > 0 && (!rows || !pos0)) return fail(SPEC_E_INVALID, "spec_op_attention_kv4: null pointer");
   std::vector<AttnSegment> segs;
@@ -484,7 +488,7 @@ Kv4Call kv4_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32
   c.R = static_cast<int>(R);
   c.status = SPEC_OK;
   if (R == 0) return c;
-  c.plan = plan_attention(segs, G, n_kv_heads, kOpMaxParts, kAttnTargetWgs, dt == 1, kv4_max_nt(dt));
+  c.plan = plan_kv4(segs, G, n_kv_heads, kOpMaxParts, dt == 0);
   c.tables = align_up(sizeof(int32_t) * static_cast<size_t>(n_seqs) * max_pages) +
              align_up(sizeof(AttnItem) * c.plan.items.size()) + align_up(sizeof(AttnGroup) * c.plan.groups.size()) +
              (c.plan.prefill ? align_up(sizeof(int32_t) * c.pages) : 0);
@@ -544,8 +548,16 @@ spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const int32_t* 
   const size_t opt = mb.add(table), oit = mb.add(c.plan.items), ogr = mb.add(c.plan.groups), osr = mb.add(src);
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const spec_status s = upload_tables(ws, mb, "spec_op_attention_kv4: larger tables than a captured call takes", st);
-  if (s != SPEC_OK) return s;
+  // small tables of a call that is one kernel travel in its arguments
+  int max_item_pages = 0, max_parts = 0;
+  for (const AttnItem& it : c.plan.items) max_item_pages = std::max(max_item_pages, (it.t1 + 15) / 16 - it.t0 / 16);
+  for (const AttnGroup& g : c.plan.groups) max_parts = std::max(max_parts, g.nparts);
+  const bool in_args = !c.plan.prefill && c.plan.groups.empty() && mb.size() <= kUploadInline &&
+                       max_item_pages <= kKv4StagedPages;
+  if (!in_args) {
+    const spec_status s = upload_tables(ws, mb, "spec_op_attention_kv4: larger tables than a captured call takes", st);
+    if (s != SPEC_OK) return s;
+  }
   AttnArgs a;
   a.dtype = dtype == SPEC_F32 ? 0 : 1;
   a.Hq = n_heads;
@@ -569,8 +581,14 @@ spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const int32_t* 
     a.vpool = ws + c.o_v;
     return hip_status(launch_attention_prefill_bf16(a, items, n_items, c.plan.few_keys, st, true));
   }
-  return hip_status(launch_attention_kv4(a, items, n_items, reinterpret_cast<const AttnGroup*>(ws + ogr),
-                                         static_cast<int>(c.plan.groups.size()), c.plan.nt, c.plan.w, st));
+  Kv4Tables t;
+  t.tables = in_args ? mb.data() : ws;
+  t.inline_bytes = in_args ? mb.size() : 0;
+  t.o_pt = opt;
+  t.o_it = oit;
+  t.o_gr = ogr;
+  return hip_status(launch_attention_kv4(a, t, n_items, static_cast<int>(c.plan.groups.size()), max_parts, c.plan.nt,
+                                         c.plan.w, st));
 } catch (const std::exception&) {
   return refuse(SPEC_E_UNSUPPORTED, "spec_op_attention_kv4: out of host memory");
 }
