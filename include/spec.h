@@ -308,11 +308,33 @@ SPEC_API spec_status spec_decode(spec_ctx* ctx, int32_t n, const int64_t* seq_id
  * Branch, for a caller that drops generated tokens itself).
  * Truncate both caches of a sequence to `new_len` positions (0 <= new_len <=
  * target length); history[new_len] becomes the pending token and outstanding
- * drafts are dropped.  Cleared in place like a commit.  Asynchronous. */
+ * drafts are dropped.  Cleared in place like a commit, but for pages that other
+ * sequences hold too (spec_seq_fork): those are given up as they are, and one that
+ * new_len ends in is replaced by a copy (SPEC_E_NOPAGES if there is no page for
+ * it).  Asynchronous. */
 SPEC_API spec_status spec_kv_rollback(spec_ctx* ctx, int64_t seq_id, int32_t new_len, void* stream);
 
-/* Forget a sequence and free its pages (the request's generation has ended,
- * Section 3.4 Cache-Miss Branch). */
+/* Further sequences with the history, pending token and caches of a live one:
+ * several continuations of one prompt, or the candidates of a beam step, each
+ * generating under its own id (and so its own noise) from here on.  new_ids:
+ * host [n], distinct, not live.  The source holds no drafts and no uncommitted
+ * verify (SPEC_E_STATE).  Pages that the caches fill are shared; each new
+ * sequence gets its own copy of a partly filled last page, so that no sequence
+ * writes where another reads.  Results are those of sequences prefilled and
+ * committed one by one with the same rows.  Pages: lowest-numbered free page
+ * first, new sequences in list order.  Asynchronous. */
+SPEC_API spec_status spec_seq_fork(spec_ctx* ctx, int64_t seq_id, int32_t n, const int64_t* new_ids, void* stream);
+
+/* Renumber both pools' pages so that those in use are 0 .. *pages_target - 1 and
+ * 0 .. *pages_draft - 1 (host outputs, either NULL allowed): what a caller does
+ * before it copies a pool's used part or gives the rest to something else.  The
+ * pages in use from there on, in ascending order, move to the free pages below, in
+ * ascending order; page tables follow (spec_seq_info).  Asynchronous. */
+SPEC_API spec_status spec_kv_compact(spec_ctx* ctx, int32_t* pages_target, int32_t* pages_draft, void* stream);
+
+/* Forget a sequence and give up its pages, which are free once no other
+ * sequence holds them (the request's generation has ended, Section 3.4
+ * Cache-Miss Branch). */
 SPEC_API spec_status spec_seq_release(spec_ctx* ctx, int64_t seq_id);
 
 /* Introspection (host outputs): committed target/draft lengths, pending token

@@ -8,6 +8,7 @@ not built this module raises on first use; there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from ctypes import POINTER, c_float, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 from typing import Optional, Sequence
@@ -74,6 +75,8 @@ SIGNATURES = {
     "spec_kv_commit": (c_int32, [_P, c_int32, _I64P, _I32P, _P]),
     "spec_kv_rollback": (c_int32, [_P, c_int64, c_int32, _P]),
     "spec_seq_release": (c_int32, [_P, c_int64]),
+    "spec_seq_fork": (c_int32, [_P, c_int64, c_int32, _I64P, _P]),
+    "spec_kv_compact": (c_int32, [_P, _I32P, _I32P, _P]),
     "spec_seq_info": (c_int32, [_P, c_int64, _I32P, _I32P, _I32P, _I32P, _I32P, _I32P, _I32P, c_int32]),
     "spec_last_logits": (c_int32, [_P, POINTER(c_void_p), _I32P]),
     "spec_set_graphs": (c_int32, [_P, c_int32]),
@@ -307,6 +310,18 @@ def spec_kv_rollback(ctx: int, seq_id: int, new_len: int, stream=None):
     check(lib().spec_kv_rollback(ctx, int(seq_id), int(new_len), stream_ptr(stream)), ctx)
 
 
+def spec_seq_fork(ctx: int, seq_id: int, new_ids, stream=None):
+    ids = _i64(new_ids)
+    check(lib().spec_seq_fork(ctx, int(seq_id), len(ids), _ptr(ids, _I64P), stream_ptr(stream)), ctx)
+
+
+def spec_kv_compact(ctx: int, stream=None):
+    """Returns the pages in use of the target's and the draft's pool."""
+    t, d = c_int32(), c_int32()
+    check(lib().spec_kv_compact(ctx, ctypes.byref(t), ctypes.byref(d), stream_ptr(stream)), ctx)
+    return t.value, d.value
+
+
 def spec_seq_release(ctx: int, seq_id: int):
     check(lib().spec_seq_release(ctx, int(seq_id)), ctx)
 
@@ -515,6 +530,7 @@ def spec_op_kv_copy_pages(pool, src_pages, dst_pages, workspace, stream=None):
                                       workspace.numel() * workspace.element_size(), stream_ptr(stream)))
 
 
+@functools.lru_cache(maxsize=None)
 def spec_kv4_page_bytes(n_kv_heads: int, head_dim: int) -> int:
     return lib().spec_kv4_page_bytes(n_kv_heads, head_dim)
 
@@ -523,7 +539,7 @@ def spec_op_rope_kv4(dtype: int, R: int, n_heads: int, n_kv_heads: int, head_dim
                      num_pages: int, q_out, k_pages, v_pages, stream=None):
     import torch
     gpu, L = torch.cuda.current_device(), lib()
-    pool = num_pages * L.spec_kv4_page_bytes(n_kv_heads, head_dim)
+    pool = num_pages * spec_kv4_page_bytes(n_kv_heads, head_dim)
     check(L.spec_op_rope_kv4(
         dtype, R, n_heads, n_kv_heads, head_dim, theta,
         _dev(qkv, torch.float32, R * (n_heads + 2 * n_kv_heads) * head_dim, "qkv", gpu),
@@ -537,7 +553,7 @@ def spec_op_kv4_read(dtype: int, R: int, n_kv_heads: int, head_dim: int, slot, n
                      k_out, v_out, stream=None):
     import torch
     gpu, L = torch.cuda.current_device(), lib()
-    n, pool, el = R * n_kv_heads * head_dim, num_pages * L.spec_kv4_page_bytes(n_kv_heads, head_dim), _elem(dtype)
+    n, pool, el = R * n_kv_heads * head_dim, num_pages * spec_kv4_page_bytes(n_kv_heads, head_dim), _elem(dtype)
     check(L.spec_op_kv4_read(
         dtype, R, n_kv_heads, head_dim, _dev(slot, torch.int32, R, "slot", gpu), num_pages,
         _dev(k_pages, torch.uint8, pool, "k_pages", gpu), _dev(v_pages, torch.uint8, pool, "v_pages", gpu),
@@ -560,7 +576,7 @@ def spec_op_attention_kv4(dtype: int, rows, pos0, page_table, num_pages: int, n_
     if r.ndim != 1 or r.shape != p.shape or pt.ndim != 2 or len(pt) != len(r):
         raise ValueError("rows and pos0: one list each, page_table: one row of page ids for each sequence")
     gpu, L = torch.cuda.current_device(), lib()
-    n, pool, el = sum(r.tolist()) * n_heads * head_dim, num_pages * L.spec_kv4_page_bytes(n_kv_heads, head_dim), _elem(dtype)
+    n, pool, el = sum(r.tolist()) * n_heads * head_dim, num_pages * spec_kv4_page_bytes(n_kv_heads, head_dim), _elem(dtype)
     check(L.spec_op_attention_kv4(
         dtype, len(r), _host(r), _host(p), _host(pt), pt.shape[1], num_pages, n_heads, n_kv_heads, head_dim,
         _dev(q, el, n, "q", gpu), _dev(k_pages, torch.uint8, pool, "k_pages", gpu),

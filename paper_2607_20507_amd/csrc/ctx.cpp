@@ -646,6 +646,29 @@ spec_status launch_clears(spec_ctx* ctx, const std::vector<int32_t>& ct, const s
   return SPEC_OK;
 }
 
+// Page copies (from, to) in every layer's K and V of a model's pool.
+spec_status launch_page_copies(spec_ctx* ctx, const Model& M, const std::vector<std::pair<int32_t, int32_t>>& moves,
+                               hipStream_t st) {
+  const size_t page_bytes = static_cast<size_t>(M.d.n_kv_heads) * 16 * M.d.head_dim * M.esz;
+  const size_t most = std::min(ctx->ws.meta_cap / sizeof(int2), kMaxGrid256 / 4096);
+  for (size_t i = 0; i < moves.size(); i += most) {
+    const size_t n = std::min(most, moves.size() - i);
+    std::vector<int2> pairs(n);
+    for (size_t j = 0; j < n; ++j) pairs[j] = make_int2(moves[i + j].first, moves[i + j].second);
+    const bool in_args = sizeof(int2) * n <= kUploadInline;
+    char* dev = nullptr;
+    if (!in_args) {
+      MetaBlock mb;
+      mb.add(pairs);
+      const spec_status s = upload_meta(ctx, mb, st, &dev);
+      if (s != SPEC_OK) return s;
+    }
+    HIPC(launch_kv_copy_pages(in_args ? pairs.data() : reinterpret_cast<const int2*>(dev), static_cast<int>(n), in_args,
+                              M.kv, 2 * M.d.n_layers, M.num_pages, page_bytes, st));
+  }
+  return SPEC_OK;
+}
+
 // The accepted path of tree verifications to consecutive cache positions:
 // mv holds (src, dst) slot pairs, off the group (sequence) boundaries.
 spec_status launch_moves(spec_ctx* ctx, const std::vector<int32_t>& mv, const std::vector<int32_t>& off,
@@ -1528,12 +1551,41 @@ spec_status spec_kv_rollback(spec_ctx* ctx, int64_t seq_id, int32_t new_len, voi
   if (it == ctx->seqs.end()) FAIL(SPEC_E_INVALID, "unknown seq_id");
   Seq& s = it->second;
   if (new_len < 0 || new_len > s.len_t) FAIL(SPEC_E_INVALID, "new_len outside 0..target length");
-  std::vector<int32_t> ct, cd;
   const int new_d = std::min(s.len_d, new_len);
-  for (int p = new_len; p < s.written_t; ++p) ct.push_back(ctx->m[0].pool.slot(s.pages_t, p));
-  for (int p = new_d; p < s.len_d; ++p) cd.push_back(ctx->m[1].pool.slot(s.pages_d, p));
-  ctx->m[0].pool.truncate(s.pages_t, new_len);
-  ctx->m[1].pool.truncate(s.pages_d, new_d);
+  // The last page kept is written next: held by another sequence too, it is
+  // replaced by a copy.  Slots of other shared pages are not cleared.
+  struct Side {
+    PagePool& pool;
+    std::vector<int32_t>& table;
+    int keep, end;
+    bool copy = false;
+    std::vector<int32_t> clear;
+    std::vector<std::pair<int32_t, int32_t>> moves;
+  } side[2] = {{ctx->m[0].pool, s.pages_t, new_len, s.written_t}, {ctx->m[1].pool, s.pages_d, new_d, s.len_d}};
+  for (Side& x : side) {
+    x.copy = x.keep % 16 != 0 && x.pool.shared(x.table[x.keep / 16]);
+    if (x.copy && x.pool.free_pages() + x.pool.freed_by(x.table, x.keep) < 1)
+      FAIL(SPEC_E_NOPAGES, "KV page pool exhausted: the rollback ends in a page that another sequence holds");
+  }
+  for (Side& x : side) {
+    const int last = x.keep / 16;
+    std::vector<int32_t> own;  // slots in pages that go or stay with this sequence alone
+    for (int p = x.keep; p < x.end; ++p)
+      if (p / 16 != last && !x.pool.shared(x.table[p / 16])) own.push_back(x.pool.slot(x.table, p));
+    x.pool.truncate(x.table, x.keep);
+    if (x.copy) {
+      const int32_t from = x.table[last], to = x.pool.take();
+      x.moves.emplace_back(from, to);
+      x.table[last] = to;
+      x.pool.drop(from);
+      // (a page that this call freed may come back as the copy: not to be cleared)
+      own.erase(std::remove_if(own.begin(), own.end(), [&](int32_t sl) { return sl / 16 == to; }), own.end());
+    }
+    // (a page that ends at the new length has gone with the others)
+    if (x.keep % 16 != 0)
+      for (int p = x.keep; p < std::min(x.end, 16 * (last + 1)); ++p) x.clear.push_back(x.pool.slot(x.table, p));
+    x.clear.insert(x.clear.end(), own.begin(), own.end());
+  }
   s.hist.resize(new_len + 1);
   s.len_t = s.written_t = new_len;
   s.len_d = new_d;
@@ -1545,7 +1597,77 @@ spec_status spec_kv_rollback(spec_ctx* ctx, int64_t seq_id, int32_t new_len, voi
   s.emitted.clear();
   s.tparent.clear();
   s.tpath.clear();
-  return launch_clears(ctx, ct, cd, st);
+  for (int i = 0; i < 2; ++i)
+    if (!side[i].moves.empty()) {
+      const spec_status r = launch_page_copies(ctx, ctx->m[i], side[i].moves, st);
+      if (r != SPEC_OK) return r;
+    }
+  return launch_clears(ctx, side[0].clear, side[1].clear, st);
+}
+
+spec_status spec_seq_fork(spec_ctx* ctx, int64_t seq_id, int32_t n, const int64_t* new_ids, void* stream) {
+  CHECK_READY();
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (n < 0 || (n > 0 && !new_ids)) FAIL(SPEC_E_INVALID, "bad arguments");
+  if (!check_ids(ctx, n, new_ids, false)) return SPEC_E_INVALID;
+  auto it = ctx->seqs.find(seq_id);
+  if (it == ctx->seqs.end()) FAIL(SPEC_E_INVALID, "unknown seq_id");
+  const Seq& src = it->second;  // (stays valid when the map grows)
+  if (src.k > 0 || src.verified || src.written_t != src.len_t)
+    FAIL(SPEC_E_STATE, "fork of a sequence with drafts or an uncommitted verify");
+  for (int i = 0; i < n; ++i)
+    if (ctx->seqs.count(new_ids[i])) FAIL(SPEC_E_INVALID, "seq_id already live");
+  if (static_cast<int>(ctx->free_slots.size()) < n) FAIL(SPEC_E_INVALID, "more live sequences than max_seqs");
+  const int len[2] = {src.len_t, src.len_d};
+  const std::vector<int32_t>* from[2] = {&src.pages_t, &src.pages_d};
+  for (int m = 0; m < ctx->n_models; ++m)
+    if (len[m] % 16 != 0 && n > ctx->m[m].pool.free_pages()) FAIL(SPEC_E_NOPAGES, "KV page pool exhausted");
+  std::vector<std::pair<int32_t, int32_t>> moves[2];
+  for (int i = 0; i < n; ++i) {
+    Seq s;
+    s.id = new_ids[i];
+    s.slot = ctx->free_slots.top();
+    ctx->free_slots.pop();
+    s.hist = src.hist;
+    s.len_t = s.written_t = src.len_t;
+    s.len_d = src.len_d;
+    std::vector<int32_t>* to[2] = {&s.pages_t, &s.pages_d};
+    for (int m = 0; m < ctx->n_models; ++m) {
+      // full pages are never written again; the last one, written next, is copied
+      PagePool& pool = ctx->m[m].pool;
+      pool.share(*from[m], len[m] / 16, *to[m]);
+      if (len[m] % 16 != 0) {
+        to[m]->push_back(pool.take());
+        moves[m].emplace_back((*from[m])[len[m] / 16], to[m]->back());
+      }
+    }
+    ctx->seqs[s.id] = std::move(s);
+  }
+  for (int m = 0; m < ctx->n_models; ++m) {
+    const spec_status r = launch_page_copies(ctx, ctx->m[m], moves[m], st);
+    if (r != SPEC_OK) return r;
+  }
+  return SPEC_OK;
+}
+
+spec_status spec_kv_compact(spec_ctx* ctx, int32_t* pages_target, int32_t* pages_draft, void* stream) {
+  CHECK_READY();
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  for (int m = 0; m < ctx->n_models; ++m) {
+    Model& M = ctx->m[m];
+    const auto moves = M.pool.compact();
+    if (moves.empty()) continue;
+    std::vector<int32_t> name(M.num_pages);
+    for (int p = 0; p < M.num_pages; ++p) name[p] = p;
+    for (const auto& mv : moves) name[mv.first] = mv.second;
+    for (auto& kv : ctx->seqs)
+      for (int32_t& p : m == 0 ? kv.second.pages_t : kv.second.pages_d) p = name[p];
+    const spec_status r = launch_page_copies(ctx, M, moves, st);
+    if (r != SPEC_OK) return r;
+  }
+  if (pages_target) *pages_target = ctx->m[0].num_pages - ctx->m[0].pool.free_pages();
+  if (pages_draft) *pages_draft = ctx->n_models == 2 ? ctx->m[1].num_pages - ctx->m[1].pool.free_pages() : 0;
+  return SPEC_OK;
 }
 
 spec_status spec_seq_release(spec_ctx* ctx, int64_t seq_id) {

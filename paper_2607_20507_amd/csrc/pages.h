@@ -3,12 +3,15 @@
 //
 // Page indices are a deterministic function of the history of lengths:
 // allocation always takes the lowest-numbered free page, and a page returns
-// to the pool as soon as it holds no position below its sequence's length.
+// to the pool as soon as no table holds it: with no sharing, as soon as it holds
+// no position below its sequence's length.  Several tables may hold a page
+// (share); whoever writes to one must hold it alone.
 #pragma once
 
 #include <cstdint>
 #include <functional>
 #include <queue>
+#include <utility>
 #include <vector>
 
 namespace spec {
@@ -22,6 +25,7 @@ class PagePool {
     num_pages_ = num_pages;
     free_ = decltype(free_)();
     for (int p = 0; p < num_pages; ++p) free_.push(p);
+    holders_.assign(num_pages, 0);
   }
 
   int page_size() const { return page_size_; }
@@ -39,19 +43,57 @@ class PagePool {
   bool ensure(std::vector<int32_t>& table, int64_t length) {
     const int n = need(table, length);
     if (n > free_pages()) return false;
-    for (int i = 0; i < n; ++i) {
-      table.push_back(free_.top());
-      free_.pop();
-    }
+    for (int i = 0; i < n; ++i) table.push_back(take());
     return true;
   }
-  // Free pages holding no position below `length`.
+  // Give up pages holding no position below `length`.
   void truncate(std::vector<int32_t>& table, int64_t length) {
     const int keep = pages_for(length);
     while (static_cast<int>(table.size()) > keep) {
-      free_.push(table.back());
+      drop(table.back());
       table.pop_back();
     }
+  }
+  // The lowest-numbered free page (there is one), held once.
+  int32_t take() {
+    const int32_t p = free_.top();
+    free_.pop();
+    holders_[p] = 1;
+    return p;
+  }
+  // Hold the first n pages of `from` in `to` (empty) too.
+  void share(const std::vector<int32_t>& from, int n, std::vector<int32_t>& to) {
+    to.assign(from.begin(), from.begin() + n);
+    for (int32_t p : to) ++holders_[p];
+  }
+  bool shared(int32_t page) const { return holders_[page] > 1; }
+  // One holder less; the page is free with the last.
+  void drop(int32_t page) {
+    if (--holders_[page] == 0) free_.push(page);
+  }
+  // Pages that truncate(table, length) would free.
+  int freed_by(const std::vector<int32_t>& table, int64_t length) const {
+    int n = 0;
+    for (size_t i = pages_for(length); i < table.size(); ++i) n += holders_[table[i]] == 1;
+    return n;
+  }
+  // Renumber the held pages to 0 .. live - 1, moving as few as possible: the held
+  // pages from `live` on, ascending, to the free ones below it, ascending.  Returns
+  // the (from, to) pairs; the caller moves the contents and renames its tables.
+  std::vector<std::pair<int32_t, int32_t>> compact() {
+    const int live = num_pages_ - free_pages();
+    std::vector<std::pair<int32_t, int32_t>> moves;
+    int to = 0;
+    for (int from = live; from < num_pages_; ++from) {
+      if (holders_[from] == 0) continue;
+      while (holders_[to] != 0) ++to;
+      moves.emplace_back(from, to++);
+    }
+    for (const auto& m : moves) std::swap(holders_[m.first], holders_[m.second]);
+    decltype(free_) left;
+    for (int p = live; p < num_pages_; ++p) left.push(p);
+    free_.swap(left);
+    return moves;
   }
   int32_t slot(const std::vector<int32_t>& table, int64_t pos) const {
     return table[pos / page_size_] * page_size_ + static_cast<int32_t>(pos % page_size_);
@@ -60,6 +102,7 @@ class PagePool {
  private:
   int page_size_ = 16;
   int num_pages_ = 0;
+  std::vector<int32_t> holders_;  // tables that hold a page
   std::priority_queue<int32_t, std::vector<int32_t>, std::greater<int32_t>> free_;
 };
 

@@ -7,6 +7,7 @@ models) into device tensors that the library reads through raw pointers.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from typing import Dict, List, Optional, Sequence
 
@@ -173,6 +174,14 @@ class SpecSession:
     def rollback(self, seq_id: int, new_len: int, stream=None):
         B.spec_kv_rollback(self.ctx, seq_id, new_len, stream)
 
+    def fork(self, seq_id: int, new_ids, stream=None):
+        """New sequences that continue where seq_id stands; full pages are shared."""
+        B.spec_seq_fork(self.ctx, seq_id, new_ids, stream)
+
+    def compact(self, stream=None):
+        """Pages in use to the front of both pools: (target, draft) pages in use."""
+        return B.spec_kv_compact(self.ctx, stream)
+
     def release(self, seq_id: int):
         B.spec_seq_release(self.ctx, seq_id)
 
@@ -191,11 +200,35 @@ class SpecSession:
         off = ptr - self.ws_view.data_ptr()
         return self.ws_view[off:off + V * 4].view(torch.float32).clone()
 
-    def last_logits(self) -> torch.Tensor:
-        """Copy of the last verify's target logits [rows, V] (fp32)."""
+    def _last_logits(self) -> torch.Tensor:
+        """The last verify's target logits [rows, V] (fp32), in this session's workspace."""
         ptr, rows = B.spec_last_logits(self.ctx)
         V = self.target.shape.vocab
         base = self.ws_view.data_ptr()
         off = ptr - base
         flat = self.ws_view[off:off + rows * V * 4].view(torch.float32)
-        return flat.view(rows, V).clone()
+        return flat.view(rows, V)
+
+    def last_logits(self) -> torch.Tensor:
+        """Copy of the last verify's target logits [rows, V] (fp32)."""
+        return self._last_logits().clone()
+
+    def token_logprobs(self, tokens=None, temps=None, n_top: int = 0, stream=None):
+        """Log probabilities of `tokens` (one per row of the last verify or target forward, host
+        ints; None: not wanted), the rows' entropy and their n_top most likely tokens, at
+        temperatures `temps` (one per row; None: 1).  Returns device tensors (logprobs or None,
+        entropy, top ids, top logprobs)."""
+        z = self._last_logits()
+        R, V = z.shape
+        dev = z.device
+        # buffers of the stream that the call runs on
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            tok = None if tokens is None else torch.from_numpy(np.asarray(tokens, dtype=np.int32)).to(dev)
+            t = None if temps is None else torch.from_numpy(np.asarray(temps, dtype=np.float32)).to(dev)
+            logp = None if tok is None else torch.empty(R, device=dev)
+            entropy = torch.empty(R, device=dev)
+            ids = torch.empty(R, n_top, dtype=torch.int32, device=dev)
+            top = torch.empty(R, n_top, device=dev)
+            ws = torch.empty(max(16, B.spec_token_logprobs_workspace_bytes(R, V, n_top)), dtype=torch.uint8, device=dev)
+            B.spec_token_logprobs(z, t, tok, logp, entropy, ids if n_top else None, top if n_top else None, ws)
+        return logp, entropy, ids, top
