@@ -479,7 +479,9 @@ def _elem(dtype: int):
 
 
 def _host(a: np.ndarray) -> int:
-    return a.__array_interface__["data"][0]
+    if a.flags.writeable and a.nbytes:
+        return ctypes.addressof(ctypes.c_char.from_buffer(a))  # a third of the time of a.ctypes
+    return a.ctypes.data
 
 
 def spec_token_logprobs_workspace_bytes(rows: int, V: int, n_top: int) -> int:

@@ -15,13 +15,15 @@
 // integer of the same order) above the complement of the id, so that equal
 // values go to the lower id and every key is different.  A workgroup keeps a
 // value that at least n_top elements with lower ids reach and collects in LDS
-// what is above it.  That value first comes from the threads' maxima of the
-// first 4096 elements; where many keys were collected it is raised to the
-// n_top-th largest of 256 disjoint subsets' maxima, above which at most n_top
-// subsets hold anything.  A chunk whose logits ascend can collect more than the
-// buffer holds: it is then read once more in steps that cannot.  Masked logits
-// (-inf) are never collected: where fewer than n_top remain, the final kernel
-// appends the first masked ids.
+// what is above it: the n_top-th largest of the threads' maxima so far, found by
+// votes after steps 1, 2, 4, 8, 12, .. (20 of 128256 normal logits collect about
+// 130 keys; with the first step's value alone 630, and a pass over 1792 rows took
+// 184 us against 16x).  Where many keys pile up all the same they are thinned to
+// those above the n_top-th largest of 256 disjoint subsets' maxima, which at most
+// n_top subsets are.  A chunk whose logits ascend can collect more than the buffer
+// holds: it is then read once more in steps that cannot.  Masked logits (-inf) are
+// never collected: where fewer than n_top remain, the final kernel appends the
+// first masked ids.
 
 #include <algorithm>
 #include <cfloat>
@@ -38,7 +40,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kPerThread = 16;
 constexpr int kStep = kThreads * kPerThread;
-constexpr int kLook = 4;              // steps between two looks at the collected keys
+constexpr int kLook = 4;              // steps between two looks at the collected keys (1 and 2 at first)
 constexpr int kLimit = 512;           // collected keys above this are thinned
 constexpr int kCap = 2048;
 constexpr int kSafeStep = kThreads * 4;  // a step of the second reading
@@ -102,7 +104,7 @@ struct Collect {
   alignas(16) uint64_t keys[kThreads];
   uint64_t buf[kCap];
   uint64_t t;
-  float first[kWaves];
+  float reach[kWaves];
   int cnt, over;
 };
 
@@ -197,6 +199,19 @@ __global__ __launch_bounds__(kThreads) void logprob_chunk_kernel(int V, const fl
       for (int e = 0; e < kPerThread; ++e) v[e] = id(base, e) < end ? z[id(base, e)] : -INFINITY;
     }
   };
+  // tv, or the value that n_top of the threads' values x reach if that is more:
+  // each wave's share of them reaches its value, so all of them the least of those
+  auto raise = [&](float x, float tv) {
+    if constexpr (TOP) {
+      const float w = reached_by(x, (n_top + kWaves - 1) / kWaves);
+      __syncthreads();
+      if ((tid & (kWave - 1)) == 0) s.reach[wave] = w;
+      __syncthreads();
+      static_assert(kWaves == 4, "one value a wave");
+      tv = fmaxf(tv, fminf(fminf(s.reach[0], s.reach[1]), fminf(s.reach[2], s.reach[3])));
+    }
+    return tv;
+  };
   LpStat st{-FLT_MAX, 0.f, 0.f, INT_MAX};
   float tv = -INFINITY;
   float v[kPerThread], next[kPerThread];
@@ -226,25 +241,15 @@ __global__ __launch_bounds__(kThreads) void logprob_chunk_kernel(int V, const fl
       st.u = fmaf(fmaxf(t, kFloor), p, st.u);
     }
     if constexpr (TOP) {
-      if (i == 0) {
-        // each wave's share of n_top maxima reaches its value, so n_top reach the least of them
-        const float w = reached_by(vm, (n_top + kWaves - 1) / kWaves);
-        if ((tid & (kWave - 1)) == 0) s.first[wave] = w;
-        __syncthreads();
-        tv = fminf(fminf(s.first[0], s.first[1]), fminf(s.first[2], s.first[3]));
-        static_assert(kWaves == 4, "one value a wave");
-        if (vm >= tv) {
-#pragma unroll
-          for (int e = 0; e < kPerThread; ++e)
-            if (v[e] >= tv && v[e] > -INFINITY) collect(s, key_of(v[e], id(base, e)));
-        }
-      } else if (vm > tv) {  // n_top elements with lower ids reach tv: an equal value here comes after them
+      // in the first step from a value that n_top elements of it reach
+      if (i == 0) tv = raise(vm, tv);
+      if (i == 0 ? vm >= tv : vm > tv) {  // (later an equal value comes after those that reach tv)
 #pragma unroll
         for (int e = 0; e < kPerThread; ++e)
-          if (v[e] > tv) collect(s, key_of(v[e], id(base, e)));
+          if ((v[e] > tv || (i == 0 && v[e] == tv)) && v[e] > -INFINITY) collect(s, key_of(v[e], id(base, e)));
       }
-      if (i % kLook == kLook - 1) {
-        __syncthreads();
+      if ((i & (i + 1)) == 0 ? i > 0 : i % kLook == kLook - 1) {
+        tv = raise(st.idx == INT_MAX ? -INFINITY : st.m, tv);
         const bool many = s.cnt > kLimit;
         __syncthreads();  // nobody adds before everybody has looked
         if (many) {
@@ -365,9 +370,22 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
     __syncthreads();
     const uint64_t* in = lists + static_cast<size_t>(r) * n_chunks * n_top;
     for (int e0 = 0; e0 < n_chunks * n_top; e0 += kSafeStep) {
-      const uint64_t t = s.t;
-      for (int e = e0 + tid; e < min(e0 + kSafeStep, n_chunks * n_top); e += kThreads)
-        if (in[e] > t) collect(s, in[e]);
+      uint64_t own[kSafeStep / kThreads], mx = s.t;
+#pragma unroll
+      for (int i = 0; i < kSafeStep / kThreads; ++i) {
+        const int e = e0 + i * kThreads + tid;
+        own[i] = e < n_chunks * n_top ? in[e] : 0;
+        mx = own[i] > mx ? own[i] : mx;
+      }
+      // a value that n_top keys reach, as in the chunks (keys below it are not needed)
+      const float w = reached_by(mx ? value_of(mx) : -INFINITY, (n_top + kWaves - 1) / kWaves);
+      if (lane == 0) s.reach[tid / kWave] = w;
+      __syncthreads();
+      const uint64_t t = static_cast<uint64_t>(
+          ordered(fminf(fminf(s.reach[0], s.reach[1]), fminf(s.reach[2], s.reach[3])))) << 32;
+#pragma unroll
+      for (int i = 0; i < kSafeStep / kThreads; ++i)
+        if (own[i] > t) collect(s, own[i]);
       __syncthreads();
       const bool many = s.cnt > kLimit;
       __syncthreads();

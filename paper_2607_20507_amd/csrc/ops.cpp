@@ -485,12 +485,22 @@ Kv4Call kv4_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32
     if (rows[i] > 0) c.pages += (len + 15) / 16;
     R += rows[i];
   }
+  if (c.pages > INT32_MAX) return fail(SPEC_E_INVALID, "spec_op_attention_kv4: too many pages");
   c.R = static_cast<int>(R);
   c.status = SPEC_OK;
   if (R == 0) return c;
   c.plan = plan_kv4(segs, G, n_kv_heads, kOpMaxParts, dt == 0);
-  c.tables = align_up(sizeof(int32_t) * static_cast<size_t>(n_seqs) * max_pages) +
-             align_up(sizeof(AttnItem) * c.plan.items.size()) + align_up(sizeof(AttnGroup) * c.plan.groups.size()) +
+  // the page ids that the call reads, one sequence after the other: an item finds
+  // its sequence's at it.seq (the kernels' max_pages is 1)
+  std::vector<int32_t> first(n_seqs, 0);
+  int64_t pages = 0;
+  for (const AttnSegment& s : segs) {
+    first[s.seq] = static_cast<int32_t>(pages);
+    pages += (static_cast<int64_t>(s.pos0) + s.nrows + 15) / 16;
+  }
+  for (AttnItem& it : c.plan.items) it.seq = first[it.seq];
+  c.tables = align_up(sizeof(int32_t) * c.pages) + align_up(sizeof(AttnItem) * c.plan.items.size()) +
+             align_up(sizeof(AttnGroup) * c.plan.groups.size()) +
              (c.plan.prefill ? align_up(sizeof(int32_t) * c.pages) : 0);
   c.o_part = c.tables;
   c.o_ml = c.o_part + align_up(sizeof(float) * static_cast<size_t>(c.plan.n_parts) * n_kv_heads * 64 * head_dim);
@@ -528,21 +538,20 @@ spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const int32_t* 
       misaligned(workspace, 256) || workspace_bytes < c.bytes)
     return refuse(SPEC_E_INVALID,
                   "spec_op_attention_kv4: buffers must be 16-byte aligned, the workspace 256-byte aligned and large enough");
-  // the pages that the call reads, compact where they are expanded
-  std::vector<int32_t> table(static_cast<size_t>(n_seqs) * max_pages, 0), src;
+  std::vector<int32_t> table, src;
+  table.reserve(c.pages);
   for (int i = 0; i < n_seqs; ++i) {
     const int n = rows[i] > 0 ? static_cast<int>((static_cast<int64_t>(pos0[i]) + rows[i] + 15) / 16) : 0;
-    for (int j = 0; j < n; ++j) {
-      const size_t e = static_cast<size_t>(i) * max_pages + j;
-      const int32_t p = page_table[e];
-      if (p < 0 || p >= num_pages) return refuse(SPEC_E_INVALID, "spec_op_attention_kv4: page outside the pool");
-      if (c.plan.prefill) {
-        table[e] = static_cast<int32_t>(src.size());
-        src.push_back(p);
-      } else {
-        table[e] = p;
-      }
-    }
+    const int32_t* from = page_table + static_cast<size_t>(i) * max_pages;
+    for (int j = 0; j < n; ++j)
+      if (from[j] < 0 || from[j] >= num_pages)
+        return refuse(SPEC_E_INVALID, "spec_op_attention_kv4: page outside the pool");
+    table.insert(table.end(), from, from + n);
+  }
+  if (c.plan.prefill) {  // the prompt kernel reads expanded pages, numbered as they are listed
+    src.swap(table);
+    table.resize(src.size());
+    for (size_t j = 0; j < table.size(); ++j) table[j] = static_cast<int32_t>(j);
   }
   MetaBlock mb;
   const size_t opt = mb.add(table), oit = mb.add(c.plan.items), ogr = mb.add(c.plan.groups), osr = mb.add(src);
@@ -567,7 +576,7 @@ spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const int32_t* 
   a.kpool = k_pages;
   a.vpool = v_pages;
   a.page_table = reinterpret_cast<const int32_t*>(ws + opt);
-  a.max_pages = max_pages;
+  a.max_pages = 1;
   a.out = out;
   a.part_o = reinterpret_cast<float*>(ws + c.o_part);
   a.part_ml = reinterpret_cast<float*>(ws + c.o_ml);
