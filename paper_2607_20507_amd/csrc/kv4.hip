@@ -315,10 +315,10 @@ __device__ __forceinline__ void store4(float* o, const f32x4& v) {
 
 // The waves' states are merged through LDS, each wave taking some of the output
 // tiles, and the output or the partial is written.  m: base-2 logit that a lane's
-// sums are relative to (-inf: no key), l: its share of the sum.
+// sums are relative to (-inf: no key), l: the wave's sum (in every element).
 template <typename T, int HD, int NT, int W>
 __device__ __forceinline__ void finish(const AttnArgs& a, const AttnItem& it, int gkv, int M, int lane, int wave,
-                                       const float (&m)[NT], const float (&l)[NT], const f32x4 (&acc)[HD / 16][NT]) {
+                                       const float (&m)[NT], const f32x4 (&l)[NT], const f32x4 (&acc)[HD / 16][NT]) {
   constexpr int DT = HD / 16;
   const int g = lane >> 4, l16 = lane & 15;
   const int G = a.Hq / a.Hkv;
@@ -329,13 +329,10 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const AttnItem& it, in
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     if (16 * nt >= M) break;
-    float lt = l[nt];
-    lt += __shfl_xor(lt, 16, kWave);
-    lt += __shfl_xor(lt, 32, kWave);
     if (nt > 0) __syncthreads();
     if (g == 0) {
       s_m[wave][l16] = m[nt];
-      s_l[wave][l16] = lt;
+      s_l[wave][l16] = l[nt][0];
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) s_acc[wave][dt][lane] = acc[dt][nt];
@@ -344,7 +341,7 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const AttnItem& it, in
     float mm = -INFINITY, e[W];
 #pragma unroll
     for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_m[w][l16]);
-    lt = 0.f;
+    float lt = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       e[w] = s_m[w][l16] == -INFINITY ? 0.f : exp2f(s_m[w][l16] - mm);
@@ -439,13 +436,18 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
   for (int nt = 0; nt < NT; ++nt) klim[nt] = vval[nt] ? min(vpos[nt], it.t1 - 1) : -1;
   // the running maximum of the raw scores, the score above which it is raised,
   // minus its base-2 logit
-  float mrun[NT], mlim[NT], mneg[NT], lrun[NT];
+  // (sums of the probabilities as the products see them, rounded, by a product
+  // with ones: 16 additions a chunk less, and the rounding cancels in the quotient)
+  float mrun[NT], mlim[NT], mneg[NT];
+  f32x4 lrun[NT];
+  const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
   bool far = false;
   f32x4 acc[DT][NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     mrun[nt] = mlim[nt] = -INFINITY;
-    mneg[nt] = lrun[nt] = 0.f;
+    mneg[nt] = 0.f;
+    lrun[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -552,7 +554,7 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
       uint4 pf[NT][NP];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float p[8], ps = 0.f;
+        float p[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(raw[nt][j], scale, mneg[nt]));
         if (far) {
@@ -561,14 +563,14 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
 #pragma unroll
           for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f((raw[nt][j] - m) * scale);
         }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) ps += p[j];
-        lrun[nt] += ps;
         uint32_t h[4][NP];
 #pragma unroll
         for (int j = 0; j < 4; ++j) split_pair<NP>(p[2 * j], p[2 * j + 1], h[j]);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) pf[nt][i] = make_uint4(h[0][i], h[1][i], h[2][i], h[3][i]);
+        for (int i = 0; i < NP; ++i) {
+          pf[nt][i] = make_uint4(h[0][i], h[1][i], h[2][i], h[3][i]);
+          lrun[nt] = mfma16x16x32(ones, pf[nt][i], lrun[nt]);
+        }
       }
       if (c0 + 32 > it.t1) {  // keys past the end hold anything, and 0 x NaN is not 0
         asm volatile("");

@@ -188,15 +188,17 @@ __global__ __launch_bounds__(kThreads) void logprob_chunk_kernel(int V, const fl
     return VEC ? base + (e / 4) * 4 * kThreads + 4 * tid + e % 4 : base + e * kThreads + tid;
   };
   auto load = [&](int base, float (&v)[kPerThread]) {
-    if (VEC && base + kStep <= end) {
+    // (chunks are multiples of 1024 elements: whole rounds of 16-byte loads, but for a row's end)
 #pragma unroll
-      for (int q = 0; q < kPerThread / 4; ++q) {
+    for (int q = 0; q < kPerThread / 4; ++q) {
+      const int q0 = base + q * 4 * kThreads;
+      if (VEC && q0 + 4 * kThreads <= end) {
         const float4 w = ld_stream(reinterpret_cast<const float4*>(z + id(base, 4 * q)));
         v[4 * q] = w.x; v[4 * q + 1] = w.y; v[4 * q + 2] = w.z; v[4 * q + 3] = w.w;
-      }
-    } else {
+      } else {
 #pragma unroll
-      for (int e = 0; e < kPerThread; ++e) v[e] = id(base, e) < end ? z[id(base, e)] : -INFINITY;
+        for (int e = 4 * q; e < 4 * q + 4; ++e) v[e] = id(base, e) < end ? z[id(base, e)] : -INFINITY;
+      }
     }
   };
   // tv, or the value that n_top of the threads' values x reach if that is more:
@@ -326,6 +328,21 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
   const float* z = logits + static_cast<int64_t>(r) * ld;
   const float T = temps ? temps[r] : 1.f;
   const float c = base2_factor(T);
+  // every load that depends on nothing goes out first
+  const uint64_t* in = lists + static_cast<size_t>(r) * n_chunks * n_top;
+  constexpr int kOwn = kSafeStep / kThreads;
+  uint64_t own[kOwn];
+  auto load = [&](int e0) {
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      const int e = e0 + i * kThreads + tid;
+      own[i] = e < n_chunks * n_top ? in[e] : 0;
+    }
+  };
+  if constexpr (TOP) load(0);
+  const int given = tokens ? tokens[r] : -1;
+  const bool given_in = given >= 0 && given < V;
+  const float z_given = given_in ? z[given] : -INFINITY;
   // every wave merges the row's records (n_chunks <= 64)
   LpStat st{-FLT_MAX, 0.f, 0.f, INT_MAX};
   const int lane = tid & (kWave - 1);
@@ -345,10 +362,8 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
   };
   if (tid == 0) {
     if (logp) {
-      const int t = tokens ? tokens[r] : -1;
-      const bool in = t >= 0 && t < V;
-      const float v = log_p(in ? z[t] : -INFINITY, t);
-      logp[r] = in || !ok ? v : -INFINITY;
+      const float p = log_p(z_given, given);
+      logp[r] = given_in || !ok ? p : -INFINITY;
     }
     if (entropy) entropy[r] = !ok ? __builtin_nanf("") : T == 0.f ? 0.f : fmaxf(log_s - st.u * kLn2 / st.s, 0.f);
   }
@@ -368,15 +383,11 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
       s.cnt = s.over = 0;
     }
     __syncthreads();
-    const uint64_t* in = lists + static_cast<size_t>(r) * n_chunks * n_top;
     for (int e0 = 0; e0 < n_chunks * n_top; e0 += kSafeStep) {
-      uint64_t own[kSafeStep / kThreads], mx = s.t;
+      if (e0 > 0) load(e0);
+      uint64_t mx = s.t;
 #pragma unroll
-      for (int i = 0; i < kSafeStep / kThreads; ++i) {
-        const int e = e0 + i * kThreads + tid;
-        own[i] = e < n_chunks * n_top ? in[e] : 0;
-        mx = own[i] > mx ? own[i] : mx;
-      }
+      for (int i = 0; i < kOwn; ++i) mx = own[i] > mx ? own[i] : mx;
       // a value that n_top keys reach, as in the chunks (keys below it are not needed)
       const float w = reached_by(mx ? value_of(mx) : -INFINITY, (n_top + kWaves - 1) / kWaves);
       if (lane == 0) s.reach[tid / kWave] = w;
@@ -384,7 +395,7 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
       const uint64_t t = static_cast<uint64_t>(
           ordered(fminf(fminf(s.reach[0], s.reach[1]), fminf(s.reach[2], s.reach[3])))) << 32;
 #pragma unroll
-      for (int i = 0; i < kSafeStep / kThreads; ++i)
+      for (int i = 0; i < kOwn; ++i)
         if (own[i] > t) collect(s, own[i]);
       __syncthreads();
       const bool many = s.cnt > kLimit;
