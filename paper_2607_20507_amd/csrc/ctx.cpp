@@ -19,6 +19,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <exception>
 #include <cstdio>
 #include <cstring>
 #include <functional>
@@ -648,7 +649,7 @@ spec_status launch_clears(spec_ctx* ctx, const std::vector<int32_t>& ct, const s
 
 // Page copies (from, to) in every layer's K and V of a model's pool.
 spec_status launch_page_copies(spec_ctx* ctx, const Model& M, const std::vector<std::pair<int32_t, int32_t>>& moves,
-                               hipStream_t st) {
+                               hipStream_t st) try {
   const size_t page_bytes = static_cast<size_t>(M.d.n_kv_heads) * 16 * M.d.head_dim * M.esz;
   const size_t most = std::min(ctx->ws.meta_cap / sizeof(int2), kMaxGrid256 / 4096);
   for (size_t i = 0; i < moves.size(); i += most) {
@@ -667,6 +668,9 @@ spec_status launch_page_copies(spec_ctx* ctx, const Model& M, const std::vector<
                               M.kv, 2 * M.d.n_layers, M.num_pages, page_bytes, st));
   }
   return SPEC_OK;
+} catch (const std::exception&) {  // the tables name the copies already
+  ctx->broken = true;
+  FAIL(SPEC_E_HIP, "out of host memory");
 }
 
 // The accepted path of tree verifications to consecutive cache positions:
@@ -1622,15 +1626,29 @@ spec_status spec_seq_fork(spec_ctx* ctx, int64_t seq_id, int32_t n, const int64_
   const std::vector<int32_t>* from[2] = {&src.pages_t, &src.pages_d};
   for (int m = 0; m < ctx->n_models; ++m)
     if (len[m] % 16 != 0 && n > ctx->m[m].pool.free_pages()) FAIL(SPEC_E_NOPAGES, "KV page pool exhausted");
+  // everything that allocates comes before the first change that lasts
   std::vector<std::pair<int32_t, int32_t>> moves[2];
+  int made = 0;
+  try {
+    for (auto& m : moves) m.reserve(n);
+    for (; made < n; ++made) {
+      Seq s;
+      s.id = new_ids[made];
+      s.hist = src.hist;
+      s.len_t = s.written_t = src.len_t;
+      s.len_d = src.len_d;
+      s.pages_t.reserve(len[0] / 16 + 1);
+      s.pages_d.reserve(len[1] / 16 + 1);
+      ctx->seqs.emplace(s.id, std::move(s));
+    }
+  } catch (const std::exception&) {
+    for (int i = 0; i < made; ++i) ctx->seqs.erase(new_ids[i]);
+    FAIL(SPEC_E_UNSUPPORTED, "out of host memory");
+  }
   for (int i = 0; i < n; ++i) {
-    Seq s;
-    s.id = new_ids[i];
+    Seq& s = ctx->seqs.find(new_ids[i])->second;
     s.slot = ctx->free_slots.top();
     ctx->free_slots.pop();
-    s.hist = src.hist;
-    s.len_t = s.written_t = src.len_t;
-    s.len_d = src.len_d;
     std::vector<int32_t>* to[2] = {&s.pages_t, &s.pages_d};
     for (int m = 0; m < ctx->n_models; ++m) {
       // full pages are never written again; the last one, written next, is copied
@@ -1641,7 +1659,6 @@ spec_status spec_seq_fork(spec_ctx* ctx, int64_t seq_id, int32_t n, const int64_
         moves[m].emplace_back((*from[m])[len[m] / 16], to[m]->back());
       }
     }
-    ctx->seqs[s.id] = std::move(s);
   }
   for (int m = 0; m < ctx->n_models; ++m) {
     const spec_status r = launch_page_copies(ctx, ctx->m[m], moves[m], st);
@@ -1655,9 +1672,15 @@ spec_status spec_kv_compact(spec_ctx* ctx, int32_t* pages_target, int32_t* pages
   hipStream_t st = static_cast<hipStream_t>(stream);
   for (int m = 0; m < ctx->n_models; ++m) {
     Model& M = ctx->m[m];
-    const auto moves = M.pool.compact();
+    std::vector<std::pair<int32_t, int32_t>> moves;
+    std::vector<int32_t> name;  // of every page after the moves
+    try {
+      name.resize(M.num_pages);
+      moves = M.pool.compact();
+    } catch (const std::exception&) {
+      FAIL(SPEC_E_UNSUPPORTED, "out of host memory");
+    }
     if (moves.empty()) continue;
-    std::vector<int32_t> name(M.num_pages);
     for (int p = 0; p < M.num_pages; ++p) name[p] = p;
     for (const auto& mv : moves) name[mv.first] = mv.second;
     for (auto& kv : ctx->seqs)

@@ -45,6 +45,14 @@ spec_status refuse(spec_status s, const char* msg) {
   return s;
 }
 
+// Status of a call's last launch, with a message if it failed.
+spec_status launched(hipError_t e, const char* call) {
+  const spec_status s = hip_status(e);
+  if (s == SPEC_E_UNSUPPORTED) set_global_error((std::string(call) + ": more workgroups than a launch holds").c_str());
+  else if (s != SPEC_OK) set_global_error((std::string(call) + ": " + hipGetErrorString(e)).c_str());
+  return s;
+}
+
 bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
 
 // Tables of a call to its workspace.  A stream that is being captured takes
@@ -361,8 +369,8 @@ spec_status spec_token_logprobs(int32_t rows, int32_t V, const float* logits, in
     return refuse(SPEC_E_INVALID, "spec_token_logprobs: misaligned logits or workspace");
   const LogprobPlan p = logprob_plan(rows, V, n_top);
   if (workspace_bytes < logprob_ws_bytes(p)) return refuse(SPEC_E_INVALID, "spec_token_logprobs: workspace too small");
-  return hip_status(launch_logprobs(p, logits, row_stride, temperature, tokens, logprobs, entropy, top_ids,
-                                    top_logprobs, workspace, static_cast<hipStream_t>(stream)));
+  return launched(launch_logprobs(p, logits, row_stride, temperature, tokens, logprobs, entropy, top_ids,
+                                    top_logprobs, workspace, static_cast<hipStream_t>(stream)), "spec_token_logprobs");
 }
 
 // ---------------------------------------------------------------------------
@@ -401,8 +409,8 @@ spec_status spec_op_kv_copy_pages(int32_t n_planes, int32_t num_pages, size_t pa
     const spec_status s = upload_tables(workspace, mb, "spec_op_kv_copy_pages: more pairs than a captured call takes", st);
     if (s != SPEC_OK) return s;
   }
-  return hip_status(launch_kv_copy_pages(in_args ? pairs.data() : static_cast<const int2*>(workspace), n, in_args, pool,
-                                         n_planes, num_pages, page_bytes, st));
+  return launched(launch_kv_copy_pages(in_args ? pairs.data() : static_cast<const int2*>(workspace), n, in_args, pool,
+                                         n_planes, num_pages, page_bytes, st), "spec_op_kv_copy_pages");
 } catch (const std::exception&) {
   return refuse(SPEC_E_UNSUPPORTED, "spec_op_kv_copy_pages: out of host memory");
 }
@@ -427,8 +435,8 @@ spec_status spec_op_rope_kv4(int32_t dtype, int32_t R, int32_t n_heads, int32_t 
     return refuse(SPEC_E_INVALID, "spec_op_rope_kv4: null pointer");
   if (misaligned(qkv, 16) || misaligned(q_out, 16) || misaligned(k_pages, 16) || misaligned(v_pages, 16))
     return refuse(SPEC_E_INVALID, "spec_op_rope_kv4: qkv, q_out and the pages must be 16-byte aligned");
-  return hip_status(launch_rope_kv4(dtype == SPEC_F32 ? 0 : 1, R, n_heads, n_kv_heads, head_dim, theta, qkv, pos, slot,
-                                    num_pages, q_out, k_pages, v_pages, static_cast<hipStream_t>(stream)));
+  return launched(launch_rope_kv4(dtype == SPEC_F32 ? 0 : 1, R, n_heads, n_kv_heads, head_dim, theta, qkv, pos, slot,
+                                    num_pages, q_out, k_pages, v_pages, static_cast<hipStream_t>(stream)), "spec_op_rope_kv4");
 }
 
 spec_status spec_op_kv4_read(int32_t dtype, int32_t R, int32_t n_kv_heads, int32_t head_dim, const int32_t* slot,
@@ -442,8 +450,8 @@ spec_status spec_op_kv4_read(int32_t dtype, int32_t R, int32_t n_kv_heads, int32
   if (!slot || !k_pages || !v_pages || !k_out || !v_out) return refuse(SPEC_E_INVALID, "spec_op_kv4_read: null pointer");
   if (misaligned(k_pages, 16) || misaligned(v_pages, 16) || misaligned(k_out, 16) || misaligned(v_out, 16))
     return refuse(SPEC_E_INVALID, "spec_op_kv4_read: the pages and outputs must be 16-byte aligned");
-  return hip_status(launch_kv4_read(dtype == SPEC_F32 ? 0 : 1, R, n_kv_heads, head_dim, slot, num_pages, k_pages,
-                                    v_pages, k_out, v_out, static_cast<hipStream_t>(stream)));
+  return launched(launch_kv4_read(dtype == SPEC_F32 ? 0 : 1, R, n_kv_heads, head_dim, slot, num_pages, k_pages,
+                                    v_pages, k_out, v_out, static_cast<hipStream_t>(stream)), "spec_op_kv4_read");
 }
 
 namespace {
@@ -585,10 +593,10 @@ spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const int32_t* 
   if (c.plan.prefill) {
     const hipError_t e = launch_kv4_expand(static_cast<int>(src.size()), reinterpret_cast<const int32_t*>(ws + osr),
                                            n_kv_heads, head_dim, k_pages, v_pages, ws + c.o_k, ws + c.o_v, st);
-    if (e != hipSuccess) return hip_status(e);
+    if (e != hipSuccess) return launched(e, "spec_op_attention_kv4");
     a.kpool = ws + c.o_k;
     a.vpool = ws + c.o_v;
-    return hip_status(launch_attention_prefill_bf16(a, items, n_items, c.plan.few_keys, st, true));
+    return launched(launch_attention_prefill_bf16(a, items, n_items, c.plan.few_keys, st, true), "spec_op_attention_kv4");
   }
   Kv4Tables t;
   t.tables = in_args ? mb.data() : ws;
@@ -596,8 +604,8 @@ spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const int32_t* 
   t.o_pt = opt;
   t.o_it = oit;
   t.o_gr = ogr;
-  return hip_status(launch_attention_kv4(a, t, n_items, static_cast<int>(c.plan.groups.size()), max_parts, c.plan.nt,
-                                         c.plan.w, st));
+  return launched(launch_attention_kv4(a, t, n_items, static_cast<int>(c.plan.groups.size()), max_parts, c.plan.nt,
+                                         c.plan.w, st), "spec_op_attention_kv4");
 } catch (const std::exception&) {
   return refuse(SPEC_E_UNSUPPORTED, "spec_op_attention_kv4: out of host memory");
 }

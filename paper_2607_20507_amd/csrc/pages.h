@@ -61,7 +61,8 @@ class PagePool {
     holders_[p] = 1;
     return p;
   }
-  // Hold the first n pages of `from` in `to` (empty) too.
+  // Hold the first n pages of `from` in `to` (empty) too (no allocation if `to` has
+  // room for them).
   void share(const std::vector<int32_t>& from, int n, std::vector<int32_t>& to) {
     to.assign(from.begin(), from.begin() + n);
     for (int32_t p : to) ++holders_[p];
@@ -89,9 +90,9 @@ class PagePool {
       while (holders_[to] != 0) ++to;
       moves.emplace_back(from, to++);
     }
-    for (const auto& m : moves) std::swap(holders_[m.first], holders_[m.second]);
     decltype(free_) left;
     for (int p = live; p < num_pages_; ++p) left.push(p);
+    for (const auto& m : moves) std::swap(holders_[m.first], holders_[m.second]);
     free_.swap(left);
     return moves;
   }

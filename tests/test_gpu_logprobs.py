@@ -158,6 +158,18 @@ def test_strided_and_unaligned_rows(off, pad):
     assert torch.equal(buf, before)
 
 
+def test_rows_beyond_32_bit_offsets():
+    dev = device()
+    V, ld, R = 5000, (1 << 30) + 4, 3  # the last row starts 8.6 GB into the buffer
+    buf = torch.empty(ld * (R - 1) + V, device=dev)
+    view = buf.as_strided((R, V), (ld, 1))
+    rng = np.random.default_rng(4)
+    z = (rng.standard_normal((R, V)) * 3).astype(np.float32)
+    view.copy_(torch.from_numpy(z))
+    tokens = rng.integers(0, V, R).astype(np.int32)
+    compare(call(view, None, torch.from_numpy(tokens).to(dev), 6, dev), reference(z, np.ones(R), tokens, 6), "far rows")
+
+
 def test_rows_do_not_depend_on_the_batch_of_equal_size():
     dev = device()
     g = torch.Generator(device=dev).manual_seed(1)
