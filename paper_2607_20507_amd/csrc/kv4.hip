@@ -474,6 +474,9 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
       const uint32_t* sp = reinterpret_cast<const uint32_t*>(blk + CB) + j * (DS / 2);
 #pragma unroll
       for (int i = 0; i < DS / 2; ++i) w.ks[i] = sp[i];
+      // (loads stay where they are issued: the compiler had moved the scales' to
+      // their use, a memory latency in every chunk)
+      asm volatile("" ::: "memory");
     };
     auto load_v = [&](Raw& w, int c0) {
       const uint8_t* blk = vp + (page(min(c0 + 8 * g, it.t1 - 1)) * a.Hkv + gkv) * BB;
@@ -485,6 +488,7 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
         const uint4 s = *(reinterpret_cast<const uint4*>(blk + CB) + th * (DS / 2) + i);
         w.vs[4 * i] = s.x; w.vs[4 * i + 1] = s.y; w.vs[4 * i + 2] = s.z; w.vs[4 * i + 3] = s.w;
       }
+      asm volatile("" ::: "memory");
     };
     // the chunk of keys c0 .. held in w, which then takes the wave's chunk of keys cn ..
     auto chunk = [&](Raw& w, int c0, int cn) {
