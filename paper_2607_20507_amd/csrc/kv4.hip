@@ -89,13 +89,23 @@ __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0
 // the 3 neighbouring lanes.  Angles, sines and the keys' rotation are in fp64,
 // so that a key's code depends on its exact value and not on the order of the
 // roundings before it; q is rotated in fp32.
+//
+// HBM bound: 8192 rows of 32 / 8 heads of 128 (202 MB of fp32 in, 76 MB out) take
+// 53 us, 5.2 TB/s.  Workgroups go to the 8 XCDs in turn, and a page's cache lines
+// hold parts of all of its tokens, so rows in their order leave every XCD's cache
+// with pieces of lines: 114 MB written.  Here kXcdRows consecutive rows share an
+// XCD (16, 32 or 64: 74.1 -> 68.6 us with the read-back of 8192 rows after it);
+// the rows behind the last whole round keep their order.
+constexpr int kXcdRows = 32;
 template <typename T>
 __global__ __launch_bounds__(256) void rope_kv4_kernel(int Hq, int Hkv, int hd, float theta,
                                                        const float* __restrict__ qkv, const int32_t* __restrict__ pos,
                                                        const int32_t* __restrict__ slot, int num_pages,
                                                        T* __restrict__ q, uint8_t* __restrict__ kpool,
                                                        uint8_t* __restrict__ vpool) {
-  const int r = blockIdx.x;
+  int r = blockIdx.x;
+  if (r < static_cast<int>(gridDim.x & ~(8u * kXcdRows - 1)))
+    r = (r & ~(8 * kXcdRows - 1)) + r % 8 * kXcdRows + r / 8 % kXcdRows;
   const int half = hd / 2, groups = half / 8;
   const float* x = qkv + static_cast<size_t>(r) * (Hq + 2 * Hkv) * hd;
   __shared__ double s_cos[64], s_sin[64];

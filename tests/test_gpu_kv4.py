@@ -84,6 +84,12 @@ def test_append_and_read(dtype, hq, hkv, hd, R, start):
         assert np.array_equal(got.double().cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("R, start", [(255, 0), (256, 7), (257, 0), (600, 1)])
+def test_append_and_read_of_rows_spread_over_the_chip(R, start):
+    """Whole rounds of 8 x 32 rows are taken in another order, the rows behind them are not."""
+    test_append_and_read(BF16, 4, 2, 64, R, start)
+
+
 def test_append_of_infinities_and_the_largest_values():
     from paper_2607_20507_amd import binding as B
     dev = device()
