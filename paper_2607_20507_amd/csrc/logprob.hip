@@ -6,7 +6,11 @@
 // both sums in one pass over the row with a running maximum (a new maximum m'
 // with d = (m - m') / T turns (S, U = sum t exp t) into (e^d S, e^d (U + d S))).
 // Every term of H is positive, so a peaked row loses nothing.  T = 0 is the
-// point mass on the first maximum.  Two launches:
+// point mass on the first maximum.
+//
+// HBM bound where there are many rows: 1792 x 128256 logits (919 MB) take 163 us a
+// call, the chunks' kernel 154 (6.0 TB/s).  8 rows of 32000 are latency, 11.7 us:
+// 7 in the chunks' kernel, 4.5 in the final one.  Two launches:
 //   1. chunk   grid rows x chunks: statistics of a chunk and its n_top largest
 //              logits, sorted
 //   2. final   one workgroup per row: merges both
@@ -17,8 +21,8 @@
 // value that at least n_top elements with lower ids reach and collects in LDS
 // what is above it: the n_top-th largest of the threads' maxima so far, found by
 // votes after steps 1, 2, 4, 8, 12, .. (20 of 128256 normal logits collect about
-// 130 keys; with the first step's value alone 630, and a pass over 1792 rows took
-// 184 us against 16x).  Where many keys pile up all the same they are thinned to
+// 130 keys; with the first step's value alone 630, and a call of 1792 rows took
+// 184 us, not 164).  Where many keys pile up all the same they are thinned to
 // those above the n_top-th largest of 256 disjoint subsets' maxima, which at most
 // n_top subsets are.  A chunk whose logits ascend can collect more than the buffer
 // holds: it is then read once more in steps that cannot.  Masked logits (-inf) are
@@ -378,35 +382,42 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
       return;
     }
     __shared__ Collect s;
-    if (tid == 0) {
-      s.t = 0;
-      s.cnt = s.over = 0;
-    }
-    __syncthreads();
-    for (int e0 = 0; e0 < n_chunks * n_top; e0 += kSafeStep) {
-      if (e0 > 0) load(e0);
-      uint64_t mx = s.t;
+    const int n_keys = n_chunks * n_top;
+    uint64_t mine = own[0];
+    int cnt = n_keys;
+    // Up to a key per thread is ranked as it is (8 rows of 11 chunks of 5 keys 12.5
+    // -> 11.7 us a call, 1792 of 2 chunks of 20 1.3 us less), more keys are thinned first.
+    if (n_keys > kThreads) {
+      if (tid == 0) {
+        s.t = 0;
+        s.cnt = s.over = 0;
+      }
+      __syncthreads();
+      for (int e0 = 0; e0 < n_keys; e0 += kSafeStep) {
+        if (e0 > 0) load(e0);
+        uint64_t mx = s.t;
 #pragma unroll
-      for (int i = 0; i < kOwn; ++i) mx = own[i] > mx ? own[i] : mx;
-      // a value that n_top keys reach, as in the chunks (keys below it are not needed)
-      const float w = reached_by(mx ? value_of(mx) : -INFINITY, (n_top + kWaves - 1) / kWaves);
-      if (lane == 0) s.reach[tid / kWave] = w;
-      __syncthreads();
-      const uint64_t t = static_cast<uint64_t>(
-          ordered(fminf(fminf(s.reach[0], s.reach[1]), fminf(s.reach[2], s.reach[3])))) << 32;
+        for (int i = 0; i < kOwn; ++i) mx = own[i] > mx ? own[i] : mx;
+        // a value that n_top keys reach, as in the chunks (keys below it are not needed)
+        const float w = reached_by(mx ? value_of(mx) : -INFINITY, (n_top + kWaves - 1) / kWaves);
+        if (lane == 0) s.reach[tid / kWave] = w;
+        __syncthreads();
+        const uint64_t t = static_cast<uint64_t>(
+            ordered(fminf(fminf(s.reach[0], s.reach[1]), fminf(s.reach[2], s.reach[3])))) << 32;
 #pragma unroll
-      for (int i = 0; i < kOwn; ++i)
-        if (own[i] > t) collect(s, own[i]);
-      __syncthreads();
-      const bool many = s.cnt > kLimit;
-      __syncthreads();
-      if (many) thin(s, n_top);
+        for (int i = 0; i < kOwn; ++i)
+          if (own[i] > t) collect(s, own[i]);
+        __syncthreads();
+        const bool many = s.cnt > kLimit;
+        __syncthreads();
+        if (many) thin(s, n_top);
+      }
+      thin(s, n_top);
+      cnt = s.cnt;
+      mine = tid < cnt ? s.buf[tid] : 0;
     }
-    thin(s, n_top);
-    const int cnt = s.cnt;
-    const uint64_t mine = tid < cnt ? s.buf[tid] : 0;
     s.keys[tid] = mine;
-    __syncthreads();
+    const int held = __syncthreads_count(mine != 0);
     if (mine != 0) {
       const int k = rank_of(s, mine, (cnt + 1) & ~1);
       if (k < n_top) {
@@ -416,7 +427,7 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
     }
     // fewer than n_top logits are not masked: the first masked ids follow (n_top <= V)
     if (tid < kWave)
-      for (int i0 = 0, found = cnt; found < n_top && i0 < V; i0 += kWave) {
+      for (int i0 = 0, found = held; found < n_top && i0 < V; i0 += kWave) {
         const bool masked = i0 + lane < V && z[i0 + lane] == -INFINITY;
         const uint64_t b = __ballot(masked);
         const int k = found + __popcll(b & ((1ull << lane) - 1));
