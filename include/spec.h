@@ -449,7 +449,8 @@ SPEC_API spec_status spec_sample_draft(int32_t n, const float* logits, int32_t V
  * pass, or expands candidates with (the target's logits of a verify are at
  * spec_last_logits).  Row r is the V floats at logits + r * row_stride (device
  * fp32, row_stride >= V) under softmax(z / T), T = temperature[r] (device fp32
- * [rows]; NULL: 1).  T = 0 is the point mass on the first maximum.
+ * [rows]; NULL: 1).  T = 0 is the point mass on the first maximum, T = inf the
+ * uniform distribution over the tokens that are not masked (-inf).
  *   logprobs[r]  log p(tokens[r]) (natural logarithm; tokens device int32
  *                [rows]; -inf for an id outside the vocabulary); NULL: not
  *                wanted, tokens may be NULL then
@@ -459,8 +460,8 @@ SPEC_API spec_status spec_sample_draft(int32_t n, const float* logits, int32_t V
  *                id, masked tokens (-inf) last; may be NULL for n_top = 0
  * A row that defines no distribution (every logit -inf; a logit +inf or NaN; a
  * temperature negative or NaN) gives NaN and ids -1.  Outputs are device
- * buffers that overlap no input.  Sums and statistics are fp32; results do not
- * depend on the other rows of a call.  workspace: device, 16-byte aligned, >=
+ * buffers that overlap no input.  Sums and statistics are fp32; a row's results
+ * depend on its own logits and on the number of rows (the order of its sums).  workspace: device, 16-byte aligned, >=
  * spec_token_logprobs_workspace_bytes, not shared by calls that overlap in time.
  * Nothing is read from the host, so the call can be captured into a graph and
  * replayed on new contents.  Rows that are 16-byte aligned (row_stride % 4 ==

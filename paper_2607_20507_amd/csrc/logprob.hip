@@ -362,6 +362,7 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
   auto log_p = [&](float v, int i) {
     if (!ok) return __builtin_nanf("");
     if (T == 0.f) return i == st.idx ? 0.f : -INFINITY;
+    if (v == -INFINITY) return v;  // masked at T = inf too, where v / T is no number
     return (v - st.m) / T - log_s;
   };
   if (tid == 0) {

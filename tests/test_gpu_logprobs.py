@@ -129,6 +129,21 @@ def test_temperatures():
     assert np.array_equal(ids[fine], np.argsort(-z, axis=1, kind="stable")[fine, :3])
 
 
+def test_masked_tokens_at_an_infinite_temperature():
+    dev = device()
+    z = np.full((2, 3000), -np.inf, np.float32)
+    z[0, [5, 700, 2999]] = [1.0, -4.0, 2.0]
+    z[1, 8] = 3.0
+    temps = np.array([np.inf, np.inf], np.float32)
+    lp, h, ids, top = (x.cpu().numpy() for x in call(torch.from_numpy(z).to(dev), torch.from_numpy(temps).to(dev),
+                                                     torch.tensor([6, 8], dtype=torch.int32, device=dev), 4, dev))
+    assert np.isneginf(lp[0]) and lp[1] == 0
+    assert abs(h[0] - math.log(3)) < H_TOL and h[1] == 0
+    assert ids.tolist() == [[2999, 5, 700, 0], [8, 0, 1, 2]]
+    assert np.all(np.abs(top[0, :3] + math.log(3)) < LP_ABS) and np.isneginf(top[0, 3])
+    assert top[1, 0] == 0 and np.isneginf(top[1, 1:]).all()
+
+
 def test_optional_outputs_and_defaults():
     dev = device()
     rng = np.random.default_rng(6)
