@@ -401,7 +401,8 @@ constexpr float kPrefillRescaleLog2 = 8.f;
 constexpr int kPrefillStagedPages = 1024;  // page ids kept in LDS (16384 keys)
 
 // FAR: a score's difference to the maximum is taken before it is scaled, one
-// instruction more per score.  The FMA of the other form rounds the scaled
+// instruction more per score (8192 rows over a 4-bit cache, 32 / 8 heads of 128:
+// 553 us, 531 without).  The FMA of the other form rounds the scaled
 // maximum, which from scores of 2^24 on is off by more than the exponents it is
 // to leave (bf16 caches of trained models stay far below; a 4-bit cache takes
 // any block's scale).

@@ -450,6 +450,8 @@ LogprobPlan logprob_plan(int rows, int V, int n_top) {
   p.rows = rows;
   p.V = V;
   p.n_top = n_top;
+  // about kTargetBlocks workgroups, at least half a step each (with one a row, 8
+  // rows of 128256 take 67 us, not 14, and 1792 rows 180, not 164)
   int want = std::max(1, (kTargetBlocks + rows - 1) / std::max(1, rows));
   want = std::min(want, std::max(1, V / (kStep / 2)));
   // at most kMaxChunks chunks, each a multiple of 1024 elements (16-byte loads)
