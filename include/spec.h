@@ -461,7 +461,8 @@ SPEC_API spec_status spec_sample_draft(int32_t n, const float* logits, int32_t V
  * A row that defines no distribution (every logit -inf; a logit +inf or NaN; a
  * temperature negative or NaN) gives NaN and ids -1.  Outputs are device
  * buffers that overlap no input.  Sums and statistics are fp32; a row's results
- * depend on its own logits and on the number of rows (the order of its sums).  workspace: device, 16-byte aligned, >=
+ * depend on its own logits and on the number of rows (the order of its sums).
+ * V <= 2^30 (SPEC_E_UNSUPPORTED beyond).  workspace: device, 16-byte aligned, >=
  * spec_token_logprobs_workspace_bytes, not shared by calls that overlap in time.
  * Nothing is read from the host, so the call can be captured into a graph and
  * replayed on new contents.  Rows that are 16-byte aligned (row_stride % 4 ==

@@ -112,15 +112,17 @@ SPEC_API spec_status spec_op_kv4_read(int32_t dtype, int32_t R, int32_t n_kv_hea
                                       const int32_t* slot, int32_t num_pages, const void* k_pages,
                                       const void* v_pages, void* k_out, void* v_out, void* stream);
 
-/* spec_op_attention over a 4-bit cache.  rows[i] may be 0 (a sequence without
- * rows in this call).  num_pages: pages of the pool; a page id outside it is
- * refused (SPEC_E_INVALID).  q, out: dtype, 16-byte aligned.  n_heads /
- * n_kv_heads <= 64 (bf16) or 32 (fp32), else SPEC_E_UNSUPPORTED.  fp32 keeps q
- * and the probabilities to 24 bits.  workspace: device, 256-byte aligned, >=
- * spec_op_attention_kv4_workspace_bytes of the same rows and positions (0 for
- * arguments the call refuses), not shared by calls that overlap in time.  A
- * captured call takes tables of at most 3 KB (SPEC_E_UNSUPPORTED beyond).
- * Asynchronous; host arrays are consumed before return. */
+/* spec_op_attention over a 4-bit cache, of at most 2^30 positions a sequence and
+ * 65535 heads (SPEC_E_INVALID beyond; 65535 in the other 4-bit calls too).
+ * rows[i] may be 0 (a sequence without rows in this call).  num_pages: pages of
+ * the pool; a page id outside it is refused (SPEC_E_INVALID).  q, out: dtype,
+ * 16-byte aligned.  n_heads / n_kv_heads <= 64 (bf16) or 32 (fp32), else
+ * SPEC_E_UNSUPPORTED.  fp32 keeps q and the probabilities to 24 bits.
+ * workspace: device, 256-byte aligned, >= spec_op_attention_kv4_workspace_bytes
+ * of the same rows and positions (0 for arguments the call refuses), not shared
+ * by calls that overlap in time.  A captured call takes tables of at most 3 KB
+ * (SPEC_E_UNSUPPORTED beyond). Asynchronous; host arrays are consumed before
+ * return. */
 SPEC_API size_t spec_op_attention_kv4_workspace_bytes(int32_t dtype, int32_t n_seqs, const int32_t* rows,
                                                       const int32_t* pos0, int32_t max_pages, int32_t n_heads,
                                                       int32_t n_kv_heads, int32_t head_dim);

@@ -1548,7 +1548,7 @@ spec_status spec_decode(spec_ctx* ctx, int32_t n, const int64_t* seq_ids, const 
   return SPEC_OK;
 }
 
-spec_status spec_kv_rollback(spec_ctx* ctx, int64_t seq_id, int32_t new_len, void* stream) {
+spec_status spec_kv_rollback(spec_ctx* ctx, int64_t seq_id, int32_t new_len, void* stream) try {
   CHECK_READY();
   hipStream_t st = static_cast<hipStream_t>(stream);
   auto it = ctx->seqs.find(seq_id);
@@ -1607,9 +1607,12 @@ spec_status spec_kv_rollback(spec_ctx* ctx, int64_t seq_id, int32_t new_len, voi
       if (r != SPEC_OK) return r;
     }
   return launch_clears(ctx, side[0].clear, side[1].clear, st);
+} catch (const std::exception&) {  // perhaps between two changes
+  ctx->broken = true;
+  FAIL(SPEC_E_HIP, "out of host memory");
 }
 
-spec_status spec_seq_fork(spec_ctx* ctx, int64_t seq_id, int32_t n, const int64_t* new_ids, void* stream) {
+spec_status spec_seq_fork(spec_ctx* ctx, int64_t seq_id, int32_t n, const int64_t* new_ids, void* stream) try {
   CHECK_READY();
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (n < 0 || (n > 0 && !new_ids)) FAIL(SPEC_E_INVALID, "bad arguments");
@@ -1665,6 +1668,8 @@ spec_status spec_seq_fork(spec_ctx* ctx, int64_t seq_id, int32_t n, const int64_
     if (r != SPEC_OK) return r;
   }
   return SPEC_OK;
+} catch (const std::exception&) {  // before any change
+  FAIL(SPEC_E_UNSUPPORTED, "out of host memory");
 }
 
 spec_status spec_kv_compact(spec_ctx* ctx, int32_t* pages_target, int32_t* pages_draft, void* stream) {

@@ -26,6 +26,8 @@ namespace {
 
 constexpr int kOpMaxParts = 4096;
 constexpr int kMaxSlotPages = INT32_MAX / kPage;  // a slot (page * 16 + offset) is an int32
+constexpr int32_t kMaxExtent = 1 << 30;           // of a row or sequence: with a tile added it is still an int32
+constexpr int32_t kMaxHeads = 65535;              // a grid dimension; an int32 also times the head dim
 
 std::mutex g_mu;
 Stager& stager() {
@@ -351,7 +353,7 @@ spec_status spec_op_attention(int32_t dtype, int32_t n_seqs, const int32_t* rows
 // token log probabilities
 
 size_t spec_token_logprobs_workspace_bytes(int32_t rows, int32_t V, int32_t n_top) {
-  if (rows <= 0 || V <= 0 || n_top < 0 || n_top > kLogprobMaxTop) return 0;
+  if (rows <= 0 || V <= 0 || V > kMaxExtent || n_top < 0 || n_top > kLogprobMaxTop) return 0;
   return logprob_ws_bytes(logprob_plan(rows, V, n_top));
 }
 
@@ -360,6 +362,7 @@ spec_status spec_token_logprobs(int32_t rows, int32_t V, const float* logits, in
                                 float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace,
                                 size_t workspace_bytes, void* stream) {
   if (rows < 0 || V <= 0 || row_stride < V) return refuse(SPEC_E_INVALID, "spec_token_logprobs: need rows >= 0, V > 0, row_stride >= V");
+  if (V > kMaxExtent) return refuse(SPEC_E_UNSUPPORTED, "spec_token_logprobs: V must be at most 2^30");
   if (n_top < 0 || n_top > kLogprobMaxTop || n_top > V)
     return refuse(SPEC_E_INVALID, "spec_token_logprobs: need 0 <= n_top <= min(64, V)");
   if (rows == 0) return SPEC_OK;
@@ -426,8 +429,8 @@ size_t spec_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim) {
 spec_status spec_op_rope_kv4(int32_t dtype, int32_t R, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                              float theta, const float* qkv, const int32_t* pos, const int32_t* slot,
                              int32_t num_pages, void* q_out, void* k_pages, void* v_pages, void* stream) {
-  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || R < 0 || n_heads <= 0 || n_kv_heads <= 0 || !(theta > 0.f) ||
-      num_pages < 0 || num_pages > kMaxSlotPages)
+  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || R < 0 || n_heads <= 0 || n_heads > kMaxHeads || n_kv_heads <= 0 ||
+      n_kv_heads > kMaxHeads || !(theta > 0.f) || num_pages < 0 || num_pages > kMaxSlotPages)
     return refuse(SPEC_E_INVALID, "spec_op_rope_kv4: bad dtype or size");
   if (head_dim != 64 && head_dim != 128) return refuse(SPEC_E_UNSUPPORTED, "spec_op_rope_kv4: head_dim must be 64 or 128");
   if (R == 0) return SPEC_OK;
@@ -442,8 +445,8 @@ spec_status spec_op_rope_kv4(int32_t dtype, int32_t R, int32_t n_heads, int32_t 
 spec_status spec_op_kv4_read(int32_t dtype, int32_t R, int32_t n_kv_heads, int32_t head_dim, const int32_t* slot,
                              int32_t num_pages, const void* k_pages, const void* v_pages, void* k_out, void* v_out,
                              void* stream) {
-  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || R < 0 || n_kv_heads <= 0 || num_pages < 0 ||
-      num_pages > kMaxSlotPages)
+  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || R < 0 || n_kv_heads <= 0 || n_kv_heads > kMaxHeads ||
+      num_pages < 0 || num_pages > kMaxSlotPages)
     return refuse(SPEC_E_INVALID, "spec_op_kv4_read: bad dtype or size");
   if (head_dim != 64 && head_dim != 128) return refuse(SPEC_E_UNSUPPORTED, "spec_op_kv4_read: head_dim must be 64 or 128");
   if (R == 0 || num_pages == 0) return SPEC_OK;
@@ -474,8 +477,8 @@ Kv4Call kv4_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32
     c.why = why;
     return c;
   };
-  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || n_seqs < 0 || max_pages <= 0 || n_heads <= 0 || n_kv_heads <= 0 ||
-      n_heads % n_kv_heads)
+  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || n_seqs < 0 || max_pages <= 0 || n_heads <= 0 || n_heads > kMaxHeads ||
+      n_kv_heads <= 0 || n_heads % n_kv_heads)
     return fail(SPEC_E_INVALID, "spec_op_attention_kv4: bad dtype or size");
   const int G = n_heads / n_kv_heads, dt = dtype == SPEC_F32 ? 0 : 1;
   if (head_dim != 64 && head_dim != 128) return fail(SPEC_E_UNSUPPORTED, "spec_op_attention_kv4: head_dim must be 64 or 128");
@@ -486,8 +489,8 @@ Kv4Call kv4_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32
   int64_t R = 0;
   for (int i = 0; i < n_seqs; ++i) {
     const int64_t len = static_cast<int64_t>(pos0[i]) + rows[i];
-    if (rows[i] < 0 || pos0[i] < 0 || len > INT32_MAX || (len + 15) / 16 > max_pages)
-      return fail(SPEC_E_INVALID, "spec_op_attention_kv4: rows beyond the page table, or a negative length");
+    if (rows[i] < 0 || pos0[i] < 0 || len > kMaxExtent || (len + 15) / 16 > max_pages)
+      return fail(SPEC_E_INVALID, "spec_op_attention_kv4: rows beyond the page table or 2^30 positions, or a negative length");
     if (R + rows[i] > INT32_MAX) return fail(SPEC_E_INVALID, "spec_op_attention_kv4: too many rows");
     if (rows[i] > 0) segs.push_back(AttnSegment{i, static_cast<int32_t>(R), rows[i], pos0[i]});
     if (rows[i] > 0) c.pages += (len + 15) / 16;

@@ -108,6 +108,21 @@ def test_attention_kv4(change, status):
         assert "spec_op_attention_kv4" in last()
 
 
+def test_sizes_that_pass_32_bits():
+    big, L = (1 << 30) + 1, B.lib()
+    r, p = i32(1), i32(big - 1)
+    assert L.spec_token_logprobs(1, big, P, big, P, P, 4, P, P, P, P, P, 1 << 40, None) == UNSUPPORTED and "2^30" in last()
+    assert L.spec_token_logprobs_workspace_bytes(1, big, 4) == 0 and L.spec_token_logprobs_workspace_bytes(1, big - 1, 4) > 0
+    assert L.spec_op_attention_kv4_workspace_bytes(1, 1, r.ctypes.data, p.ctypes.data, big, 8, 2, 128) == 0
+    assert "2^30" in last()
+    p = i32(big - 2)  # the longest
+    assert L.spec_op_attention_kv4_workspace_bytes(1, 1, r.ctypes.data, p.ctypes.data, big, 8, 2, 128) > 4 * (big // 16)
+    assert L.spec_op_rope_kv4(1, 4, 65536, 2, 128, 1e4, P, P, P, 8, P, P, P, None) == INVALID
+    assert L.spec_op_rope_kv4(1, 4, 2, 65536, 128, 1e4, P, P, P, 8, P, P, P, None) == INVALID
+    assert L.spec_op_kv4_read(1, 4, 65536, 128, P, 8, P, P, P, P, None) == INVALID
+    assert L.spec_op_attention_kv4_workspace_bytes(1, 1, r.ctypes.data, r.ctypes.data, 1, 65536, 65536, 128) == 0
+
+
 def test_attention_kv4_workspace():
     f = B.lib().spec_op_attention_kv4_workspace_bytes
     r, p = i32(6), i32(2047)
