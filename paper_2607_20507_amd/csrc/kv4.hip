@@ -279,9 +279,10 @@ __global__ __launch_bounds__(256) void kv4_expand_kernel(const int32_t* __restri
 // of fraction), whose products with the cache's values are exact in fp32.
 //
 // Bound by HBM where a tile has up to 16 query vectors: 131000 keys of 8 heads of
-// 128 (142 MB) take 26 us, 5.5 TB/s.  With 32 by instruction issue: of the cycles
-// of 64 sequences of 4 .. 8 rows and 512 .. 4096 keys (127 MB, 31 us) vector
-// instructions take 68% and matrix ones 27%; a 32-key chunk has about 235 of the
+// 128 (142 MB) take 26 us, 5.5 TB/s.  With 32 by instruction issue and the
+// longest items' chains: at 64 sequences of 4 .. 8 rows and 512 .. 4096 keys (127
+// MB, 31 us) a CU holds waves in 55 of 86 thousand cycles, and of those vector
+// instructions take 68%, matrix ones 27%; a 32-key chunk has about 235 of the
 // former, 64 of them conversions, 32 that bring tokens beside each other, 32 that
 // shift scales and 32 exponents and their arguments.  Small calls are latency: one
 // sequence of 2000 keys 12.9 us.

@@ -162,7 +162,8 @@ AttnPlan plan_kv4(const std::vector<AttnSegment>& segs, int G, int Hkv, int max_
     // tiles (16 rows of 8 sequences of 2000 keys 28.4 us, with 512 40.6).  Where a
     // batch has nearly as many before any split, only its longest sequences are
     // split (64 of 512 .. 4096 keys: 300 41.4 us, 256 43.8, 512 45.2; but 131000
-    // keys of one sequence 44.4 us with 300, 35.2 with 512).
+    // keys of one sequence 44.4 us with 300, 35.2 with 512; in even parts instead of
+    // full ones and a remainder the 64 take 2 us more).
     const int target = p.nt >= 4 ? 256 : wgs < 256 ? 512 : 300;
     p.w = 4;
     split = (total_keys * Hkv + target - 1) / target;
