@@ -1556,39 +1556,20 @@ spec_status spec_kv_rollback(spec_ctx* ctx, int64_t seq_id, int32_t new_len, voi
   Seq& s = it->second;
   if (new_len < 0 || new_len > s.len_t) FAIL(SPEC_E_INVALID, "new_len outside 0..target length");
   const int new_d = std::min(s.len_d, new_len);
-  // The last page kept is written next: held by another sequence too, it is
-  // replaced by a copy.  Slots of other shared pages are not cleared.
   struct Side {
     PagePool& pool;
     std::vector<int32_t>& table;
     int keep, end;
-    bool copy = false;
     std::vector<int32_t> clear;
     std::vector<std::pair<int32_t, int32_t>> moves;
   } side[2] = {{ctx->m[0].pool, s.pages_t, new_len, s.written_t}, {ctx->m[1].pool, s.pages_d, new_d, s.len_d}};
-  for (Side& x : side) {
-    x.copy = x.keep % 16 != 0 && x.pool.shared(x.table[x.keep / 16]);
-    if (x.copy && x.pool.free_pages() + x.pool.freed_by(x.table, x.keep) < 1)
+  for (const Side& x : side)
+    if (!x.pool.can_cut(x.table, x.keep))
       FAIL(SPEC_E_NOPAGES, "KV page pool exhausted: the rollback ends in a page that another sequence holds");
-  }
   for (Side& x : side) {
-    const int last = x.keep / 16;
-    std::vector<int32_t> own;  // slots in pages that go or stay with this sequence alone
-    for (int p = x.keep; p < x.end; ++p)
-      if (p / 16 != last && !x.pool.shared(x.table[p / 16])) own.push_back(x.pool.slot(x.table, p));
-    x.pool.truncate(x.table, x.keep);
-    if (x.copy) {
-      const int32_t from = x.table[last], to = x.pool.take();
-      x.moves.emplace_back(from, to);
-      x.table[last] = to;
-      x.pool.drop(from);
-      // (a page that this call freed may come back as the copy: not to be cleared)
-      own.erase(std::remove_if(own.begin(), own.end(), [&](int32_t sl) { return sl / 16 == to; }), own.end());
-    }
-    // (a page that ends at the new length has gone with the others)
-    if (x.keep % 16 != 0)
-      for (int p = x.keep; p < std::min(x.end, 16 * (last + 1)); ++p) x.clear.push_back(x.pool.slot(x.table, p));
-    x.clear.insert(x.clear.end(), own.begin(), own.end());
+    PagePool::Cut c = x.pool.cut(x.table, x.keep, x.end);
+    x.clear = std::move(c.clear);
+    if (c.to >= 0) x.moves.emplace_back(c.from, c.to);
   }
   s.hist.resize(new_len + 1);
   s.len_t = s.written_t = new_len;

@@ -8,6 +8,7 @@
 // (share); whoever writes to one must hold it alone.
 #pragma once
 
+#include <algorithm>
 #include <cstdint>
 #include <functional>
 #include <queue>
@@ -77,6 +78,34 @@ class PagePool {
     int n = 0;
     for (size_t i = pages_for(length); i < table.size(); ++i) n += holders_[table[i]] == 1;
     return n;
+  }
+  // A table cut to `keep` of its `end` positions.  The page that keep ends in is
+  // written next: held by another table too, it is replaced by a copy.
+  struct Cut {
+    int32_t from = -1, to = -1;  // the page to copy and its copy (-1: none)
+    std::vector<int32_t> clear;  // slots from keep on that no other table holds, those of the copy among them
+  };
+  bool can_cut(const std::vector<int32_t>& table, int64_t keep) const {
+    return keep % page_size_ == 0 || !shared(table[keep / page_size_]) || free_pages() + freed_by(table, keep) > 0;
+  }
+  Cut cut(std::vector<int32_t>& table, int64_t keep, int64_t end) {
+    Cut c;
+    const int64_t last = keep / page_size_;
+    const bool copied = keep % page_size_ != 0 && shared(table[last]);
+    for (int64_t p = keep; p < end; ++p)
+      if (!shared(table[p / page_size_])) c.clear.push_back(slot(table, p));
+    truncate(table, keep);
+    if (copied) {
+      c.from = table[last];
+      c.to = take();
+      table[last] = c.to;
+      drop(c.from);
+      // (a page that this cut freed may come back as the copy: not to be cleared as such)
+      c.clear.erase(std::remove_if(c.clear.begin(), c.clear.end(), [&](int32_t s) { return s / page_size_ == c.to; }),
+                    c.clear.end());
+      for (int64_t p = keep; p < std::min(end, page_size_ * (last + 1)); ++p) c.clear.push_back(slot(table, p));
+    }
+    return c;
   }
   // Renumber the held pages to 0 .. live - 1, moving as few as possible: the held
   // pages from `live` on, ascending, to the free ones below it, ascending.  Returns
