@@ -111,3 +111,24 @@ def attention(q, k, v, pos0):
         out[:, h], mag[:, h] = p @ vv, p @ np.abs(vv)
         big = max(big, float(np.where(hidden, 0, np.abs(q[:, h]) @ np.abs(kk).T).max()) / np.sqrt(hd))
     return out, mag, big
+
+
+def attention_rows(q, k, v, pos0):
+    """As attention(), of the keys that a row sees alone (what later keys hold does not enter), with the
+    largest sum |q k| / sqrt(hd) of each row and head [r, Hq, 1]."""
+    r, hq, hd = q.shape
+    G = hq // k.shape[1]
+    out, mag, big = np.empty(q.shape), np.empty(q.shape), np.empty((r, hq, 1))
+    with np.errstate(invalid="ignore", over="ignore"):
+        for g in range(k.shape[1]):
+            kt, vv = np.ascontiguousarray(k[:, g].T), np.ascontiguousarray(v[:, g])
+            ka, va = np.abs(kt), np.abs(vv)
+            for i in range(r):
+                n = pos0 + i + 1
+                rows = q[i, g * G:(g + 1) * G]
+                s = rows @ kt[:, :n] / np.sqrt(hd)
+                p = np.exp(s - s.max(1, keepdims=True))
+                p /= p.sum(1, keepdims=True)
+                out[i, g * G:(g + 1) * G], mag[i, g * G:(g + 1) * G] = p @ vv[:n], p @ va[:n]
+                big[i, g * G:(g + 1) * G, 0] = (np.abs(rows) @ ka[:, :n]).max(1) / np.sqrt(hd)
+    return out, mag, big
