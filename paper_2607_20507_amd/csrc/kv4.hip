@@ -308,10 +308,14 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&w)[N]) {
 }
 
 // Exponents are one FMA, p = 2^(raw scale - M), with M the rounded base-2 logit of
-// the maximum: exact as long as M is used for the sums too, but off by up to
-// M 2^-24 from the largest exponent, 0.  Above this M a wave takes the difference of
-// the raw scores first (one instruction more per score), which a 4-bit cache, whose
-// blocks have any scale, may need.
+// the maximum, and the wave's sums are relative to 2^M: a new maximum rescales them
+// by 2^(M - M'), not by the raw difference.  The largest exponent is off from 0 by
+// up to M 2^-24.  Above this M a wave takes the difference of the raw scores first
+// (one instruction more per score), which a 4-bit cache, whose blocks have any
+// scale, may need; its sums are then relative to the raw maximum.  Waves and parts
+// are joined by the differences of their raw maxima, which fp32 holds where it
+// does not hold those of the logits M; a wave that ends in the first form
+// brings its sums to the raw maximum first (to_raw).
 constexpr float kFarLog2 = 16777216.f;
 // A maximum is raised only by a score more than 2^8 times as probable: fewer
 // rescalings, and probabilities stay below 2^8.
@@ -339,8 +343,17 @@ __device__ __forceinline__ void store4(float* o, const f32x4& v) {
 }
 
 // The waves' states are merged through LDS, each wave taking some of the output
-// tiles, and the output or the partial is written.  m: base-2 logit that a lane's
+// tiles, and the output or the partial is written.  m: raw score that a lane's
 // sums are relative to (-inf: no key), l: the wave's sum (in every element).
+template <int HD>
+__device__ __forceinline__ float score_scale() { return kLog2e / sqrtf(static_cast<float>(HD)); }
+
+// Factor of sums relative to 2^-mneg (mneg = -(m scale), rounded) that makes them
+// relative to 2^(m scale).
+__device__ __forceinline__ float to_raw(float m, float scale, float mneg) {
+  return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(-fmaf(m, scale, mneg));
+}
+
 template <typename T, int HD, int NT, int W>
 __device__ __forceinline__ void finish(const AttnArgs& a, const AttnItem& it, int gkv, int M, int lane, int wave,
                                        const float (&m)[NT], const f32x4 (&l)[NT], const f32x4 (&acc)[HD / 16][NT]) {
@@ -369,7 +382,7 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const AttnItem& it, in
     float lt = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      e[w] = s_m[w][l16] == -INFINITY ? 0.f : exp2f(s_m[w][l16] - mm);
+      e[w] = s_m[w][l16] == -INFINITY ? 0.f : exp2f((s_m[w][l16] - mm) * score_scale<HD>());
       lt += e[w] * s_l[w][l16];
     }
     if (v < M)
@@ -454,7 +467,7 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
       }
     }
   }
-  const float scale = kLog2e / sqrtf(static_cast<float>(HD));
+  const float scale = score_scale<HD>();
   const int pos_lo = it.pos0;  // every row of the item sees the keys up to here
   int klim[NT];                // the last key a query vector sees (-1: none, a padding vector)
 #pragma unroll
@@ -568,17 +581,27 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
           float m = mx[nt];
           m = fmaxf(m, __shfl_xor(m, 16, kWave));
           m = fmaxf(m, __shfl_xor(m, 32, kWave));
-          m = m > mlim[nt] ? m : mrun[nt];
-          const float alpha = mrun[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mrun[nt] - m) * scale);
+          mx[nt] = m > mlim[nt] ? m : mrun[nt];
+          large |= fabsf(mx[nt] * scale) > kFarLog2 && mx[nt] > -INFINITY;
+        }
+        const bool was_far = far;
+        far |= __any(large) != 0;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float m = mx[nt], neg = m == -INFINITY ? 0.f : -m * scale;
+          float alpha = __builtin_amdgcn_exp2f(neg - mneg[nt]);
+          if (far) {
+            alpha = __builtin_amdgcn_exp2f((mrun[nt] - m) * scale);
+            if (!was_far) alpha *= to_raw(mrun[nt], scale, mneg[nt]);
+          }
+          if (mrun[nt] == -INFINITY) alpha = 0.f;
           mrun[nt] = m;
           mlim[nt] = m + kRescaleLog2 / scale;
-          mneg[nt] = m == -INFINITY ? 0.f : -m * scale;
-          large |= fabsf(mneg[nt]) > kFarLog2;
+          mneg[nt] = neg;
           lrun[nt] *= alpha;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= alpha;
         }
-        far |= __any(large) != 0;
       }
       uint4 pf[NT][NP];
 #pragma unroll
@@ -641,14 +664,20 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
     if (staged) walk(std::true_type{});
     else walk(std::false_type{});
   }
-  float m[NT];
+  if (!far) {
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) m[nt] = mrun[nt] == -INFINITY ? -INFINITY : -mneg[nt];
-  finish<T, HD, NT, W>(a, it, gkv, M, lane, wave, m, lrun, acc);
+    for (int nt = 0; nt < NT; ++nt) {
+      const float f = to_raw(mrun[nt], scale, mneg[nt]);
+      lrun[nt] *= f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= f;
+    }
+  }
+  finish<T, HD, NT, W>(a, it, gkv, M, lane, wave, mrun, lrun, acc);
 }
 
-// Merges the parts of split items: with M the largest maximum, out = sum 2^(m - M) o
-// over sum 2^(m - M) l.  A query vector's parts are shared by P threads for each 4
+// Merges the parts of split items: with M the largest maximum of raw scores, out =
+// sum 2^((m - M) scale) o over sum 2^((m - M) scale) l.  A query vector's parts are shared by P threads for each 4
 // dims, 8 / P vectors a workgroup of 256 (head dim 64: twice as many): a thread's
 // loads of up to 8 parts are in flight together.  A launch and two round trips to
 // memory: 4 us with 2 parts a vector (64 sequences) and with 64 (131000 keys).
@@ -663,6 +692,7 @@ __global__ __launch_bounds__(256) void combine_kv4_kernel(AttnArgs a, const Attn
   const size_t base = (static_cast<size_t>(gr.part0) * a.Hkv + gkv) * 64 + (in ? v : 0);
   const size_t stride = static_cast<size_t>(a.Hkv) * 64;
   const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+  const float scale = score_scale<HD>();
   float M = -INFINITY, den = 0.f;
   f32x4 num = {0.f, 0.f, 0.f, 0.f};
   for (int p0 = pg; p0 < gr.nparts; p0 += B * P) {
@@ -679,13 +709,13 @@ __global__ __launch_bounds__(256) void combine_kv4_kernel(AttnArgs a, const Attn
 #pragma unroll
     for (int i = 0; i < B; ++i) mx = fmaxf(mx, c[i].x);
     if (mx == -INFINITY) continue;
-    const float e0 = M == -INFINITY ? 0.f : exp2f(M - mx);
+    const float e0 = M == -INFINITY ? 0.f : exp2f((M - mx) * scale);
     num *= e0;
     den *= e0;
     M = mx;
 #pragma unroll
     for (int i = 0; i < B; ++i) {
-      const float e = c[i].x == -INFINITY ? 0.f : exp2f(c[i].x - mx);
+      const float e = c[i].x == -INFINITY ? 0.f : exp2f((c[i].x - mx) * scale);
       num += e * o[i];
       den += e * c[i].y;
     }
@@ -705,7 +735,7 @@ __global__ __launch_bounds__(256) void combine_kv4_kernel(AttnArgs a, const Attn
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const int t = threadIdx.x + i * TQ;
-      const float e = s_m[t] == -INFINITY ? 0.f : exp2f(s_m[t] - M);
+      const float e = s_m[t] == -INFINITY ? 0.f : exp2f((s_m[t] - M) * scale);
       num += e * s_num[t];
       den += e * s_den[t];
     }

@@ -172,6 +172,59 @@ def test_a_prompt_chunk_behind_many_keys():
 
 
 # ---------------------------------------------------------------------------
+# Scores of 2^17 to 2^25 in base 2, whose differences are a few units: sums of a few numbers that fp32 holds
+# exactly in any order, so that the scores have no error and only their differences count.
+
+def far_keys(rng, n, hkv, hd, unit):
+    """Dims 0 .. 2: 1; dim 32: a multiple of `unit`, small for most keys, larger for some of the later ones."""
+    k = np.zeros((n, hkv, hd))
+    k[..., :3] = 1
+    fine = rng.choice([0, 1, 2, 3], (n, hkv))
+    late = (np.arange(n)[:, None] > n // 3) & (rng.random((n, hkv)) < 0.02)
+    k[..., 32] = np.where(late, rng.choice([6, 8, 12], (n, hkv)), fine) * unit
+    return k
+
+
+def bf16_parts(x):
+    """x as a sum of three bf16 numbers."""
+    parts = []
+    for _ in range(3):
+        p = float(torch.tensor(x, dtype=torch.float64).to(torch.bfloat16))
+        parts.append(p)
+        x -= p
+    assert x == 0
+    return parts
+
+
+def border(hd):
+    """The score at which the exponent form changes (2^24 in base 2), less a few units of 8."""
+    return float(int(2.0 ** 24 / (1.4426950408889634 / hd ** 0.5)) // 8 * 8 - 24)
+
+
+@pytest.mark.parametrize("dtype, hq, hkv, hd", [(F32, 4, 4, 64), (F32, 8, 2, 128), (BF16, 8, 2, 128), (BF16, 16, 4, 64), (BF16, 64, 1, 64)])
+@pytest.mark.parametrize("base", [2.0 ** 20, -2.0 ** 20, 2.0 ** 24, 2.0 ** 26, -2.0 ** 26, "border", 2.0 ** 27, -2.0 ** 27])
+@pytest.mark.parametrize("rows, pos0", [(1, 39), (6, 700), (3, 3000), (64, 340), (100, 500)])
+def test_scores_far_from_zero(dtype, hq, hkv, hd, base, rows, pos0):
+    dev = device()
+    base = border(hd) if base == "border" else base
+    unit = 16.0 if abs(base) >= 2.0 ** 27 else 8.0
+    say("far scores", dtype, hq, hkv, hd, base, rows, pos0)
+    rng = np.random.default_rng([hq, hd, rows, pos0])
+    table, (kp, vp), ((k, v),) = pages(rng, [rows + pos0], hkv, hd, dev, lambda n: far_keys(rng, n, hkv, hd, unit),
+                                       lambda n: rng.standard_normal((n, hkv, hd)).astype(np.float32).astype(np.float64))
+    q = np.zeros((rows, hq, hd))
+    q[..., :3] = bf16_parts(base)
+    q[..., 32] = 1
+    got = attend(dtype, [rows], [pos0], table, len(kp), hq, hkv, hd, to(dev, q, TYPES[dtype]), to(dev, kp, torch.uint8),
+                 to(dev, vp, torch.uint8), dev).double().cpu().numpy().reshape(rows, hq, hd)
+    q[..., :3] = 0  # the same for every key: the softmax is that of the rest
+    want, mag, _ = ref.attention_rows(q, k, v, pos0)
+    # the scores are exact; their differences, at most 12 units, lose 3 roundings
+    tol = bound(dtype, hd, rows + pos0, want, mag, 12 * unit / hd ** 0.5 * 3 / (hd + 5))
+    assert fits(got, want, tol), float(np.max(np.abs(got - want) / tol))
+
+
+# ---------------------------------------------------------------------------
 # captured calls
 
 @pytest.mark.parametrize("rows, pos0, taken", [([6], [2047], True), ([1], [100], True), ([1], [2600], True), ([3, 2, 4], [50, 900, 20], True),
