@@ -703,12 +703,16 @@ __global__ __launch_bounds__(256) void combine_kv4_kernel(AttnArgs a, const Attn
       const size_t pm = base + min(p0 + i * P, gr.nparts - 1) * stride;
       c[i] = ml[pm];
       o[i] = *reinterpret_cast<const f32x4*>(a.part_o + pm * HD + d0);
-      if (p0 + i * P >= gr.nparts) c[i].x = -INFINITY;
+      if (p0 + i * P >= gr.nparts) c[i] = make_float2(-INFINITY, 0.f);
     }
     float mx = M;
 #pragma unroll
     for (int i = 0; i < B; ++i) mx = fmaxf(mx, c[i].x);
-    if (mx == -INFINITY) continue;
+    if (mx == -INFINITY) {  // sums of 0, or NaN where every score of a part was one (it raises no maximum)
+#pragma unroll
+      for (int i = 0; i < B; ++i) den += c[i].y;
+      continue;
+    }
     const float e0 = M == -INFINITY ? 0.f : exp2f((M - mx) * scale);
     num *= e0;
     den *= e0;

@@ -225,6 +225,26 @@ def test_scores_far_from_zero(dtype, hq, hkv, hd, base, rows, pos0):
 
 
 # ---------------------------------------------------------------------------
+# NaN and infinities
+
+@pytest.mark.parametrize("dtype, hq, hkv, hd", [(F32, 4, 4, 64), (BF16, 64, 1, 64)])
+def test_no_part_loses_a_nan(dtype, hq, hkv, hd):
+    """A part of a split context (128 keys here) whose scores are all NaN: so is every row."""
+    dev = device()
+    for n, blocks in ((1290, range(11)), (66 * 128, (0, 5, 63, 64, 65))):
+        rng = np.random.default_rng(n)
+        of = lambda m: rng.standard_normal((m, hkv, hd))  # noqa: E731
+        table, (kp, vp), _ = pages(rng, [n], hkv, hd, dev, of, of)
+        kp, vp = to(dev, kp, torch.uint8), to(dev, vp, torch.uint8)
+        q = to(dev, rng.standard_normal((1, hq, hd)), TYPES[dtype])
+        for b in blocks:
+            k = kp.clone()
+            k[torch.from_numpy(table[0, 8 * b:8 * b + 8].astype(np.int64)).to(dev)] = 0xFF
+            out = attend(dtype, [1], [n - 1], table, len(kp), hq, hkv, hd, q, k, vp, dev)
+            assert bool(out.isnan().all()), (n, b)
+
+
+# ---------------------------------------------------------------------------
 # captured calls
 
 @pytest.mark.parametrize("rows, pos0, taken", [([6], [2047], True), ([1], [100], True), ([1], [2600], True), ([3, 2, 4], [50, 900, 20], True),
