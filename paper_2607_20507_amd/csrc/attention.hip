@@ -516,6 +516,7 @@ __device__ __forceinline__ void attn_prefill_body(const AttnArgs& a, const AttnI
         for (int hh = 0; hh < 2; ++hh) sc[nt][hh] = mfma16x16x32(kf[hh][s], qf[nt][s], sc[nt][hh]);
   };
   // output update with the chunk of keys c0 .. in vf and its probabilities in pf
+  bool dropped = false;
   auto output = [&](int c0) {
     if (c0 + 32 > t1) {
       // keys past the sequence hold stale or uninitialised V (their
@@ -528,6 +529,21 @@ __device__ __forceinline__ void attn_prefill_body(const AttnArgs& a, const AttnI
         vf[dt].y = mask_pair(vf[dt].y, nvalid - 2);
         vf[dt].z = mask_pair(vf[dt].z, nvalid - 4);
         vf[dt].w = mask_pair(vf[dt].w, nvalid - 6);
+      }
+    }
+    // FAR: a value that is not finite may lie in a key that some row does not see
+    if constexpr (FAR) {
+      if (c0 + 31 > pos_lo) {
+        asm volatile("");
+        uint32_t bad = 0;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+          bad |= nonfinite_bits(vf[dt].x) | nonfinite_bits(vf[dt].y) | nonfinite_bits(vf[dt].z) | nonfinite_bits(vf[dt].w);
+        if (__any(bad != 0)) {
+          dropped = true;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) vf[dt] = drop_nonfinite(vf[dt]);
+        }
       }
     }
 #pragma unroll
@@ -668,6 +684,23 @@ __device__ __forceinline__ void attn_prefill_body(const AttnArgs& a, const AttnI
     }
     if (64 * ns - 32 <= pos_hi) output(64 * ns - 32);
     if (wave < 4) phase_end();
+  }
+  if constexpr (FAR) {
+    // what the dropped values do to the rows that see them (rare, so after the
+    // walk, where it takes no registers from it)
+    if (dropped)
+      for (int c0 = max(pos_lo - 31, 0) / 32 * 32; c0 <= pos_hi; c0 += 32) {
+        if (c0 + 31 <= pos_lo) continue;
+        const uint4* vb = reinterpret_cast<const uint4*>(
+            vp + (static_cast<size_t>(s_pt[min((c0 + 8 * g) >> 4, np - 1)]) * a.Hkv + gkv) * 16 * HD);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const uint4 marks = nonfinite_marks(vb[(dt * 2 + (g & 1)) * 16 + l16]);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            acc[dt][nt] += nonfinite_sum(mfma16x16x32(marks, seen_keys(klim[nt] - (c0 + 8 * g)), f32x4{0.f, 0.f, 0.f, 0.f}));
+        }
+      }
   }
 
 #pragma unroll

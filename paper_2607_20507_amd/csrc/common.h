@@ -102,6 +102,48 @@ __device__ __forceinline__ f32x4 mfma16x16x32v(const u32x4& a, const u32x4& b, f
 }
 
 // ---------------------------------------------------------------------------
+// Attention where a value that some rows do not see is not finite: its product
+// with their probability 0 would be NaN.  Such values are dropped from the
+// product, and what they do to the rows that see their keys is counted apart, by a
+// product of marks (+inf 1, -inf 2^8, NaN 2^16; of 32 keys the counts do not run
+// into each other and are exact in fp32) with the keys seen.
+
+// Non-zero where a bf16 half of w is an infinity or a NaN.
+__device__ __forceinline__ uint32_t nonfinite_bits(uint32_t w) { return ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+
+__device__ __forceinline__ uint32_t nonfinite_marks(uint32_t w) {
+  auto mark = [](uint32_t h) -> uint32_t {  // as bf16
+    return (h & 0x7F80u) != 0x7F80u ? 0u : (h & 0x7Fu) ? 0x4780u : (h & 0x8000u) ? 0x4380u : 0x3F80u;
+  };
+  return mark(w & 0xFFFFu) | mark(w >> 16) << 16;
+}
+__device__ __forceinline__ uint4 nonfinite_marks(const uint4& v) {
+  return make_uint4(nonfinite_marks(v.x), nonfinite_marks(v.y), nonfinite_marks(v.z), nonfinite_marks(v.w));
+}
+__device__ __forceinline__ uint4 drop_nonfinite(const uint4& v) {
+  auto keep = [](uint32_t w) {
+    const uint32_t b = nonfinite_bits(w) >> 15;  // 1 in the halves to drop
+    return w & ~(b * 0xFFFFu);
+  };
+  return make_uint4(keep(v.x), keep(v.y), keep(v.z), keep(v.w));
+}
+// bf16 ones for the keys 0 .. last of 8 (last < 0: none).
+__device__ __forceinline__ uint4 seen_keys(int last) {
+  auto two = [&](int j) { return (j <= last ? 0x3F80u : 0u) | (j + 1 <= last ? 0x3F800000u : 0u); };
+  return make_uint4(two(0), two(2), two(4), two(6));
+}
+// What the counted values add to a row's sums.
+__device__ __forceinline__ f32x4 nonfinite_sum(const f32x4& count) {
+  f32x4 s;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t n = static_cast<uint32_t>(count[i]), minus = n >> 8 & 255u, plus = n & 255u;
+    s[i] = n >> 16 || (minus && plus) ? __builtin_nanf("") : minus ? -INFINITY : plus ? INFINITY : 0.f;
+  }
+  return s;
+}
+
+// ---------------------------------------------------------------------------
 // Direct-to-LDS loads (global -> LDS with no register staging) and the
 // explicit waits their users issue.
 

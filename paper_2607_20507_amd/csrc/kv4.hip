@@ -56,6 +56,29 @@ __device__ __forceinline__ void get8_tokens(uint32_t w0, uint32_t w1, uint32_t s
   hi = make_uint4(high(t0, t1), high(t2, t3), high(t4, t5), high(t6, t7));
 }
 
+// Whether one of 4 scale bytes is at least 252: no other block holds a value that
+// is not finite.
+__device__ __forceinline__ bool scale_near_top(uint32_t w) {
+  const uint32_t x = ~w & 0xFCFCFCFCu;  // a byte of 0 for each such scale
+  return ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
+}
+
+// 0xFF in the bytes of w that equal b.
+__device__ __forceinline__ uint32_t bytes_equal(uint32_t w, uint32_t b) {
+  const uint32_t x = w ^ (b * 0x01010101u);
+  return ((~(((x & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | x) & 0x80808080u) >> 7) * 255u;
+}
+
+// Zeroes the values that are not finite among 4 bytes of codes with their scales:
+// all under the scale 255, magnitudes of 2^128 and more under 253 (4 and 6) and
+// 254 (2 and more).
+__device__ __forceinline__ void drop_nonfinite(uint32_t& codes, uint32_t& scales) {
+  const uint32_t nan = bytes_equal(scales, 255u);
+  const uint32_t two = codes >> 2 & 0x11111111u, four = two & codes >> 1;
+  codes &= ~(nan | bytes_equal(scales, 253u) & (four * 15u) | bytes_equal(scales, 254u) & (two * 15u));
+  scales &= ~nan;
+}
+
 template <typename T>
 __device__ __forceinline__ void put8(T* dst, const float (&v)[8]) {
   if constexpr (sizeof(T) == 2) {
@@ -479,7 +502,7 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
   float mrun[NT], mlim[NT], mneg[NT];
   f32x4 lrun[NT];
   const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
-  bool far = false;
+  bool far = false, dropped = false;
   f32x4 acc[DT][NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -634,6 +657,18 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
           w.vs[i] &= static_cast<uint32_t>(i % 2 ? keep >> 32 : keep);
         }
       }
+      if (!full || NP > 1) {
+        // a value that is not finite may lie in a key that some row does not see, and
+        // the parts of a probability may be 0 or negative
+        bool top = false;
+#pragma unroll
+        for (int i = 0; i < 2 * DS; ++i) top |= scale_near_top(w.vs[i]);
+        if (__any(top)) {
+          dropped = true;
+#pragma unroll
+          for (int i = 0; i < 2 * DS; ++i) drop_nonfinite(w.vc[i], w.vs[i]);
+        }
+      }
 #pragma unroll
       for (int b = 0; b < DS; ++b) {
         uint4 v[2];
@@ -657,6 +692,25 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
       load_v(raw, cfirst);
     }
     for (int c0 = cfirst; c0 < it.t1; c0 += 32 * W) chunk(raw, c0, min(c0 + 32 * W, it.t1 - 1));
+    // what the dropped values do to the rows that see them (rare, so after the walk,
+    // where it takes no registers from it)
+    if (dropped)
+      for (int c0 = cfirst; c0 < it.t1; c0 += 32 * W) {
+        if (NP == 1 && c0 + 32 <= it.t1 && c0 + 31 <= pos_lo) continue;  // nothing was dropped there
+        load_v(raw, c0);
+#pragma unroll
+        for (int b = 0; b < DS; ++b) {
+          uint4 v[2];
+          get8_tokens(raw.vc[2 * b], raw.vc[2 * b + 1], raw.vs[2 * b], raw.vs[2 * b + 1], v[0], v[1]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint4 marks = nonfinite_marks(v[i]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              acc[2 * b + i][nt] += nonfinite_sum(mfma16x16x32(marks, seen_keys(klim[nt] - (c0 + 8 * g)), f32x4{0.f, 0.f, 0.f, 0.f}));
+          }
+        }
+      }
   };
   if constexpr (kInArgs) {
     walk(std::true_type{});
@@ -703,7 +757,10 @@ __global__ __launch_bounds__(256) void combine_kv4_kernel(AttnArgs a, const Attn
       const size_t pm = base + min(p0 + i * P, gr.nparts - 1) * stride;
       c[i] = ml[pm];
       o[i] = *reinterpret_cast<const f32x4*>(a.part_o + pm * HD + d0);
-      if (p0 + i * P >= gr.nparts) c[i] = make_float2(-INFINITY, 0.f);
+      if (p0 + i * P >= gr.nparts) {
+        c[i] = make_float2(-INFINITY, 0.f);
+        o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
     }
     float mx = M;
 #pragma unroll

@@ -244,6 +244,37 @@ def test_no_part_loses_a_nan(dtype, hq, hkv, hd):
             assert bool(out.isnan().all()), (n, b)
 
 
+@pytest.mark.parametrize("dtype, hq, hkv, hd", [(F32, 4, 4, 64), (F32, 8, 2, 128), (BF16, 8, 2, 128), (BF16, 4, 2, 64), (BF16, 64, 1, 64)])
+@pytest.mark.parametrize("what", ["nan value", "infinite value", "nan key"])
+@pytest.mark.parametrize("rows, pos0, bad", [(8, 40, 43), (8, 40, 47), (17, 20, 31), (5, 1290, 1293), (64, 0, 30), (100, 300, 333), (200, 100, 130), (130, 380, 509)])
+def test_keys_that_a_row_does_not_see(dtype, hq, hkv, hd, what, rows, pos0, bad):
+    """A NaN or an infinity in a key or value behind a row's position leaves the row as it is."""
+    dev = device()
+    say("hidden", what, dtype, hq, hkv, hd, rows, pos0, bad)
+    rng = np.random.default_rng([rows, pos0, hd])
+    n = rows + pos0
+    of = lambda m: rng.standard_normal((m, hkv, hd)).astype(np.float32).astype(np.float64)  # noqa: E731
+    table, pools, ((k, v),) = pages(rng, [n], hkv, hd, dev, of, of)
+    pool, place = (pools[0], ref.k_place) if what == "nan key" else (pools[1], ref.v_place)
+    x = np.zeros((1, hkv, hd))
+    x[..., 32:64] = np.nan if what[0] == "n" else 1.9 * 2.0 ** 127  # (held as 2^128, an infinity in fp32)
+    slot = [table[0, bad // 16] * 16 + bad % 16]
+    ref.put(pool, slot, x, place)
+    held = ref.get(pool, np.asarray(slot), hd, place)[0]
+    (k if what == "nan key" else v)[bad] = np.where(np.abs(held) >= 2.0 ** 128, np.inf, held)
+    q = to(dev, rng.standard_normal((rows, hq, hd)), TYPES[dtype])
+    got = attend(dtype, [rows], [pos0], table, len(pools[0]), hq, hkv, hd, q, to(dev, pools[0], torch.uint8),
+                 to(dev, pools[1], torch.uint8), dev).double().cpu().numpy().reshape(rows, hq, hd)
+    want, mag, big = ref.attention_rows(q.double().cpu().numpy(), k, v, pos0)
+    assert np.isfinite(want[:bad - pos0]).all() and not np.isfinite(want[bad - pos0:, :, 32:64]).any()
+    assert np.array_equal(np.isnan(got), np.isnan(want)), "NaN"
+    assert np.array_equal(np.isposinf(got), np.isposinf(want)), "infinities"
+    fine = np.isfinite(want)
+    big = np.where(np.isfinite(big), big, 0)
+    tol = bound(dtype, hd, n, np.where(fine, want, 0), np.where(fine, mag, 0), big)
+    assert np.all(np.abs(got[fine] - want[fine]) <= tol[fine])
+
+
 # ---------------------------------------------------------------------------
 # captured calls
 
