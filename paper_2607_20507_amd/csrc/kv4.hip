@@ -331,14 +331,14 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&w)[N]) {
 }
 
 // Exponents are one FMA, p = 2^(raw scale - M), with M the rounded base-2 logit of
-// the maximum, and the wave's sums are relative to 2^M: a new maximum rescales them
+// the maximum, and a wave's sums are relative to 2^M: a new maximum rescales them
 // by 2^(M - M'), not by the raw difference.  The largest exponent is off from 0 by
-// up to M 2^-24.  Above this M a wave takes the difference of the raw scores first
-// (one instruction more per score), which a 4-bit cache, whose blocks have any
-// scale, may need; its sums are then relative to the raw maximum.  Waves and parts
-// are joined by the differences of their raw maxima, which fp32 holds where it
-// does not hold those of the logits M; a wave that ends in the first form
-// brings its sums to the raw maximum first (to_raw).
+// up to M 2^-24.  A 4-bit cache, whose blocks have any scale, may have larger M than
+// this: a wave that meets one starts over in a form that takes the difference of
+// the raw scores first (one instruction more per score) and whose sums are relative
+// to the raw maximum.  (Both forms in one loop: 16 rows of 64 sequences of 1000 keys
+// 54 us, 50 so.)  Waves and parts are joined by the differences of their raw
+// maxima, which fp32 holds where it does not hold those of the logits M.
 constexpr float kFarLog2 = 16777216.f;
 // A maximum is raised only by a score more than 2^8 times as probable: fewer
 // rescalings, and probabilities stay below 2^8.
@@ -365,49 +365,63 @@ __device__ __forceinline__ void store4(float* o, const f32x4& v) {
   *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
 }
 
-// The waves' states are merged through LDS, each wave taking some of the output
-// tiles, and the output or the partial is written.  m: raw score that a lane's
-// sums are relative to (-inf: no key), l: the wave's sum (in every element).
 template <int HD>
 __device__ __forceinline__ float score_scale() { return kLog2e / sqrtf(static_cast<float>(HD)); }
 
-// Factor of sums relative to 2^-mneg (mneg = -(m scale), rounded) that makes them
-// relative to 2^(m scale).
-__device__ __forceinline__ float to_raw(float m, float scale, float mneg) {
-  return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(-fmaf(m, scale, mneg));
-}
+// Exponent of the factor that brings sums relative to 2^M (M = m scale, rounded) to
+// 2^(m scale).
+__device__ __forceinline__ float to_raw(float m, float scale, float M) { return -fmaf(m, scale, -M); }
 
+// The waves' states are merged through LDS, each wave taking some of the output
+// tiles, and the output or the partial is written.  m: raw score of a query vector's
+// maximum in the wave (-inf: no key), to which (far) or to whose rounded logit the
+// wave's sums are relative; l: the wave's sum (in every element).
 template <typename T, int HD, int NT, int W>
-__device__ __forceinline__ void finish(const AttnArgs& a, const AttnItem& it, int gkv, int M, int lane, int wave,
+__device__ __forceinline__ void finish(const AttnArgs& a, const AttnItem& it, int gkv, int M, int lane, int wave, bool far,
                                        const float (&m)[NT], const f32x4 (&l)[NT], const f32x4 (&acc)[HD / 16][NT]) {
   constexpr int DT = HD / 16;
   const int g = lane >> 4, l16 = lane & 15;
   const int G = a.Hq / a.Hkv;
+  const float scale = score_scale<HD>();
   // one query tile after the other: the buffer of all would leave room for fewer
   // workgroups on a CU
   __shared__ f32x4 s_acc[W][DT][kWave];
-  __shared__ float s_m[W][16], s_l[W][16];
+  __shared__ f32x4 s_st[W][16];  // logit of the maximum, sum, maximum, whether far
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     if (16 * nt >= M) break;
     if (nt > 0) __syncthreads();
-    if (g == 0) {
-      s_m[wave][l16] = m[nt];
-      s_l[wave][l16] = l[nt][0];
-    }
+    if (g == 0) s_st[wave][l16] = f32x4{m[nt] * scale, l[nt][0], m[nt], far ? 1.f : 0.f};
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) s_acc[wave][dt][lane] = acc[dt][nt];
     __syncthreads();
     const int v = 16 * nt + l16;
-    float mm = -INFINITY, e[W];
-#pragma unroll
-    for (int w = 0; w < W; ++w) mm = fmaxf(mm, s_m[w][l16]);
-    float lt = 0.f;
+    f32x4 st[W];
+    float mm = -INFINITY, any = 0.f, e[W], lt = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      e[w] = s_m[w][l16] == -INFINITY ? 0.f : exp2f((s_m[w][l16] - mm) * score_scale<HD>());
-      lt += e[w] * s_l[w][l16];
+      st[w] = s_st[w][l16];
+      mm = fmaxf(mm, st[w][0]);
+      any += st[w][3];
     }
+    float part = 1.f, top = -INFINITY;  // what a partial's sums are multiplied by, and its raw maximum
+    if (it.part >= 0 || any > 0.f) {
+#pragma unroll
+      for (int w = 0; w < W; ++w) top = fmaxf(top, st[w][2]);
+    }
+    if (any > 0.f) {
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+        e[w] = st[w][2] == -INFINITY
+                   ? 0.f
+                   : exp2f(fmaf(st[w][2] - top, scale, st[w][3] > 0.f ? 0.f : to_raw(st[w][2], scale, st[w][0])));
+    } else {
+#pragma unroll
+      for (int w = 0; w < W; ++w) e[w] = st[w][0] == -INFINITY ? 0.f : exp2f(st[w][0] - mm);
+      if (it.part >= 0 && top > -INFINITY) part = exp2f(to_raw(top, scale, mm));
+    }
+#pragma unroll
+    for (int w = 0; w < W; ++w) lt += e[w] * st[w][1];
     if (v < M)
     for (int dt = wave; dt < DT; dt += W) {
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -418,8 +432,8 @@ __device__ __forceinline__ void finish(const AttnArgs& a, const AttnItem& it, in
                o * (1.f / lt));
       } else {
         const size_t pm = (static_cast<size_t>(it.part) * a.Hkv + gkv) * 64 + v;
-        store4(a.part_o + pm * HD + 16 * dt + 4 * g, o);
-        if (dt == 0 && g == 0) reinterpret_cast<float2*>(a.part_ml)[pm] = make_float2(mm, lt);
+        store4(a.part_o + pm * HD + 16 * dt + 4 * g, o * part);
+        if (dt == 0 && g == 0) reinterpret_cast<float2*>(a.part_ml)[pm] = make_float2(top, lt * part);
       }
     }
   }
@@ -502,28 +516,47 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
   float mrun[NT], mlim[NT], mneg[NT];
   f32x4 lrun[NT];
   const uint4 ones = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
-  bool far = false, dropped = false;
+  bool dropped;
   f32x4 acc[DT][NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    mrun[nt] = mlim[nt] = -INFINITY;
-    mneg[nt] = 0.f;
-    lrun[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  const int cfirst = it.t0 + 32 * wave;  // the wave's first chunk; it takes every W-th
+  auto any_page = [&](int t) -> size_t {
+    if (kInArgs || staged) return s_pt[(t >> 4) - p0];
+    return global_page(tab, pt + (t >> 4));
+  };
 
-  auto walk = [&](auto from_lds) {
-    auto page = [&](int t) -> size_t {
-      if constexpr (kInArgs || decltype(from_lds)::value) return s_pt[(t >> 4) - p0];
-      else return global_page(tab, pt + (t >> 4));
-    };
-    // codes and scales of one 32-key chunk's operands (keys past t1 clamped to
-    // a valid page; their scores are masked and their V entries zeroed)
-    struct Raw {
-      uint32_t kc[2 * DS], ks[DS / 2];  // [key tile][step] (hd 64 too: a lane's 16 bytes hold both tiles)
-      uint32_t vc[2 * DS], vs[2 * DS];  // [block][token half]
-    };
+  // codes and scales of one 32-key chunk's operands (keys past t1 clamped to
+  // a valid page; their scores are masked and their V entries zeroed)
+  struct Raw {
+    uint32_t kc[2 * DS], ks[DS / 2];  // [key tile][step] (hd 64 too: a lane's 16 bytes hold both tiles)
+    uint32_t vc[2 * DS], vs[2 * DS];  // [block][token half]
+  };
+  auto load_v = [&](Raw& w, int c0, auto page) {
+    const uint8_t* blk = vp + (page(min(c0 + 8 * g, it.t1 - 1)) * a.Hkv + gkv) * BB;
+    const int th = g & 1;
+#pragma unroll
+    for (int i = 0; i < HD / 64; ++i) {
+      const uint4 u = ld_stream(reinterpret_cast<const uint4*>(blk) + (i * 2 + th) * 16 + l16);
+      w.vc[4 * i] = u.x; w.vc[4 * i + 1] = u.y; w.vc[4 * i + 2] = u.z; w.vc[4 * i + 3] = u.w;
+      const uint4 s = *(reinterpret_cast<const uint4*>(blk + CB) + th * (DS / 2) + i);
+      w.vs[4 * i] = s.x; w.vs[4 * i + 1] = s.y; w.vs[4 * i + 2] = s.z; w.vs[4 * i + 3] = s.w;
+    }
+    asm volatile("" ::: "memory");
+  };
+
+  // The wave's sums over its chunks, in the form for large logits (FAR) or not; whether
+  // the form does not hold a logit.
+  auto walk = [&](auto page, auto far_form) -> bool {
+    constexpr bool FAR = decltype(far_form)::value;
+    bool far = false;
+    dropped = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      mrun[nt] = mlim[nt] = -INFINITY;
+      mneg[nt] = 0.f;
+      lrun[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     auto load_k = [&](Raw& w, int c0) {
       const uint8_t* blk = kp + (page(min(c0 + 16 * (l16 >> 3), it.t1 - 1)) * a.Hkv + gkv) * BB;
       const int j = l16 & 7;
@@ -537,18 +570,6 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
       for (int i = 0; i < DS / 2; ++i) w.ks[i] = sp[i];
       // (loads stay where they are issued: the compiler had moved the scales' to
       // their use, a memory latency in every chunk)
-      asm volatile("" ::: "memory");
-    };
-    auto load_v = [&](Raw& w, int c0) {
-      const uint8_t* blk = vp + (page(min(c0 + 8 * g, it.t1 - 1)) * a.Hkv + gkv) * BB;
-      const int th = g & 1;
-#pragma unroll
-      for (int i = 0; i < HD / 64; ++i) {
-        const uint4 u = ld_stream(reinterpret_cast<const uint4*>(blk) + (i * 2 + th) * 16 + l16);
-        w.vc[4 * i] = u.x; w.vc[4 * i + 1] = u.y; w.vc[4 * i + 2] = u.z; w.vc[4 * i + 3] = u.w;
-        const uint4 s = *(reinterpret_cast<const uint4*>(blk + CB) + th * (DS / 2) + i);
-        w.vs[4 * i] = s.x; w.vs[4 * i + 1] = s.y; w.vs[4 * i + 2] = s.z; w.vs[4 * i + 3] = s.w;
-      }
       asm volatile("" ::: "memory");
     };
     // the chunk of keys c0 .. held in w, which then takes the wave's chunk of keys cn ..
@@ -604,40 +625,28 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
           float m = mx[nt];
           m = fmaxf(m, __shfl_xor(m, 16, kWave));
           m = fmaxf(m, __shfl_xor(m, 32, kWave));
-          mx[nt] = m > mlim[nt] ? m : mrun[nt];
-          large |= fabsf(mx[nt] * scale) > kFarLog2 && mx[nt] > -INFINITY;
-        }
-        const bool was_far = far;
-        far |= __any(large) != 0;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float m = mx[nt], neg = m == -INFINITY ? 0.f : -m * scale;
-          float alpha = __builtin_amdgcn_exp2f(neg - mneg[nt]);
-          if (far) {
-            alpha = __builtin_amdgcn_exp2f((mrun[nt] - m) * scale);
-            if (!was_far) alpha *= to_raw(mrun[nt], scale, mneg[nt]);
-          }
-          if (mrun[nt] == -INFINITY) alpha = 0.f;
+          m = m > mlim[nt] ? m : mrun[nt];
+          const float neg = m == -INFINITY ? 0.f : -m * scale;
+          const float alpha =
+              mrun[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(FAR ? (mrun[nt] - m) * scale : neg - mneg[nt]);
           mrun[nt] = m;
           mlim[nt] = m + kRescaleLog2 / scale;
           mneg[nt] = neg;
+          large |= fabsf(neg) > kFarLog2;
           lrun[nt] *= alpha;
 #pragma unroll
           for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= alpha;
         }
+        if constexpr (!FAR) far |= __any(large) != 0;
       }
       uint4 pf[NT][NP];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float p[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(raw[nt][j], scale, mneg[nt]));
-        if (far) {
-          asm volatile("");
-          const float m = mrun[nt] == -INFINITY ? 0.f : mrun[nt];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f((raw[nt][j] - m) * scale);
-        }
+        for (int j = 0; j < 8; ++j)
+          p[j] = __builtin_amdgcn_exp2f(FAR ? (raw[nt][j] - (mrun[nt] == -INFINITY ? 0.f : mrun[nt])) * scale
+                                            : fmaf(raw[nt][j], scale, mneg[nt]));
         uint32_t h[4][NP];
 #pragma unroll
         for (int j = 0; j < 4; ++j) split_pair<NP>(p[2 * j], p[2 * j + 1], h[j]);
@@ -680,54 +689,48 @@ __global__ __launch_bounds__(64 * W, NT * Parts<T>::n <= 3 ? 2 : 1) void attn_kv
 #pragma unroll
             for (int n = 0; n < NP; ++n) acc[2 * b + i][nt] = mfma16x16x32(v[i], pf[nt][n], acc[2 * b + i][nt]);
       }
-      load_v(w, cn);
+      load_v(w, cn, page);
     };
     // The wave's chunks: the next one's operands are loaded as soon as this one's
     // are converted.  (Two chunks in flight took more registers and no less time:
     // 64 sequences 42.7 .. 47.1 us against 43.7 .. 47.1, 131000 keys 37.3 and 36.4.)
     Raw raw;
-    const int cfirst = it.t0 + 32 * wave;
     if (cfirst < it.t1) {
       load_k(raw, cfirst);
-      load_v(raw, cfirst);
+      load_v(raw, cfirst, page);
     }
-    for (int c0 = cfirst; c0 < it.t1; c0 += 32 * W) chunk(raw, c0, min(c0 + 32 * W, it.t1 - 1));
-    // what the dropped values do to the rows that see them (rare, so after the walk,
-    // where it takes no registers from it)
-    if (dropped)
-      for (int c0 = cfirst; c0 < it.t1; c0 += 32 * W) {
-        if (NP == 1 && c0 + 32 <= it.t1 && c0 + 31 <= pos_lo) continue;  // nothing was dropped there
-        load_v(raw, c0);
+    for (int c0 = cfirst; c0 < it.t1 && !far; c0 += 32 * W) chunk(raw, c0, min(c0 + 32 * W, it.t1 - 1));
+    return far;
+  };
+  bool far;
+  if constexpr (kInArgs) {
+    far = walk([&](int t) -> size_t { return s_pt[(t >> 4) - p0]; }, std::false_type{});
+  } else {
+    if (staged) far = walk([&](int t) -> size_t { return s_pt[(t >> 4) - p0]; }, std::false_type{});
+    else far = walk([&](int t) -> size_t { return global_page(tab, pt + (t >> 4)); }, std::false_type{});
+  }
+  if (far) walk(any_page, std::true_type{});
+  // what the dropped values do to the rows that see them (rare, so after the walk,
+  // where it takes no registers from it)
+  if (dropped)
+    for (int c0 = cfirst; c0 < it.t1; c0 += 32 * W) {
+      if (NP == 1 && c0 + 32 <= it.t1 && c0 + 31 <= pos_lo) continue;  // nothing was dropped there
+      Raw raw;
+      load_v(raw, c0, any_page);
 #pragma unroll
-        for (int b = 0; b < DS; ++b) {
-          uint4 v[2];
-          get8_tokens(raw.vc[2 * b], raw.vc[2 * b + 1], raw.vs[2 * b], raw.vs[2 * b + 1], v[0], v[1]);
+      for (int b = 0; b < DS; ++b) {
+        uint4 v[2];
+        get8_tokens(raw.vc[2 * b], raw.vc[2 * b + 1], raw.vs[2 * b], raw.vs[2 * b + 1], v[0], v[1]);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint4 marks = nonfinite_marks(v[i]);
+        for (int i = 0; i < 2; ++i) {
+          const uint4 marks = nonfinite_marks(v[i]);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              acc[2 * b + i][nt] += nonfinite_sum(mfma16x16x32(marks, seen_keys(klim[nt] - (c0 + 8 * g)), f32x4{0.f, 0.f, 0.f, 0.f}));
-          }
+          for (int nt = 0; nt < NT; ++nt)
+            acc[2 * b + i][nt] += nonfinite_sum(mfma16x16x32(marks, seen_keys(klim[nt] - (c0 + 8 * g)), f32x4{0.f, 0.f, 0.f, 0.f}));
         }
       }
-  };
-  if constexpr (kInArgs) {
-    walk(std::true_type{});
-  } else {
-    if (staged) walk(std::true_type{});
-    else walk(std::false_type{});
-  }
-  if (!far) {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const float f = to_raw(mrun[nt], scale, mneg[nt]);
-      lrun[nt] *= f;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= f;
     }
-  }
-  finish<T, HD, NT, W>(a, it, gkv, M, lane, wave, mrun, lrun, acc);
+  finish<T, HD, NT, W>(a, it, gkv, M, lane, wave, far, mrun, lrun, acc);
 }
 
 // Merges the parts of split items: with M the largest maximum of raw scores, out =
