@@ -74,15 +74,19 @@ __device__ __forceinline__ uint64_t key_of(float v, int i) {
 __device__ __forceinline__ float value_of(uint64_t k) { return unordered(static_cast<uint32_t>(k >> 32)); }
 __device__ __forceinline__ int id_of(uint64_t k) { return static_cast<int>(~static_cast<uint32_t>(k)); }
 
-// 1 / T in base 2, finite and above 0, so that 0 and -inf times it stay what they
-// are (T = 0, negative and NaN rows: any such factor)
+// (a - m) / 2: fp32 holds it where a - m passes the type's range, and it is as exact
+// as that (but for values below 2^-126), in one instruction too.
+__device__ __forceinline__ float half_diff(float a, float m) { return fmaf(a, 0.5f, -0.5f * m); }
+
+// 2 / T in base 2 (for half_diff), finite and above 0, so that 0 and -inf times it
+// stay what they are (T = 0, negative and NaN rows: any such factor)
 __device__ __forceinline__ float base2_factor(float t) {
-  return t > 0.f ? fmaxf(fminf(fminf(1.f / t, FLT_MAX) * kLog2e, FLT_MAX), __uint_as_float(1u)) : kLog2e;
+  return t > 0.f ? fmaxf(fminf(fminf(2.f / t, FLT_MAX) * kLog2e, FLT_MAX), __uint_as_float(1u)) : kLog2e;
 }
 
 __device__ __forceinline__ void stat_merge(LpStat& a, const LpStat& b, float c) {
   const float M = fmaxf(a.m, b.m);
-  const float da = fmaxf((a.m - M) * c, kFloor), db = fmaxf((b.m - M) * c, kFloor);
+  const float da = fmaxf(half_diff(a.m, M) * c, kFloor), db = fmaxf(half_diff(b.m, M) * c, kFloor);
   const float ea = exp2f(da), eb = exp2f(db);
   a.u = ea * (a.u + da * a.s) + eb * (b.u + db * b.s);
   a.s = ea * a.s + eb * b.s;
@@ -229,7 +233,7 @@ __global__ __launch_bounds__(kThreads) void logprob_chunk_kernel(int V, const fl
 #pragma unroll
     for (int e = 1; e < kPerThread; ++e) vm = fmaxf(vm, v[e]);
     if (vm > st.m || (vm == st.m && st.idx == INT_MAX)) {
-      const float d = fmaxf((st.m - vm) * c, kFloor), a = exp2f(d);
+      const float d = fmaxf(half_diff(st.m, vm) * c, kFloor), a = exp2f(d);
       st.u = a * (st.u + d * st.s);
       st.s *= a;
       st.m = vm;
@@ -241,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void logprob_chunk_kernel(int V, const fl
     }
 #pragma unroll
     for (int e = 0; e < kPerThread; ++e) {
-      const float t = (v[e] - st.m) * c;
+      const float t = half_diff(v[e], st.m) * c;
       const float p = __builtin_amdgcn_exp2f(t);  // (a NaN stays one; a masked logit's p is 0)
       st.s += p;
       st.u = fmaf(fmaxf(t, kFloor), p, st.u);
@@ -363,7 +367,7 @@ __global__ __launch_bounds__(kThreads) void logprob_final_kernel(int V, const fl
     if (!ok) return __builtin_nanf("");
     if (T == 0.f) return i == st.idx ? 0.f : -INFINITY;
     if (v == -INFINITY) return v;  // masked at T = inf too, where v / T is no number
-    return (v - st.m) / T - log_s;
+    return 2.f * (half_diff(v, st.m) / T) - log_s;
   };
   if (tid == 0) {
     if (logp) {
