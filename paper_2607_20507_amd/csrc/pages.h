@@ -119,10 +119,11 @@ class PagePool {
       while (holders_[to] != 0) ++to;
       moves.emplace_back(from, to++);
     }
-    decltype(free_) left;
-    for (int p = live; p < num_pages_; ++p) left.push(p);
+    std::vector<int32_t> left;
+    left.reserve(num_pages_);  // (pages are given up without an allocation)
+    for (int p = live; p < num_pages_; ++p) left.push_back(p);
     for (const auto& m : moves) std::swap(holders_[m.first], holders_[m.second]);
-    free_.swap(left);
+    free_ = decltype(free_)(std::greater<int32_t>(), std::move(left));
     return moves;
   }
   int32_t slot(const std::vector<int32_t>& table, int64_t pos) const {

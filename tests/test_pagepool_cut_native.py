@@ -98,3 +98,10 @@ def test_against_a_model(exe, seed):
             slots = [int(s) for s in head[2:]]
             assert len(slots) == len(set(slots)) and set(slots) == w[2], script[line]
         assert {k: v for k, v in tables.items() if v} == {k: v for k, v in wt.items() if v}, script[line]
+
+
+def test_giving_up_pages_allocates_nothing(exe):
+    """Also after a compaction: the calls that give up pages pass no exception on."""
+    script = [f"E {i} 64" for i in range(10)] + ["C 3 0 64", "C 7 16 64", "K 0 0", "D 0 0", "E 1 640", "D 0 0"]
+    got = run(exe, 40, script)
+    assert [g[0] for g in got if g[0][0] == "allocated"] == [["allocated", "0"]] * 2
