@@ -220,15 +220,18 @@ class SpecSession:
         entropy, top ids, top logprobs)."""
         z = self._last_logits()
         R, V = z.shape
-        dev = z.device
+        dev, f32 = z.device, torch.float32
+        for what, a in (("tokens", tokens), ("temps", temps)):
+            if a is not None and len(a) != R:
+                raise ValueError(f"{what}: one for each of the {R} rows")
         # buffers of the stream that the call runs on
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
             tok = None if tokens is None else torch.from_numpy(np.asarray(tokens, dtype=np.int32)).to(dev)
             t = None if temps is None else torch.from_numpy(np.asarray(temps, dtype=np.float32)).to(dev)
-            logp = None if tok is None else torch.empty(R, device=dev)
-            entropy = torch.empty(R, device=dev)
+            logp = None if tok is None else torch.empty(R, dtype=f32, device=dev)
+            entropy = torch.empty(R, dtype=f32, device=dev)
             ids = torch.empty(R, n_top, dtype=torch.int32, device=dev)
-            top = torch.empty(R, n_top, device=dev)
+            top = torch.empty(R, n_top, dtype=f32, device=dev)
             ws = torch.empty(max(16, B.spec_token_logprobs_workspace_bytes(R, V, n_top)), dtype=torch.uint8, device=dev)
             B.spec_token_logprobs(z, t, tok, logp, entropy, ids if n_top else None, top if n_top else None, ws)
         return logp, entropy, ids, top
