@@ -1,6 +1,8 @@
 /*
  * spec_ops.h - single-kernel entry points of the verify step, for checking
- * each kernel on its own at full workload sizes.  Same conventions as spec.h:
+ * each kernel on its own at full workload sizes, and operators beside it (page
+ * copies; a 4-bit cache, which no context holds) for callers that run them one
+ * by one.  Same conventions as spec.h:
  * "device" pointers are HIP device addresses, "host" pointers CPU memory,
  * stream is a hipStream_t as void*, errors are spec_status codes and the
  * caller owns every buffer.
@@ -78,7 +80,7 @@ SPEC_API spec_status spec_op_attention(int32_t dtype, int32_t n_seqs, const int3
  * aligned, >= spec_op_kv_copy_pages_workspace_bytes(n), not shared by calls that
  * overlap in time.  A captured call takes at most 384 pairs
  * (SPEC_E_UNSUPPORTED beyond).  Asynchronous; host arrays are consumed before
- * return. */
+ * return (more pairs are staged as the larger tables of spec_op_attention_kv4). */
 SPEC_API size_t spec_op_kv_copy_pages_workspace_bytes(int32_t n);
 SPEC_API spec_status spec_op_kv_copy_pages(int32_t n_planes, int32_t num_pages, size_t page_bytes, void* pool,
                                            int32_t n, const int32_t* src_pages, const int32_t* dst_pages,
@@ -92,8 +94,9 @@ SPEC_API spec_status spec_op_kv_copy_pages(int32_t n_planes, int32_t num_pages, 
  * integer >= -126 with max |x| <= 6 2^E, and for every x the nearest of 0, 0.5,
  * 1, 1.5, 2, 3, 4, 6 times 2^E with its sign (ties to the one of even code 0, 2,
  * 4, 6 in that order).  A block with an infinity or a NaN reads back as NaN.
- * Every value held is a bf16 number.  The library alone writes the pages
- * (kv4_layout.h has the byte order). */
+ * Every value held is a bf16 number, but for magnitudes from 1.75 2^127 on, which
+ * are held as 2^128 and read back as infinities.  The library alone writes the
+ * pages (kv4_layout.h has the byte order). */
 SPEC_API size_t spec_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim);
 
 /* spec_op_rope_kv into a 4-bit cache: q_out <- the rotated q (dtype), the
@@ -117,12 +120,17 @@ SPEC_API spec_status spec_op_kv4_read(int32_t dtype, int32_t R, int32_t n_kv_hea
  * rows[i] may be 0 (a sequence without rows in this call).  num_pages: pages of
  * the pool; a page id outside it is refused (SPEC_E_INVALID).  q, out: dtype,
  * 16-byte aligned.  n_heads / n_kv_heads <= 64 (bf16) or 32 (fp32), else
- * SPEC_E_UNSUPPORTED.  fp32 keeps q and the probabilities to 24 bits.
+ * SPEC_E_UNSUPPORTED.  Scores and sums are fp32; the probabilities' product with
+ * V takes them to 24 bits in fp32, and rounded to bf16's 8 in bf16, as
+ * spec_op_attention does.  A NaN or an infinity in the cache reaches the rows
+ * that see its key only.
  * workspace: device, 256-byte aligned, >= spec_op_attention_kv4_workspace_bytes
  * of the same rows and positions (0 for arguments the call refuses), not shared
  * by calls that overlap in time.  A captured call takes tables of at most 3 KB
- * (SPEC_E_UNSUPPORTED beyond). Asynchronous; host arrays are consumed before
- * return. */
+ * (SPEC_E_UNSUPPORTED beyond).  Asynchronous, host arrays are consumed before
+ * return; but larger tables go through four staging buffers that the context-free
+ * calls of a process share, and with four such calls in flight the host waits for
+ * the oldest one's tables to be taken. */
 SPEC_API size_t spec_op_attention_kv4_workspace_bytes(int32_t dtype, int32_t n_seqs, const int32_t* rows,
                                                       const int32_t* pos0, int32_t max_pages, int32_t n_heads,
                                                       int32_t n_kv_heads, int32_t head_dim);

@@ -114,7 +114,7 @@ __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0
 // roundings before it; q is rotated in fp32.
 //
 // HBM bound: 8192 rows of 32 / 8 heads of 128 (202 MB of fp32 in, 76 MB out) take
-// 53 us, 5.2 TB/s.  Workgroups go to the 8 XCDs in turn, and a page's cache lines
+// 51 us, 5.4 TB/s.  Workgroups go to the 8 XCDs in turn, and a page's cache lines
 // hold parts of all of its tokens, so rows in their order leave every XCD's cache
 // with pieces of lines: 114 MB written.  Here kXcdRows consecutive rows share an
 // XCD (16, 32 or 64: 74.1 -> 68.6 us with the read-back of 8192 rows after it);
@@ -257,8 +257,9 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(int R, int Hkv, int hd, c
 // ---------------------------------------------------------------------------
 // Expansion to bf16 pages, which the prompt form's attention reads: one workgroup
 // per (page, kv head).  A prompt's attention reads every key once for each 256 / G
-// of its rows, so converting them once and writing them out (HBM bound: 8192 keys
-// of 8 heads of 128, 8.9 MB in and 33.5 out, 8.6 us, 4.9 TB/s) is 2% of its time.
+// of its rows, so they are converted once and written out (HBM bound: 8192 keys
+// of 8 heads of 128, 8.9 MB in and 33.5 out, 8.5 us, 4.9 TB/s): 2% of the time of 8192
+// rows, and much of it for few rows behind many keys (the planner's comment).
 template <int HD>
 __global__ __launch_bounds__(256) void kv4_expand_kernel(const int32_t* __restrict__ src, int Hkv,
                                                          const uint8_t* __restrict__ kpool,
@@ -302,10 +303,10 @@ __global__ __launch_bounds__(256) void kv4_expand_kernel(const int32_t* __restri
 // of fraction), whose products with the cache's values are exact in fp32.
 //
 // Bound by HBM where a tile has up to 16 query vectors: 131000 keys of 8 heads of
-// 128 (142 MB) take 26 us, 5.5 TB/s.  With 32 by instruction issue and the
+// 128 (142 MB) take 26 us, 5.4 TB/s.  With 32 by instruction issue and the
 // longest items' chains: at 64 sequences of 4 .. 8 rows and 512 .. 4096 keys (127
-// MB, 31 us) a CU holds waves in 55 of 86 thousand cycles, and of those vector
-// instructions take 68%, matrix ones 27%; a 32-key chunk has about 235 of the
+// MB, 30 us) a CU holds waves in 56 of 86 thousand cycles, and of those vector
+// instructions take 67%, matrix ones 26%; a 32-key chunk has about 235 of the
 // former, 64 of them conversions, 32 that bring tokens beside each other, 32 that
 // shift scales and 32 exponents and their arguments.  Small calls are latency: one
 // sequence of 2000 keys 12.9 us.
@@ -317,7 +318,10 @@ struct Parts<bf16_t> { static constexpr int n = 1; };
 template <>
 struct Parts<float> { static constexpr int n = 3; };
 
-// Two fp32 -> N pairs of bf16 whose sums are the values (N = 1: rounded once).
+// Two fp32 -> N pairs of bf16 whose sums are the values (N = 1: rounded once, which
+// for probabilities is what the matrix instructions take: three parts would triple
+// the products of instruction-bound tiles for an error against 64 bits of 0.0017
+// instead of 0.0022 to 0.0024, the output's own rounding in both).
 template <int N>
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t (&w)[N]) {
 #pragma unroll

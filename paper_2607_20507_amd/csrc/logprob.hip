@@ -9,8 +9,9 @@
 // point mass on the first maximum.
 //
 // HBM bound where there are many rows: 1792 x 128256 logits (919 MB) take 163 us a
-// call, the chunks' kernel 154 (6.0 TB/s).  8 rows of 32000 are latency, 11.7 us:
-// 7 in the chunks' kernel, 4.5 in the final one.  Two launches:
+// call, the chunks' kernel 156 (5.9 TB/s).  8 rows of 32000 are latency, 11.7 us: 7
+// in the chunks' kernel (the votes' ballots one after another, the collection), 4 to 5
+// in the final one (the ranking).  Two launches:
 //   1. chunk   grid rows x chunks: statistics of a chunk and its n_top largest
 //              logits, sorted
 //   2. final   one workgroup per row: merges both

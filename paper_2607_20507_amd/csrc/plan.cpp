@@ -128,6 +128,12 @@ AttnPlan plan_attention(const std::vector<AttnSegment>& segs, int G, int Hkv, in
 
 AttnPlan plan_kv4(const std::vector<AttnSegment>& segs, int G, int Hkv, int max_parts, bool fp32) {
   AttnPlan p;
+  // The prompt form at plan_prefill's border, which the bf16 attention's kernels set
+  // (64 rows of every sequence).  Over a 4-bit cache (8b shape, prompt form / tiles,
+  // us) it is the faster one from about 2000 rows on, 8192 rows 516 / 684, 4096 142 /
+  // 194, 2048 behind 8192 keys 286 / 456, and not below, where its blocks leave CUs
+  // idle and every key is expanded for few rows: 2048 rows 69 / 65, 1000 40 / 31, 512
+  // 27 / 13, 64 18 / 12; behind 8192 keys 1000 rows 253 / 203, 64 rows 227 / 33.
   if (!fp32 && plan_prefill(segs, G, p)) return p;
   int max_rows = 1, max_keys = 0;
   for (const auto& s : segs) {
@@ -163,7 +169,10 @@ AttnPlan plan_kv4(const std::vector<AttnSegment>& segs, int G, int Hkv, int max_
     // batch has nearly as many before any split, only its longest sequences are
     // split (64 of 512 .. 4096 keys: 300 41.4 us, 256 43.8, 512 45.2; but 131000
     // keys of one sequence 44.4 us with 300, 35.2 with 512; in even parts instead of
-    // full ones and a remainder the 64 take 2 us more).
+    // full ones and a remainder the 64 take 2 us more).  Above the border, 300 / 512: 33
+    // sequences of 512 .. 4096 keys 31.9 / 34.5, 48 36.2 / 39.3; 48 of 300 .. 8000
+    // 38.9 / 37.7.  Below it uneven batches would do better with 300 too (16 of 512 ..
+    // 4096 keys 26 / 36, 24 28 / 30.4).
     const int target = p.nt >= 4 ? 256 : wgs < 256 ? 512 : 300;
     p.w = 4;
     split = (total_keys * Hkv + target - 1) / target;
