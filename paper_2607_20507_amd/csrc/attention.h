@@ -49,7 +49,7 @@ hipError_t launch_attention_bf16(const AttnArgs& a, const AttnItem* d_items, int
 // 256 / G consecutive rows of one sequence against keys 0 .. t1 - 1, t0 = 0,
 // part < 0), heaviest first; grid n_items x Hkv (kv head = block % Hkv).
 // few_keys: every item has at most kPrefillShortKeys keys.  far: scores may be
-// of any size.
+// of any size, and values that are not finite reach the rows that see them only.
 constexpr int kPrefillShortKeys = 384;
 hipError_t launch_attention_prefill_bf16(const AttnArgs& a, const AttnItem* d_items, int n_items, bool few_keys,
                                          hipStream_t st, bool far = false);
