@@ -1,8 +1,8 @@
 /*
  * spec_ops.h - single-kernel entry points of the verify step, for checking
  * each kernel on its own at full workload sizes, and operators beside it (page
- * copies; a 4-bit cache, which no context holds) for callers that run them one
- * by one.  Same conventions as spec.h:
+ * copies; a 4-bit cache and a cache of latent vectors, which no context holds)
+ * for callers that run them one by one.  Same conventions as spec.h:
  * "device" pointers are HIP device addresses, "host" pointers CPU memory,
  * stream is a hipStream_t as void*, errors are spec_status codes and the
  * caller owns every buffer.
@@ -140,6 +140,58 @@ SPEC_API spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const 
                                            int32_t head_dim, const void* q, const void* k_pages,
                                            const void* v_pages, void* out, void* workspace,
                                            size_t workspace_bytes, void* stream);
+
+/* The KV cache of a model whose attention keeps one latent vector a token, for one
+ * layer: pages (device, 16-byte aligned, dtype) [num_pages][16][rank + rope_dim],
+ * each entry the token's latent c, normed, then one rotated key that all heads
+ * share.  Head h's key is [w_k[h] c | shared key], its value w_v[h] c.
+ * nope_dim 64 or 128, rope_dim 32 or 64, rank 256 or 512, v_dim 64 or 128
+ * (SPEC_E_UNSUPPORTED otherwise), at most 65535 heads.  Page copies are
+ * spec_op_kv_copy_pages' with such pages. */
+
+/* Append: q (device fp32 [R, Hq, nope_dim + rope_dim], a head's unrotated dims
+ * first) to q_out (the same in dtype) with its last rope_dim dims rotated; kv
+ * (device fp32 [R, rank + rope_dim]) into slot[r]: the first rank values as
+ * c = x / sqrt(mean(x^2) + eps) * norm_w (norm_w: device, dtype [rank]), the rest
+ * rotated.  Pairs (i, i + rope_dim / 2) turn by pos[r] theta^(-2i / rope_dim).  pos
+ * and slot device int32 [R] (slot = page * 16 + offset); a row with a slot outside
+ * 0 .. 16 num_pages - 1 (padding: -1) has its q written and no entry.  Two rows of
+ * one call must not have one slot.  Buffers 16-byte aligned, pos and slot 4. */
+SPEC_API spec_status spec_op_rope_latent(int32_t dtype, int32_t R, int32_t n_heads, int32_t nope_dim,
+                                         int32_t rope_dim, int32_t rank, float theta, float eps, const float* q,
+                                         const float* kv, const void* norm_w, const int32_t* pos,
+                                         const int32_t* slot, int32_t num_pages, void* q_out, void* pages,
+                                         void* stream);
+
+/* Paged causal attention over a latent cache, arranged as spec_op_attention:
+ * rows[i] (may be 0) query rows of sequence i at positions pos0[i].. through row i
+ * of page_table (host int32 [n_seqs, max_pages]).  q device dtype [sum rows, Hq,
+ * nope_dim + rope_dim] as spec_op_rope_latent leaves it; w_k [Hq][nope_dim][rank]
+ * and w_v [Hq][v_dim][rank] (device, dtype, row-major; w_k_stride and w_v_stride
+ * elements from one head to the next, so both may be parts of one weight); out
+ * device dtype [sum rows, Hq * v_dim]; scale multiplies the scores (1 / sqrt(nope_dim +
+ * rope_dim) for most models).  A page id outside 0 .. num_pages - 1 is refused
+ * (SPEC_E_INVALID), as are more than 2^30 positions a sequence or rows x heads.
+ * Buffers 16-byte aligned (head strides too).
+ * Scores and sums are fp32.  bf16 rounds the queries in the latents' space, the
+ * probabilities and the sums of latents to bf16; probabilities below 2^-126 of a
+ * row's largest count as 0.  A cache entry that is not finite reaches the rows that
+ * see its key only.
+ * workspace: device, 256-byte aligned, >= spec_op_attention_latent_workspace_bytes
+ * of the same rows and positions (0 for arguments the call refuses), not shared by
+ * calls that overlap in time.  Captured calls and host arrays as
+ * spec_op_attention_kv4. */
+SPEC_API size_t spec_op_attention_latent_workspace_bytes(int32_t dtype, int32_t n_seqs, const int32_t* rows,
+                                                         const int32_t* pos0, int32_t max_pages, int32_t n_heads,
+                                                         int32_t nope_dim, int32_t rope_dim, int32_t rank,
+                                                         int32_t v_dim);
+SPEC_API spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_t* rows,
+                                              const int32_t* pos0, const int32_t* page_table, int32_t max_pages,
+                                              int32_t num_pages, int32_t n_heads, int32_t nope_dim,
+                                              int32_t rope_dim, int32_t rank, int32_t v_dim, float scale,
+                                              const void* q, const void* pages, const void* w_k,
+                                              int64_t w_k_stride, const void* w_v, int64_t w_v_stride, void* out,
+                                              void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -122,6 +122,13 @@ SIGNATURES = {
                                                          c_int32]),
     "spec_op_attention_kv4": (c_int32, [c_int32, c_int32, _P, _P, _P, c_int32, c_int32, c_int32, c_int32, c_int32,
                                         _P, _P, _P, _P, _P, c_size_t, _P]),
+    "spec_op_rope_latent": (c_int32, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_float, c_float, _P, _P, _P,
+                                      _P, _P, c_int32, _P, _P, _P]),
+    "spec_op_attention_latent_workspace_bytes": (c_size_t, [c_int32, c_int32, _P, _P, c_int32, c_int32, c_int32, c_int32,
+                                                            c_int32, c_int32]),
+    "spec_op_attention_latent": (c_int32, [c_int32, c_int32, _P, _P, _P, c_int32, c_int32, c_int32, c_int32, c_int32,
+                                           c_int32, c_int32, c_float, _P, _P, _P, c_int64, _P, c_int64, _P, _P, c_size_t,
+                                           _P]),
 }
 
 _lib = None
@@ -584,3 +591,53 @@ def spec_op_attention_kv4(dtype: int, rows, pos0, page_table, num_pages: int, n_
         _dev(q, el, n, "q", gpu), _dev(k_pages, torch.uint8, pool, "k_pages", gpu),
         _dev(v_pages, torch.uint8, pool, "v_pages", gpu), _dev(out, el, n, "out", gpu),
         _dev(workspace, None, 0, "workspace", gpu), workspace.numel() * workspace.element_size(), stream_ptr(stream)))
+
+
+def spec_op_rope_latent(dtype: int, R: int, n_heads: int, nope_dim: int, rope_dim: int, rank: int, theta: float,
+                        eps: float, q, kv, norm_w, pos, slot, num_pages: int, q_out, pages, stream=None):
+    import torch
+    gpu, el, n = torch.cuda.current_device(), _elem(dtype), R * n_heads * (nope_dim + rope_dim)
+    check(lib().spec_op_rope_latent(
+        dtype, R, n_heads, nope_dim, rope_dim, rank, theta, eps, _dev(q, torch.float32, n, "q", gpu),
+        _dev(kv, torch.float32, R * (rank + rope_dim), "kv", gpu), _dev(norm_w, el, rank, "norm_w", gpu),
+        _dev(pos, torch.int32, R, "pos", gpu), _dev(slot, torch.int32, R, "slot", gpu), num_pages,
+        _dev(q_out, el, n, "q_out", gpu), _dev(pages, el, num_pages * 16 * (rank + rope_dim), "pages", gpu),
+        stream_ptr(stream)))
+
+
+def spec_op_attention_latent_workspace_bytes(dtype: int, rows, pos0, max_pages: int, n_heads: int, nope_dim: int,
+                                             rope_dim: int, rank: int, v_dim: int) -> int:
+    r, p = _i32(rows), _i32(pos0)
+    if r.ndim != 1 or r.shape != p.shape:
+        raise ValueError("rows and pos0: one list each, of one length")
+    return lib().spec_op_attention_latent_workspace_bytes(dtype, len(r), _host(r), _host(p), max_pages, n_heads, nope_dim,
+                                                          rope_dim, rank, v_dim)
+
+
+def _head_weight(w, dtype, shape, what: str, gpu: int):
+    """Address and head stride of a weight [heads, dims, rank] whose heads are contiguous matrices."""
+    if w.get_device() != gpu:
+        raise ValueError(f"{what}: not on the current GPU")
+    if w.dtype is not dtype or tuple(w.shape) != shape or w.stride(2) != 1 or w.stride(1) != shape[2]:
+        raise ValueError(f"{what}: {dtype} {list(shape)}, each head contiguous")
+    return w.data_ptr(), w.stride(0) if shape[0] > 1 else shape[1] * shape[2]
+
+
+def spec_op_attention_latent(dtype: int, rows, pos0, page_table, num_pages: int, n_heads: int, nope_dim: int,
+                             rope_dim: int, rank: int, v_dim: int, scale: float, q, pages, w_k, w_v, out, workspace,
+                             stream=None):
+    """w_k [n_heads, nope_dim, rank] and w_v [n_heads, v_dim, rank] may be views of one weight [n_heads, nope_dim + v_dim,
+    rank]."""
+    import torch
+    r, p, pt = _i32(rows), _i32(pos0), _i32(page_table)
+    if r.ndim != 1 or r.shape != p.shape or pt.ndim != 2 or len(pt) != len(r):
+        raise ValueError("rows and pos0: one list each, page_table: one row of page ids for each sequence")
+    gpu, el, n = torch.cuda.current_device(), _elem(dtype), sum(r.tolist()) * n_heads
+    wk, wk_stride = _head_weight(w_k, el, (n_heads, nope_dim, rank), "w_k", gpu)
+    wv, wv_stride = _head_weight(w_v, el, (n_heads, v_dim, rank), "w_v", gpu)
+    check(lib().spec_op_attention_latent(
+        dtype, len(r), _host(r), _host(p), _host(pt), pt.shape[1], num_pages, n_heads, nope_dim, rope_dim, rank, v_dim,
+        scale, _dev(q, el, n * (nope_dim + rope_dim), "q", gpu),
+        _dev(pages, el, num_pages * 16 * (rank + rope_dim), "pages", gpu), wk, wk_stride, wv, wv_stride,
+        _dev(out, el, n * v_dim, "out", gpu), _dev(workspace, None, 0, "workspace", gpu),
+        workspace.numel() * workspace.element_size(), stream_ptr(stream)))

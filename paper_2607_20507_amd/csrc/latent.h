@@ -1,0 +1,77 @@
+// Attention of models that keep one latent vector and one rotated key a token:
+// its paged cache's append and the attention over it (host-side launch interface).
+//
+// A token's cache entry is [latent c (rank) | shared key (rope)], row-major in
+// pages of 16 tokens.  Head h has the key [w_k[h] c | shared key] and the value
+// w_v[h] c.  The absorbed form never makes them: it takes a query's unrotated
+// part to the latents' space first (q' = w_k[h]^T q), attends to the latents
+// themselves, and takes the sum back (out = w_v[h] o').  Every head then reads the
+// same keys and values, so that a tile's query vectors are any rows and heads of
+// one sequence: query vector row * H + head.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <vector>
+
+namespace spec {
+
+// Query vectors [qv0, qv0 + nqv) of one sequence, whose first row (of all
+// sequences' rows) is row0 at position pos0 and whose page ids start at entry
+// page0 of the page list, against its keys [t0, t1), t0 a multiple of 32.
+// part >= 0: an unnormalised partial; part < 0: the normalised output.
+struct LatentItem {
+  int32_t qv0, nqv, row0, pos0, page0, t0, t1, part;
+};
+
+// The parts of one tile's query vectors.
+struct LatentGroup {
+  int32_t qv0, nqv, part0, nparts;
+};
+
+// A sequence's rows [row0, row0 + nrows) at positions pos0.. .
+struct LatentSegment {
+  int32_t row0, nrows, pos0, page0;
+};
+
+struct LatentPlan {
+  int tile = 16;  // query vectors an item holds at most: 16, 32, 64 or 128 (fp32: 16)
+  std::vector<LatentItem> items;
+  std::vector<LatentGroup> groups;
+  int n_parts = 0;
+};
+
+// Tiles and key splits of the absorbed form; at most max_parts partials.
+LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_parts, bool fp32);
+
+struct LatentArgs {
+  int dtype;  // 0 fp32, 1 bf16 (q, pages, weights, out, q_lat, o_lat)
+  int R, H, nope, rope, rank, vdim;
+  float scale;             // of the scores, times log2 e
+  const void* q;           // [R, H, nope + rope]
+  const void* pages;       // [P][16][rank + rope]
+  const void* w_k;         // [H][nope][rank], k_stride elements between heads
+  const void* w_v;         // [H][vdim][rank], v_stride elements between heads
+  int64_t k_stride, v_stride;
+  const int32_t* page_list;
+  void* out;               // [R, H, vdim]
+  void* q_lat;             // [R, H, rank]: the queries in the latents' space
+  void* o_lat;             // [R, H, rank]: the weighted sums of latents
+  float* part_o;           // [parts][tile][rank]
+  float* part_ml;          // [parts][tile][2]: raw maximum and sum
+};
+
+// q_out [R, H, nope + rope] <- q with its rotary part rotated; the slots' entries
+// <- the normed latents and rotated keys.  Rows whose slot is outside 0 ..
+// 16 num_pages - 1 have only their q written.
+hipError_t launch_rope_latent(int dtype, int R, int H, int nope, int rope, int rank, float theta, float eps,
+                              const float* q, const float* kv, const void* norm_w, const int32_t* pos,
+                              const int32_t* slot, int num_pages, void* q_out, void* pages, hipStream_t st);
+
+hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st);
+hipError_t launch_latent_attention(const LatentArgs& a, const LatentItem* items, int n_items, int tile, hipStream_t st);
+hipError_t launch_latent_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int tile, hipStream_t st);
+hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st);
+
+}  // namespace spec

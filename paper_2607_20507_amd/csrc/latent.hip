@@ -1,0 +1,863 @@
+// Attention over a cache of latent vectors on gfx950: append, the products into
+// and out of the latents' space, and the absorbed attention between them.
+
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
+#include <type_traits>
+
+#include "common.h"
+#include "latent.h"
+
+namespace spec {
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+
+constexpr float kLatentRescaleLog2 = 8.f;
+
+// Transposed read of 16-bit values: the 16 lanes 16 n .. give, four lanes a row, the
+// addresses of 8 bytes each of a 4 x 16 block, and lane i receives its column i % 16.
+__device__ __forceinline__ uint2 read_tr(uint32_t lds) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(uintptr_t)lds));
+}
+
+__device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
+
+__device__ __forceinline__ void wave_fence() {
+  __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void block_sync() {
+  wave_fence();
+  __builtin_amdgcn_s_barrier();
+  wave_fence();
+}
+
+template <typename T>
+__device__ __forceinline__ void put4(T* p, float a, float b, float c, float d) {
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(p) = make_uint2(cvt_pk_bf16(a, b), cvt_pk_bf16(c, d));
+  else
+    *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+}
+template <typename T>
+__device__ __forceinline__ void put8(T* p, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]),
+                                              cvt_pk_bf16(v[6], v[7]));
+  } else {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+__device__ __forceinline__ void get8(const float* p, float (&v)[8]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+__device__ __forceinline__ void get8(const bf16_t* p, float (&v)[8]) {
+  const uint4 w = *reinterpret_cast<const uint4*>(p);
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(u[i] << 16), v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+}
+
+// ---------------------------------------------------------------------------
+// Append: one workgroup per row and share of the heads.  A thread's unit is 8
+// consecutive values (or 8 rotary pairs, whose halves are 8 consecutive values
+// each).  The first share's first wave norms the latent: 8 values a lane.
+
+template <typename T>
+__global__ __launch_bounds__(256) void rope_latent_kernel(int H, int nope, int rope, int rank, float theta, float eps,
+                                                          const float* __restrict__ q, const float* __restrict__ kv,
+                                                          const T* __restrict__ norm_w, const int32_t* __restrict__ pos,
+                                                          const int32_t* __restrict__ slot, uint32_t n_slots,
+                                                          T* __restrict__ q_out, T* __restrict__ pages) {
+  __shared__ float s_cos[32], s_sin[32];
+  const int r = blockIdx.x, half = rope / 2, hq = nope + rope;
+  const int h0 = static_cast<int>(static_cast<int64_t>(H) * blockIdx.y / gridDim.y);
+  const int h1 = static_cast<int>(static_cast<int64_t>(H) * (blockIdx.y + 1) / gridDim.y);
+  const float* qr = q + (static_cast<size_t>(r) * H + h0) * hq;
+  T* o = q_out + (static_cast<size_t>(r) * H + h0) * hq;
+  const uint32_t sl = static_cast<uint32_t>(slot[r]);
+  const bool kept = sl < n_slots;  // (a negative slot is large)
+  const float* x = kv + static_cast<size_t>(r) * (rank + rope);
+  T* entry = pages + static_cast<size_t>(kept ? sl : 0) * (rank + rope);
+
+  // the angles, in fp64, by the last threads
+  const int ai = static_cast<int>(threadIdx.x) - (256 - half);
+  if (ai >= 0) {
+    double sn, cs;
+    sincos(static_cast<double>(pos[r]) * exp(-(2.0 * ai / rope) * log(static_cast<double>(theta))), &sn, &cs);
+    s_cos[ai] = static_cast<float>(cs);
+    s_sin[ai] = static_cast<float>(sn);
+  }
+  if (blockIdx.y == 0 && threadIdx.x < kWave && kept) {
+    const int e = 8 * static_cast<int>(threadIdx.x);
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, w[8], ss = 0.f;
+    if (e < rank) {
+      get8(x + e, v);
+      get8(norm_w + e, w);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss = fmaf(v[j], v[j], ss);
+    const float inv = 1.f / sqrtf(wave_sum(ss) / static_cast<float>(rank) + eps);
+    if (e < rank) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = v[j] * inv * w[j];
+      put8(entry + e, v);
+    }
+  }
+  // the unrotated part
+  const int un = nope / 8;
+  for (int e = threadIdx.x; e < (h1 - h0) * un; e += 256) {
+    const int at = e / un * hq + e % un * 8;
+    float v[8];
+    get8(qr + at, v);
+    put8(o + at, v);
+  }
+  __syncthreads();
+  // the rotated one, and the shared key as one more head
+  const int ur = half / 8, own = blockIdx.y == 0 && kept ? 1 : 0;
+  for (int e = threadIdx.x; e < (h1 - h0 + own) * ur; e += 256) {
+    const int h = e / ur, i0 = e % ur * 8;
+    const bool key = h == h1 - h0;
+    const float* src = key ? x + rank : qr + h * hq + nope;
+    T* dst = key ? entry + rank : o + h * hq + nope;
+    float a[8], b[8], ra[8], rb[8];
+    get8(src + i0, a);
+    get8(src + half + i0, b);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float c = s_cos[i0 + j], sn = s_sin[i0 + j];
+      ra[j] = a[j] * c - b[j] * sn;
+      rb[j] = b[j] * c + a[j] * sn;
+    }
+    put8(dst + i0, ra);
+    put8(dst + half + i0, rb);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Queries into the latents' space: q' [row, h, c] = sum_n q[row, h, n] w_k[h, n, c].
+// A workgroup holds w_k's columns 64 cb .. of one head, one wave 16 of them as MFMA
+// operands for all of its rows.
+
+template <int NOPE>
+__global__ __launch_bounds__(256) void latent_absorb_bf16_kernel(LatentArgs a) {
+  constexpr int KS = NOPE / 32;
+  __shared__ uint4 sw[NOPE * 8];
+  const int blocks = a.rank / 64;
+  const int h = blockIdx.x / blocks, c0 = blockIdx.x % blocks * 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
+  const bf16_t* w = static_cast<const bf16_t*>(a.w_k) + static_cast<int64_t>(h) * a.k_stride + c0;
+  // row n's 16-byte chunks c at c ^ f(n): reads of four rows' 32 bytes, and writes, take every bank
+  auto f = [](int n) { return (n & 3) << 1 | (n >> 2 & 1); };
+#pragma unroll
+  for (int i = 0; i < NOPE * 8 / 256; ++i) {
+    const int u = i * 256 + threadIdx.x, n = u >> 3, c = u & 7;
+    sw[n * 8 + (c ^ f(n))] = *reinterpret_cast<const uint4*>(w + static_cast<size_t>(n) * a.rank + 8 * c);
+  }
+  __syncthreads();
+  uint4 wf[KS];
+  const uint32_t base = lds_addr(sw);
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    uint2 p[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int n = 32 * s + 8 * g + 4 * t + (l16 >> 2), c = 2 * wave + (l16 >> 1 & 1);
+      p[t] = read_tr(base + (n * 8 + (c ^ f(n))) * 16 + (l16 & 1) * 8);
+    }
+    wf[s] = make_uint4(p[0].x, p[0].y, p[1].x, p[1].y);
+  }
+  const bf16_t* q = static_cast<const bf16_t*>(a.q);
+  bf16_t* to = static_cast<bf16_t*>(a.q_lat);
+  const int hq = NOPE + a.rope;
+  for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += 16 * gridDim.y) {
+    const int r = r0 + l16;
+    const size_t qv = static_cast<size_t>(min(r, a.R - 1)) * a.H + h;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    uint4 qf[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const uint4*>(q + qv * hq + 32 * s + 8 * g);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) acc = mfma16x16x32(wf[s], qf[s], acc);
+    if (r < a.R) put4(to + qv * a.rank + c0 + 16 * wave + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+  }
+}
+
+template <int NOPE>
+__global__ __launch_bounds__(256) void latent_absorb_f32_kernel(LatentArgs a) {
+  constexpr int J = NOPE / 16;
+  const int blocks = a.rank / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
+  const int h = blockIdx.x / blocks, c0 = blockIdx.x % blocks * 64 + 16 * wave;
+  const float* w = static_cast<const float*>(a.w_k) + static_cast<int64_t>(h) * a.k_stride + c0 + l16;
+  // step (j, i) takes n = 16 j + 4 g + i in lane group g, so that a lane's q are float4s
+  float wf[J][4];
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) wf[j][i] = w[static_cast<size_t>(16 * j + 4 * g + i) * a.rank];
+  const float* q = static_cast<const float*>(a.q);
+  float* to = static_cast<float*>(a.q_lat);
+  const int hq = NOPE + a.rope;
+  for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += 16 * gridDim.y) {
+    const int r = r0 + l16;
+    const size_t qv = static_cast<size_t>(min(r, a.R - 1)) * a.H + h;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    f32x4 qf[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) qf[j] = *reinterpret_cast<const f32x4*>(q + qv * hq + 16 * j + 4 * g);
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc = mfma_f32(wf[j][i], qf[j][i], acc);
+    if (r < a.R) put4(to + qv * a.rank + c0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Sums of latents to values: out[row, h, d] = sum_c o'[row, h, c] w_v[h, d, c].  A
+// workgroup makes 16 dims of one head, its four waves a quarter of the sum each.
+
+template <int RANK>
+__global__ __launch_bounds__(256) void latent_values_bf16_kernel(LatentArgs a) {
+  constexpr int KS = RANK / 128;
+  __shared__ f32x4 part[4][64];
+  const int tiles = a.vdim / 16;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
+  const int h = blockIdx.x / tiles, d0 = blockIdx.x % tiles * 16;
+  const int c0 = wave * (RANK / 4) + 8 * g;
+  const bf16_t* w = static_cast<const bf16_t*>(a.w_v) + static_cast<int64_t>(h) * a.v_stride +
+                    static_cast<size_t>(d0 + l16) * RANK + c0;
+  uint4 wf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) wf[s] = *reinterpret_cast<const uint4*>(w + 32 * s);
+  const bf16_t* o = static_cast<const bf16_t*>(a.o_lat);
+  bf16_t* out = static_cast<bf16_t*>(a.out);
+  for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += 16 * gridDim.y) {
+    const int r = r0 + l16;
+    const size_t qv = static_cast<size_t>(min(r, a.R - 1)) * a.H + h;
+    uint4 of[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) of[s] = *reinterpret_cast<const uint4*>(o + qv * RANK + c0 + 32 * s);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) acc = mfma16x16x32(wf[s], of[s], acc);
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (wave == 0 && r < a.R) {
+      acc = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+      put4(out + qv * a.vdim + d0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+    }
+    __syncthreads();
+  }
+}
+
+template <int RANK>
+__global__ __launch_bounds__(256) void latent_values_f32_kernel(LatentArgs a) {
+  constexpr int J = RANK / 64;
+  __shared__ f32x4 part[4][64];
+  const int tiles = a.vdim / 16;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
+  const int h = blockIdx.x / tiles, d0 = blockIdx.x % tiles * 16;
+  const int c0 = wave * (RANK / 4) + 4 * g;
+  const float* w = static_cast<const float*>(a.w_v) + static_cast<int64_t>(h) * a.v_stride +
+                   static_cast<size_t>(d0 + l16) * RANK + c0;
+  f32x4 wf[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) wf[j] = *reinterpret_cast<const f32x4*>(w + 16 * j);
+  const float* o = static_cast<const float*>(a.o_lat);
+  float* out = static_cast<float*>(a.out);
+  for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += 16 * gridDim.y) {
+    const int r = r0 + l16;
+    const size_t qv = static_cast<size_t>(min(r, a.R - 1)) * a.H + h;
+    f32x4 of[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) of[j] = *reinterpret_cast<const f32x4*>(o + qv * RANK + c0 + 16 * j);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc = mfma_f32(wf[j][i], of[j][i], acc);
+    part[wave][lane] = acc;
+    __syncthreads();
+    if (wave == 0 && r < a.R) {
+      acc = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+      put4(out + qv * a.vdim + d0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Joining a wave's or a part's state (raw maximum m, sum l, unnormalised o) with
+// others': weight 2^((m - max m) scale).  A state that saw no key has m = -FLT_MAX
+// and l = 0.  What is not finite stays so: a NaN anywhere, or a maximum of +inf,
+// makes the row NaN; a row whose every score is -inf has l = 0 and becomes 0 / 0.
+
+__device__ __forceinline__ float join_weight(float m, float top, float scale) {
+  return __builtin_amdgcn_exp2f((m - top) * scale);
+}
+
+// The waves' states, in LDS as [WK][Q][RANK + 4] and [WK][Q][2], to the item's output.
+template <typename T, int RANK, int WK, int Q>
+__device__ __forceinline__ void join_waves(const LatentArgs& a, const LatentItem& it, const float* so, const float* sml,
+                                           int tile) {
+  constexpr int U = RANK / 4;
+  for (int u = threadIdx.x; u < Q * U; u += 256) {
+    const int m = u / U, c = u % U * 4;
+    if (m >= it.nqv) break;
+    float top = sml[2 * m];
+#pragma unroll
+    for (int k = 1; k < WK; ++k) top = fmaxf(top, sml[2 * (k * Q + m)]);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+#pragma unroll
+    for (int k = 0; k < WK; ++k) {
+      const float w = join_weight(sml[2 * (k * Q + m)], top, a.scale);
+      l += w * sml[2 * (k * Q + m) + 1];
+      o += w * *reinterpret_cast<const f32x4*>(so + (k * Q + m) * (RANK + 4) + c);
+    }
+    if (it.part < 0) {
+      const float inv = 1.f / l;
+      put4(static_cast<T*>(a.o_lat) + static_cast<size_t>(it.qv0 + m) * RANK + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    } else {
+      const size_t pv = static_cast<size_t>(it.part) * tile + m;
+      *reinterpret_cast<f32x4*>(a.part_o + pv * RANK + c) = o;
+      if (c == 0) {
+        a.part_ml[2 * pv] = top;
+        a.part_ml[2 * pv + 1] = l;
+      }
+    }
+  }
+}
+
+// One workgroup per query vector of a group: four values a thread.
+template <typename T, int RANK>
+__global__ __launch_bounds__(RANK / 4) void latent_combine_kernel(LatentArgs a, const LatentGroup* __restrict__ groups,
+                                                                  int tile) {
+  const LatentGroup gr = groups[blockIdx.x / tile];
+  const int m = blockIdx.x % tile, c = 4 * threadIdx.x;
+  if (m >= gr.nqv) return;
+  const float* ml = a.part_ml + 2 * (static_cast<size_t>(gr.part0) * tile + m);
+  const float* po = a.part_o + (static_cast<size_t>(gr.part0) * tile + m) * RANK + c;
+  float top = ml[0];
+  for (int p = 1; p < gr.nparts; ++p) top = fmaxf(top, ml[static_cast<size_t>(2) * tile * p]);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  constexpr int B = 8;
+  for (int p0 = 0; p0 < gr.nparts; p0 += B) {
+    f32x4 v[B];
+    float m2[B], l2[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const size_t p = min(p0 + b, gr.nparts - 1);
+      v[b] = *reinterpret_cast<const f32x4*>(po + p * tile * RANK);
+      m2[b] = ml[2 * tile * p];
+      l2[b] = ml[2 * tile * p + 1];
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      if (p0 + b >= gr.nparts) break;
+      const float w = join_weight(m2[b], top, a.scale);
+      l += w * l2[b];
+      o += w * v[b];
+    }
+  }
+  const float inv = 1.f / l;
+  put4(static_cast<T*>(a.o_lat) + static_cast<size_t>(gr.qv0 + m) * RANK + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+}
+
+// ---------------------------------------------------------------------------
+// Absorbed attention, bf16.  A workgroup holds 16 NT WQ query vectors of one
+// sequence; its four waves are WQ shares of them times WK shares of the keys.  32
+// keys at a time go to LDS (direct loads of their two pages), where the waves of a
+// share read them twice: as rows for S^T = C Q'^T (A = 16 keys x 32 dims), and
+// transposed for O'^T = C^T P^T (A = 16 dims x 32 keys).  The transposed reads take
+// the keys in the order in which a lane's score accumulators hold them, so the
+// probabilities go from one product to the other in registers.
+// Chunks of 16 bytes of token t's latent sit at c ^ f(t): the 8 lanes of a row read
+// (8 tokens, one chunk) and the 16 of a transposed one (4 tokens, two chunks) take
+// every bank once.
+// The running maximum (of raw scores) is raised only when a score exceeds it by more
+// than 2^8; differences are taken before the scale, so scores of any size keep theirs.
+// A key that some row of the wave does not see may hold a value that is not finite
+// (a slot past the sequence anything at all).  Its scores are not finite then, which
+// sends the wave through a form that drops such values from the second product and
+// gives the rows that see the key a NaN score.
+
+template <int RANK, int ROPE, int NT, int WQ, int WK>
+__global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, const LatentItem* __restrict__ items) {
+  constexpr int CL = RANK / 8, CR = ROPE / 8;    // 16-byte chunks of a token's latent and key
+  constexpr int DL = RANK / 32, DR = ROPE / 32;  // k-steps of the scores
+  constexpr int DT = RANK / 16;                  // 16-dim output tiles
+  constexpr int NB = WK == 4 ? 1 : 2;            // chunk buffers of a key share
+  constexpr int BU = 32 * (CL + CR);             // units of one
+  constexpr int Q = 16 * NT * WQ;
+  constexpr int TP = 64 / CL, RT = 64 / CR;      // tokens a load covers: latents, keys
+  constexpr int NLL = 32 / TP, NL = NLL + 32 / RT;
+  constexpr int kJoin = WK > 1 ? WK * Q * (RANK + 4) * 4 / 16 : 0;
+  constexpr int kUnits = WK * NB * BU > kJoin ? WK * NB * BU : kJoin;
+  static_assert(WQ * WK == 4 && (WK == 1 || NT == 1));
+  __shared__ uint4 buf[kUnits];
+  __shared__ float s_ml[WK > 1 ? 2 * WK * Q : 1];
+  const LatentItem it = items[blockIdx.x];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wq = wave % WQ, wk = wave / WQ;
+  const int g = lane >> 4, l16 = lane & 15;
+  const char* pool = static_cast<const char*>(a.pages);
+  const int32_t* list = a.page_list + it.page0;
+  const int np = (it.t1 + 15) >> 4;
+  const int c0 = it.t0 >> 5, nch = (it.t1 - it.t0 + 31) >> 5;
+  const int nit = (nch + WK - 1) / WK;
+  auto f = [](int t) { return (t & 3) << 1 | (t >> 2 & 1); };
+  auto fr = [&](int t) { return CR == 8 ? f(t) : t >> 1 & 3; };
+
+  // the wave's loads of chunk c into buffer b
+  auto issue = [&](int c, int b) {
+    size_t page[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      page[i] = static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(list[min(2 * c + i, np - 1)])));
+    const uint32_t dst = lds_addr(&buf[(wk * NB + b) * BU]);
+#pragma unroll
+    for (int j = 0; j < (NL + WQ - 1) / WQ; ++j) {
+      const int i = WQ * j + wq;
+      if (i >= NL) break;
+      const bool key = i >= NLL;
+      const int first = key ? (i - NLL) * RT : i * TP;
+      const int t = key ? first + lane / CR : first + lane / CL;
+      const int ch = key ? CL + (lane % CR ^ fr(t)) : lane % CL ^ f(t);
+      const char* base = pool + (first >> 4 ? page[1] : page[0]) * (16 * (CL + CR) * 16);
+      load_lds16(base, ((t & 15) * (CL + CR) + ch) * 16, dst + i * 1024);
+    }
+  };
+
+  // query vectors
+  uint4 qf[NT][DL + DR];
+  int klim[NT];  // the last key each sees (-1: none, a padding vector)
+  float mneg[NT], mlim[NT], lrun[NT][2];
+  f32x4 acc[DT][NT];
+  const int m0 = 16 * NT * wq;
+  auto pos_of = [&](int m) { return it.pos0 + (it.qv0 + m) / a.H - it.row0; };
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int m = m0 + 16 * nt + l16;
+    const bool ok = m < it.nqv;
+    klim[nt] = ok ? min(pos_of(m), it.t1 - 1) : -1;
+    const size_t qv = static_cast<size_t>(it.qv0 + (ok ? m : 0));
+    const bf16_t* ql = static_cast<const bf16_t*>(a.q_lat) + qv * RANK + 8 * g;
+    const bf16_t* qr = static_cast<const bf16_t*>(a.q) + qv * (a.nope + ROPE) + a.nope + 8 * g;
+#pragma unroll
+    for (int s = 0; s < DL + DR; ++s)
+      qf[nt][s] = ok ? *reinterpret_cast<const uint4*>(s < DL ? ql + 32 * s : qr + 32 * (s - DL)) : make_uint4(0, 0, 0, 0);
+    mneg[nt] = FLT_MAX;
+    mlim[nt] = -INFINITY;
+    lrun[nt][0] = lrun[nt][1] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const bool active = m0 < it.nqv;
+  const int pos_lo = active ? pos_of(m0) : -1;
+  const int pos_hi = active ? min(pos_of(min(m0 + 16 * NT, it.nqv) - 1), it.t1 - 1) : -1;
+
+  // lane constants of the reads
+  const int fk = f(l16);
+  const int k_off0 = l16 * CL + (g ^ fk), k_off1 = l16 * CL + ((4 + g) ^ fk);
+  const int fv = (l16 >> 2) << 1 | (g & 1);
+  uint32_t v_off[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    v_off[i] = (4 * g + (l16 >> 2)) * (RANK * 2) + ((2 * i + (l16 >> 1 & 1)) ^ fv) * 16 + (l16 & 1) * 8;
+
+  auto chunk = [&](int c, int b) {
+    const uint4* kb = &buf[(wk * NB + b) * BU];
+    const uint4* rb = kb + 32 * CL;
+    const uint32_t vb = lds_addr(kb);
+    const int t0 = 32 * c;
+    auto read_v = [&](int dt) {
+      const uint32_t at = vb + v_off[dt & 3] + (dt >> 2) * 128;
+      const uint2 x = read_tr(at), y = read_tr(at + 16 * RANK * 2);
+      return make_uint4(x.x, x.y, y.x, y.y);
+    };
+    f32x4 sc[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < DL + DR; ++s)
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        uint4 k;
+        if (s < DL) k = kb[16 * hh * CL + (s & 1 ? k_off1 : k_off0) + 8 * (s >> 1)];
+        else if (CR == 8) k = rb[(16 * hh + l16) * 8 + ((4 * (s - DL) + g) ^ fk)];
+        else k = rb[(16 * hh + l16) * 4 + (g ^ (l16 >> 1 & 3))];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sc[nt][hh] = mfma16x16x32(k, qf[nt][s], sc[nt][hh]);
+      }
+    bool bad = false;
+    if (t0 + 31 > pos_lo || t0 + 31 >= it.t1) {  // some key that some row does not see
+      asm volatile("");
+      bool odd = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) odd |= !finite(sc[nt][j / 4][j % 4]);
+      bad = __any(odd);
+      uint32_t flags = 0;  // of the lane's 8 keys: a latent that is not finite
+      if (bad) {
+#pragma unroll 1
+        for (int i = 0; i < DT / 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t at = vb + v_off[j] + i * 128;
+            const uint2 x = read_tr(at), y = read_tr(at + 16 * RANK * 2);
+            const uint32_t w[4] = {x.x, x.y, y.x, y.y};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t n = nonfinite_bits(w[e]);
+              flags |= (n >> 15 & 1u) << (2 * e) | (n >> 31) << (2 * e + 1);
+            }
+          }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) flags |= __shfl_xor(flags, o, kWave);
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (t0 + 16 * (j / 4) + 4 * g + j % 4 > klim[nt]) sc[nt][j / 4][j % 4] = -INFINITY;
+          else if (flags >> j & 1) sc[nt][j / 4][j % 4] = __builtin_nanf("");
+        }
+    }
+    float mx[NT];
+    bool raise = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      mx[nt] = sc[nt][0][0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) mx[nt] = fmaxf(mx[nt], sc[nt][j / 4][j % 4]);
+      raise |= mx[nt] > mlim[nt];
+    }
+    if (__any(raise)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float m = mx[nt];
+        m = fmaxf(m, __shfl_xor(m, 16, kWave));
+        m = fmaxf(m, __shfl_xor(m, 32, kWave));
+        if (m > mlim[nt]) {
+          const float alpha = __builtin_amdgcn_exp2f((-mneg[nt] - m) * a.scale);
+          mneg[nt] = -m;
+          mlim[nt] = m + kLatentRescaleLog2 / a.scale;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) lrun[nt][i] *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= alpha;
+        }
+      }
+    }
+    uint4 pf[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float p[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f((sc[nt][j / 4][j % 4] + mneg[nt]) * a.scale);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) lrun[nt][j % 2] += p[j];
+      // bf16, as the values that it weights: its rounding stays below the output's
+      pf[nt] = make_uint4(cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7]));
+    }
+    if (bad) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint4 v = drop_nonfinite(read_v(dt));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[dt][nt] = mfma16x16x32(v, pf[nt], acc[dt][nt]);
+      }
+    } else {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint4 v = read_v(dt);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[dt][nt] = mfma16x16x32(v, pf[nt], acc[dt][nt]);
+      }
+    }
+  };
+
+  if (NB == 2 && wk < nch) issue(c0 + wk, 0);
+  for (int j = 0; j < nit; ++j) {
+    const int i = j * WK + wk, c = c0 + i;
+    if (NB == 2) {
+      SPEC_WAIT_VM_LDS(0);
+      block_sync();  // chunk j has landed, and every wave is done with the one before
+      if (i + WK < nch) issue(c + WK, (j + 1) & 1);
+    } else {  // a buffer of the wave's own
+      SPEC_WAIT_VM_LDS(0);
+      wave_fence();
+      if (i < nch) issue(c, 0);
+      SPEC_WAIT_VM_LDS(0);
+      wave_fence();
+    }
+    if (i < nch && 32 * c <= pos_hi) chunk(c, NB == 2 ? j & 1 : 0);
+  }
+
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float l = lrun[nt][0] + lrun[nt][1];
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    const int m = m0 + 16 * nt + l16;
+    if constexpr (WK == 1) {
+      if (m >= it.nqv) continue;
+      if (it.part < 0) {
+        const float inv = 1.f / l;
+        bf16_t* o = static_cast<bf16_t*>(a.o_lat) + static_cast<size_t>(it.qv0 + m) * RANK + 4 * g;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const f32x4 v = acc[dt][nt] * inv;
+          put4(o + 16 * dt, v[0], v[1], v[2], v[3]);
+        }
+      } else {
+        const size_t pv = static_cast<size_t>(it.part) * Q + m;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(a.part_o + pv * RANK + 16 * dt + 4 * g) = acc[dt][nt];
+        if (g == 0) {
+          a.part_ml[2 * pv] = -mneg[nt];
+          a.part_ml[2 * pv + 1] = l;
+        }
+      }
+    } else {
+      __syncthreads();  // every wave is done with its keys
+      float* so = reinterpret_cast<float*>(buf);
+      const int at = wk * Q + m;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(so + at * (RANK + 4) + 16 * dt + 4 * g) = acc[dt][nt];
+      if (g == 0) {
+        s_ml[2 * at] = -mneg[nt];
+        s_ml[2 * at + 1] = l;
+      }
+    }
+  }
+  if constexpr (WK > 1) {
+    __syncthreads();
+    join_waves<bf16_t, RANK, WK, Q>(a, it, reinterpret_cast<const float*>(buf), s_ml, Q);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Absorbed attention, fp32: 16 query vectors a workgroup, whose four waves take its
+// pages in turn.  fp32 MFMA throughout (16 x 16 x 4), operands straight from the
+// cache: k-step (j, i) of the scores takes dim 16 j + 4 g + i in lane group g, and
+// output tile (j, t) holds dims 64 j + 4 row + t, so that every load is 16 bytes a
+// lane and a lane's scores are the probabilities it supplies.
+
+template <int RANK, int ROPE>
+__global__ __launch_bounds__(256, 1) void attn_latent_f32_kernel(LatentArgs a, const LatentItem* __restrict__ items) {
+  constexpr int D = RANK + ROPE, J = D / 16, JV = RANK / 64;
+  constexpr int WK = 4, Q = 16;
+  __shared__ float so[WK * Q * (RANK + 4)];
+  __shared__ float s_ml[2 * WK * Q];
+  const LatentItem it = items[blockIdx.x];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, l16 = lane & 15;
+  const float* pool = static_cast<const float*>(a.pages);
+  const int32_t* list = a.page_list + it.page0;
+  const bool ok = l16 < it.nqv;
+  const size_t qv = static_cast<size_t>(it.qv0 + (ok ? l16 : 0));
+  auto pos_of = [&](int m) { return it.pos0 + (it.qv0 + m) / a.H - it.row0; };
+  const int klim = ok ? min(pos_of(l16), it.t1 - 1) : -1;
+  const int pos_lo = pos_of(0), pos_hi = min(pos_of(it.nqv - 1), it.t1 - 1);
+  f32x4 qf[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const float* src = 16 * j < RANK ? static_cast<const float*>(a.q_lat) + qv * RANK + 16 * j
+                                     : static_cast<const float*>(a.q) + qv * (a.nope + ROPE) + a.nope + 16 * j - RANK;
+    qf[j] = ok ? *reinterpret_cast<const f32x4*>(src + 4 * g) : f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  float mneg = FLT_MAX, mlim = -INFINITY, lrun = 0.f;
+  f32x4 acc[4 * JV];
+#pragma unroll
+  for (int i = 0; i < 4 * JV; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  for (int t0 = it.t0 + 16 * wave; t0 <= pos_hi; t0 += 16 * WK) {
+    const float* page = pool + static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(list[t0 >> 4]))) * (16 * D);
+    f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const f32x4 k = *reinterpret_cast<const f32x4*>(page + l16 * D + 16 * j + 4 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc[i & 1] = mfma_f32(k[i], qf[j][i], sc[i & 1]);
+    }
+    f32x4 s = sc[0] + sc[1];
+    const float* vrow = page + 4 * g * D + 4 * l16;  // keys 4 g + i
+    bool bad = false;
+    if (t0 + 15 > pos_lo || t0 + 15 >= it.t1) {
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) odd |= !finite(s[i]);
+      bad = __any(odd);
+      uint32_t flags = 0;
+      if (bad) {
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i)
+#pragma unroll 1
+          for (int j = 0; j < JV; ++j) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(vrow + i * D + 64 * j);
+            if (!(finite(v[0]) && finite(v[1]) && finite(v[2]) && finite(v[3]))) flags |= 1u << i;
+          }
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) flags |= __shfl_xor(flags, o, kWave);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (t0 + 4 * g + i > klim) s[i] = -INFINITY;
+        else if (flags >> i & 1) s[i] = __builtin_nanf("");
+      }
+    }
+    float m = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+    if (__any(m > mlim)) {
+      m = fmaxf(m, __shfl_xor(m, 16, kWave));
+      m = fmaxf(m, __shfl_xor(m, 32, kWave));
+      if (m > mlim) {
+        const float alpha = __builtin_amdgcn_exp2f((-mneg - m) * a.scale);
+        mneg = -m;
+        mlim = m + kLatentRescaleLog2 / a.scale;
+        lrun *= alpha;
+#pragma unroll
+        for (int i = 0; i < 4 * JV; ++i) acc[i] *= alpha;
+      }
+    }
+    f32x4 p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      p[i] = __builtin_amdgcn_exp2f((s[i] + mneg) * a.scale);
+      lrun += p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < JV; ++j) {
+        f32x4 v = *reinterpret_cast<const f32x4*>(vrow + i * D + 64 * j);
+        if (bad) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) v[t] = finite(v[t]) ? v[t] : 0.f;
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[4 * j + t] = mfma_f32(v[t], p[i], acc[4 * j + t]);
+      }
+  }
+  lrun += __shfl_xor(lrun, 16, kWave);
+  lrun += __shfl_xor(lrun, 32, kWave);
+  const int at = wave * Q + l16;
+#pragma unroll
+  for (int j = 0; j < JV; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      *reinterpret_cast<f32x4*>(so + at * (RANK + 4) + 64 * j + 16 * g + 4 * r) =
+          f32x4{acc[4 * j][r], acc[4 * j + 1][r], acc[4 * j + 2][r], acc[4 * j + 3][r]};
+  if (g == 0) {
+    s_ml[2 * at] = -mneg;
+    s_ml[2 * at + 1] = lrun;
+  }
+  __syncthreads();
+  join_waves<float, RANK, WK, Q>(a, it, so, s_ml, Q);
+}
+
+template <int RANK, int ROPE>
+hipError_t launch_attention(const LatentArgs& a, const LatentItem* items, int n, int tile, hipStream_t st) {
+  if (a.dtype == 0) {
+    if (tile != 16) return hipErrorInvalidValue;
+    launch_kernel(attn_latent_f32_kernel<RANK, ROPE>, dim3(n), dim3(256), 0, st, a, items);
+  } else if (tile == 16) {
+    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 1, 1, 4>, dim3(n), dim3(256), 0, st, a, items);
+  } else if (tile == 32) {
+    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 1, 2, 2>, dim3(n), dim3(256), 0, st, a, items);
+  } else if (tile == 64) {
+    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 1, 4, 1>, dim3(n), dim3(256), 0, st, a, items);
+  } else if (tile == 128) {
+    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 2, 4, 1>, dim3(n), dim3(256), 0, st, a, items);
+  } else {
+    return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
+}
+
+// Row blocks of the two products: at most about 1024 workgroups.
+unsigned row_blocks(int R, unsigned columns) {
+  const unsigned tiles = (static_cast<unsigned>(R) + 15) / 16;
+  return std::max(1u, std::min(tiles, 1024 / std::max(1u, columns)));
+}
+
+}  // namespace
+
+hipError_t launch_rope_latent(int dtype, int R, int H, int nope, int rope, int rank, float theta, float eps,
+                              const float* q, const float* kv, const void* norm_w, const int32_t* pos,
+                              const int32_t* slot, int num_pages, void* q_out, void* pages, hipStream_t st) {
+  if (R <= 0) return hipSuccess;
+  if (static_cast<size_t>(R) > kMaxGrid256) return hipErrorInvalidValue;
+  // a row's heads are shared out while that fills the chip
+  int shares = std::max(1, std::min(H / 4, 512 / R));
+  const dim3 grid(R, shares);
+  const uint32_t n_slots = 16u * static_cast<uint32_t>(num_pages);
+  if (dtype == 0)
+    launch_kernel(rope_latent_kernel<float>, grid, dim3(256), 0, st, H, nope, rope, rank, theta, eps, q, kv,
+                  static_cast<const float*>(norm_w), pos, slot, n_slots, static_cast<float*>(q_out), static_cast<float*>(pages));
+  else
+    launch_kernel(rope_latent_kernel<bf16_t>, grid, dim3(256), 0, st, H, nope, rope, rank, theta, eps, q, kv,
+                  static_cast<const bf16_t*>(norm_w), pos, slot, n_slots, static_cast<bf16_t*>(q_out), static_cast<bf16_t*>(pages));
+  return hipGetLastError();
+}
+
+hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st) {
+  const unsigned columns = static_cast<unsigned>(a.H) * (a.rank / 64);
+  const dim3 grid(columns, row_blocks(a.R, columns));
+  if (a.nope == 64 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<64>, grid, dim3(256), 0, st, a);
+  else if (a.nope == 128 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<128>, grid, dim3(256), 0, st, a);
+  else if (a.nope == 64) launch_kernel(latent_absorb_bf16_kernel<64>, grid, dim3(256), 0, st, a);
+  else if (a.nope == 128) launch_kernel(latent_absorb_bf16_kernel<128>, grid, dim3(256), 0, st, a);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st) {
+  const unsigned columns = static_cast<unsigned>(a.H) * (a.vdim / 16);
+  const dim3 grid(columns, row_blocks(a.R, columns));
+  if (a.rank == 256 && a.dtype == 0) launch_kernel(latent_values_f32_kernel<256>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 512 && a.dtype == 0) launch_kernel(latent_values_f32_kernel<512>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 256) launch_kernel(latent_values_bf16_kernel<256>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 512) launch_kernel(latent_values_bf16_kernel<512>, grid, dim3(256), 0, st, a);
+  else return hipErrorInvalidValue;
+  return hipGetLastError();
+}
+
+hipError_t launch_latent_attention(const LatentArgs& a, const LatentItem* items, int n_items, int tile, hipStream_t st) {
+  if (n_items <= 0) return hipSuccess;
+  if (static_cast<size_t>(n_items) > kMaxGrid256) return hipErrorInvalidValue;
+  if (a.rank == 512 && a.rope == 64) return launch_attention<512, 64>(a, items, n_items, tile, st);
+  if (a.rank == 512 && a.rope == 32) return launch_attention<512, 32>(a, items, n_items, tile, st);
+  if (a.rank == 256 && a.rope == 64) return launch_attention<256, 64>(a, items, n_items, tile, st);
+  if (a.rank == 256 && a.rope == 32) return launch_attention<256, 32>(a, items, n_items, tile, st);
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_latent_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int tile, hipStream_t st) {
+  if (n_groups <= 0) return hipSuccess;
+  if (static_cast<size_t>(n_groups) * tile > kMaxGrid256) return hipErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>(n_groups) * tile);
+  if (a.dtype == 0 && a.rank == 512) launch_kernel(latent_combine_kernel<float, 512>, grid, dim3(128), 0, st, a, groups, tile);
+  else if (a.dtype == 0) launch_kernel(latent_combine_kernel<float, 256>, grid, dim3(64), 0, st, a, groups, tile);
+  else if (a.rank == 512) launch_kernel(latent_combine_kernel<bf16_t, 512>, grid, dim3(128), 0, st, a, groups, tile);
+  else launch_kernel(latent_combine_kernel<bf16_t, 256>, grid, dim3(64), 0, st, a, groups, tile);
+  return hipGetLastError();
+}
+
+}  // namespace spec

@@ -1,0 +1,55 @@
+// Work of the attention over a latent cache: query tiles and key splits.
+
+#include <algorithm>
+
+#include "latent.h"
+
+namespace spec {
+
+LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_parts, bool fp32) {
+  LatentPlan p;
+  int64_t most = 1;
+  for (const LatentSegment& s : segs) most = std::max<int64_t>(most, static_cast<int64_t>(s.nrows) * H);
+  p.tile = fp32 || most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 128;
+  struct Tile {
+    int32_t qv0, nqv, row0, pos0, page0, kend;
+  };
+  std::vector<Tile> tiles;
+  int64_t keys = 0;
+  for (const LatentSegment& s : segs) {
+    const int64_t first = static_cast<int64_t>(s.row0) * H, n = static_cast<int64_t>(s.nrows) * H;
+    for (int64_t m = 0; m < n; m += p.tile) {
+      const int64_t c = std::min<int64_t>(p.tile, n - m);
+      const int kend = static_cast<int>(s.pos0 + (m + c - 1) / H + 1);  // keys 0 .. its last row's position
+      tiles.push_back(Tile{static_cast<int32_t>(first + m), static_cast<int32_t>(c), s.row0, s.pos0, s.page0, kend});
+      keys += kend;
+    }
+  }
+  const int target = 256;
+  int64_t split = std::max<int64_t>(128, (keys + target - 1) / target);
+  split = (split + 31) / 32 * 32;
+  auto parts = [&](int64_t sp) {
+    int64_t n = 0;
+    for (const Tile& t : tiles) n += t.kend > sp ? (t.kend + sp - 1) / sp : 0;
+    return n;
+  };
+  while (parts(split) > max_parts) split *= 2;
+  for (const Tile& t : tiles) {
+    const int c = static_cast<int>((t.kend + split - 1) / split);
+    if (c <= 1) {
+      p.items.push_back(LatentItem{t.qv0, t.nqv, t.row0, t.pos0, t.page0, 0, t.kend, -1});
+      continue;
+    }
+    p.groups.push_back(LatentGroup{t.qv0, t.nqv, p.n_parts, c});
+    for (int i = 0; i < c; ++i)
+      p.items.push_back(LatentItem{t.qv0, t.nqv, t.row0, t.pos0, t.page0, static_cast<int32_t>(i * split),
+                                   static_cast<int32_t>(std::min<int64_t>(t.kend, (i + 1) * split)), p.n_parts + i});
+    p.n_parts += c;
+  }
+  // longest key ranges first, so that the short ones fill in behind them
+  std::stable_sort(p.items.begin(), p.items.end(),
+                   [](const LatentItem& x, const LatentItem& y) { return x.t1 - x.t0 > y.t1 - y.t0; });
+  return p;
+}
+
+}  // namespace spec

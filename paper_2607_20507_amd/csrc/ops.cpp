@@ -17,6 +17,7 @@
 #include "host_util.h"
 #include "kv4.h"
 #include "kv4_layout.h"
+#include "latent.h"
 #include "logprob.h"
 #include "vocab.h"
 
@@ -611,6 +612,174 @@ spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const int32_t* 
                                          c.plan.w, st), "spec_op_attention_kv4");
 } catch (const std::exception&) {
   return refuse(SPEC_E_UNSUPPORTED, "spec_op_attention_kv4: out of host memory");
+}
+
+// ---------------------------------------------------------------------------
+// the latent cache
+
+namespace {
+
+// Sizes of a latent cache's heads and entries that the kernels are built for.
+bool latent_sizes(int32_t nope_dim, int32_t rope_dim, int32_t rank) {
+  return (nope_dim == 64 || nope_dim == 128) && (rope_dim == 32 || rope_dim == 64) && (rank == 256 || rank == 512);
+}
+
+}  // namespace
+
+spec_status spec_op_rope_latent(int32_t dtype, int32_t R, int32_t n_heads, int32_t nope_dim, int32_t rope_dim,
+                                int32_t rank, float theta, float eps, const float* q, const float* kv,
+                                const void* norm_w, const int32_t* pos, const int32_t* slot, int32_t num_pages,
+                                void* q_out, void* pages, void* stream) {
+  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || R < 0 || n_heads <= 0 || n_heads > kMaxHeads || !(theta > 0.f) ||
+      !(eps >= 0.f) || num_pages < 0 || num_pages > kMaxSlotPages)
+    return refuse(SPEC_E_INVALID, "spec_op_rope_latent: bad dtype or size");
+  if (!latent_sizes(nope_dim, rope_dim, rank))
+    return refuse(SPEC_E_UNSUPPORTED, "spec_op_rope_latent: nope_dim must be 64 or 128, rope_dim 32 or 64, rank 256 or 512");
+  if (R == 0) return SPEC_OK;
+  if (!q || !kv || !norm_w || !pos || !slot || !q_out || (num_pages > 0 && !pages))
+    return refuse(SPEC_E_INVALID, "spec_op_rope_latent: null pointer");
+  if (misaligned(q, 16) || misaligned(kv, 16) || misaligned(norm_w, 16) || misaligned(q_out, 16) || misaligned(pages, 16))
+    return refuse(SPEC_E_INVALID, "spec_op_rope_latent: q, kv, norm_w, q_out and the pages must be 16-byte aligned");
+  return launched(launch_rope_latent(dtype == SPEC_F32 ? 0 : 1, R, n_heads, nope_dim, rope_dim, rank, theta, eps, q, kv,
+                                     norm_w, pos, slot, num_pages, q_out, pages, static_cast<hipStream_t>(stream)),
+                  "spec_op_rope_latent");
+}
+
+namespace {
+
+// One spec_op_attention_latent call: its work and the layout of its workspace.
+struct LatentCall {
+  spec_status status = SPEC_E_INVALID;
+  const char* why = "";
+  int R = 0;
+  int64_t pages = 0;  // of all sequences with rows
+  LatentPlan plan;
+  size_t o_q = 0, o_o = 0, o_part = 0, o_ml = 0, bytes = 0;
+};
+
+LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32_t* pos0, int32_t max_pages,
+                       int32_t n_heads, int32_t nope_dim, int32_t rope_dim, int32_t rank, int32_t v_dim) {
+  LatentCall c;
+  auto fail = [&](spec_status s, const char* why) {
+    c.status = s;
+    c.why = why;
+    return c;
+  };
+  if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || n_seqs < 0 || max_pages <= 0 || n_heads <= 0 || n_heads > kMaxHeads)
+    return fail(SPEC_E_INVALID, "spec_op_attention_latent: bad dtype or size");
+  if (!latent_sizes(nope_dim, rope_dim, rank) || (v_dim != 64 && v_dim != 128))
+    return fail(SPEC_E_UNSUPPORTED,
+                "spec_op_attention_latent: nope_dim and v_dim must be 64 or 128, rope_dim 32 or 64, rank 256 or 512");
+  if (n_seqs > 0 && (!rows || !pos0)) return fail(SPEC_E_INVALID, "spec_op_attention_latent: null pointer");
+  std::vector<LatentSegment> segs;
+  int64_t R = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    const int64_t len = static_cast<int64_t>(pos0[i]) + rows[i];
+    if (rows[i] < 0 || pos0[i] < 0 || len > kMaxExtent || (len + 15) / 16 > max_pages)
+      return fail(SPEC_E_INVALID, "spec_op_attention_latent: rows beyond the page table or 2^30 positions, or a negative length");
+    if ((R + rows[i]) * n_heads > kMaxExtent) return fail(SPEC_E_INVALID, "spec_op_attention_latent: more than 2^30 rows x heads");
+    if (rows[i] > 0) {
+      if (c.pages > kMaxExtent) return fail(SPEC_E_INVALID, "spec_op_attention_latent: too many pages");
+      segs.push_back(LatentSegment{static_cast<int32_t>(R), rows[i], pos0[i], static_cast<int32_t>(c.pages)});
+      c.pages += (len + 15) / 16;
+    }
+    R += rows[i];
+  }
+  c.R = static_cast<int>(R);
+  c.status = SPEC_OK;
+  if (R == 0) return c;
+  c.plan = plan_latent(segs, n_heads, kOpMaxParts, dtype == SPEC_F32);
+  const size_t elem = dtype == SPEC_F32 ? 4 : 2, lat = align_up(elem * R * n_heads * rank);
+  c.o_q = align_up(sizeof(int32_t) * c.pages) + align_up(sizeof(LatentItem) * c.plan.items.size()) +
+          align_up(sizeof(LatentGroup) * c.plan.groups.size());
+  c.o_o = c.o_q + lat;
+  c.o_part = c.o_o + lat;
+  c.o_ml = c.o_part + align_up(sizeof(float) * static_cast<size_t>(c.plan.n_parts) * c.plan.tile * rank);
+  c.bytes = c.o_ml + align_up(sizeof(float) * static_cast<size_t>(c.plan.n_parts) * c.plan.tile * 2);
+  return c;
+}
+
+}  // namespace
+
+size_t spec_op_attention_latent_workspace_bytes(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32_t* pos0,
+                                                int32_t max_pages, int32_t n_heads, int32_t nope_dim, int32_t rope_dim,
+                                                int32_t rank, int32_t v_dim) try {
+  const LatentCall c = latent_call(dtype, n_seqs, rows, pos0, max_pages, n_heads, nope_dim, rope_dim, rank, v_dim);
+  if (c.status != SPEC_OK) set_global_error(c.why);
+  return c.status == SPEC_OK ? c.bytes : 0;
+} catch (const std::exception&) {
+  set_global_error("spec_op_attention_latent: out of host memory");
+  return 0;
+}
+
+spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32_t* pos0,
+                                     const int32_t* page_table, int32_t max_pages, int32_t num_pages, int32_t n_heads,
+                                     int32_t nope_dim, int32_t rope_dim, int32_t rank, int32_t v_dim, float scale,
+                                     const void* q, const void* pages, const void* w_k, int64_t w_k_stride,
+                                     const void* w_v, int64_t w_v_stride, void* out, void* workspace,
+                                     size_t workspace_bytes, void* stream) try {
+  const LatentCall c = latent_call(dtype, n_seqs, rows, pos0, max_pages, n_heads, nope_dim, rope_dim, rank, v_dim);
+  if (c.status != SPEC_OK) return refuse(c.status, c.why);
+  if (!(scale > 0.f) || !(scale <= 1e30f)) return refuse(SPEC_E_INVALID, "spec_op_attention_latent: scale must be positive and finite");
+  if (c.R == 0) return SPEC_OK;
+  if (!page_table || !q || !pages || !w_k || !w_v || !out || !workspace)
+    return refuse(SPEC_E_INVALID, "spec_op_attention_latent: null pointer");
+  const int64_t unit = dtype == SPEC_F32 ? 4 : 8;  // elements in 16 bytes
+  if (w_k_stride < static_cast<int64_t>(nope_dim) * rank || w_v_stride < static_cast<int64_t>(v_dim) * rank ||
+      w_k_stride % unit || w_v_stride % unit || w_k_stride > (int64_t{1} << 40) || w_v_stride > (int64_t{1} << 40))
+    return refuse(SPEC_E_INVALID, "spec_op_attention_latent: a head stride that is short, odd or beyond 2^40");
+  if (misaligned(q, 16) || misaligned(pages, 16) || misaligned(w_k, 16) || misaligned(w_v, 16) || misaligned(out, 16) ||
+      misaligned(workspace, 256) || workspace_bytes < c.bytes)
+    return refuse(SPEC_E_INVALID,
+                  "spec_op_attention_latent: buffers must be 16-byte aligned, the workspace 256-byte aligned and large enough");
+  std::vector<int32_t> table;
+  table.reserve(c.pages);
+  for (int i = 0; i < n_seqs; ++i) {
+    const int n = rows[i] > 0 ? static_cast<int>((static_cast<int64_t>(pos0[i]) + rows[i] + 15) / 16) : 0;
+    const int32_t* from = page_table + static_cast<size_t>(i) * max_pages;
+    for (int j = 0; j < n; ++j)
+      if (from[j] < 0 || from[j] >= num_pages)
+        return refuse(SPEC_E_INVALID, "spec_op_attention_latent: page outside the pool");
+    table.insert(table.end(), from, from + n);
+  }
+  MetaBlock mb;
+  const size_t opt = mb.add(table), oit = mb.add(c.plan.items), ogr = mb.add(c.plan.groups);
+  char* ws = static_cast<char*>(workspace);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const spec_status up = upload_tables(ws, mb, "spec_op_attention_latent: larger tables than a captured call takes", st);
+  if (up != SPEC_OK) return up;
+  LatentArgs a;
+  a.dtype = dtype == SPEC_F32 ? 0 : 1;
+  a.R = c.R;
+  a.H = n_heads;
+  a.nope = nope_dim;
+  a.rope = rope_dim;
+  a.rank = rank;
+  a.vdim = v_dim;
+  a.scale = scale * 1.4426950408889634f;
+  a.q = q;
+  a.pages = pages;
+  a.w_k = w_k;
+  a.w_v = w_v;
+  a.k_stride = w_k_stride;
+  a.v_stride = w_v_stride;
+  a.page_list = reinterpret_cast<const int32_t*>(ws + opt);
+  a.out = out;
+  a.q_lat = ws + c.o_q;
+  a.o_lat = ws + c.o_o;
+  a.part_o = reinterpret_cast<float*>(ws + c.o_part);
+  a.part_ml = reinterpret_cast<float*>(ws + c.o_ml);
+  hipError_t e = launch_latent_absorb(a, st);
+  if (e == hipSuccess)
+    e = launch_latent_attention(a, reinterpret_cast<const LatentItem*>(ws + oit), static_cast<int>(c.plan.items.size()),
+                                c.plan.tile, st);
+  if (e == hipSuccess)
+    e = launch_latent_combine(a, reinterpret_cast<const LatentGroup*>(ws + ogr), static_cast<int>(c.plan.groups.size()),
+                              c.plan.tile, st);
+  if (e == hipSuccess) e = launch_latent_values(a, st);
+  return launched(e, "spec_op_attention_latent");
+} catch (const std::exception&) {
+  return refuse(SPEC_E_UNSUPPORTED, "spec_op_attention_latent: out of host memory");
 }
 
 }  // extern "C"
