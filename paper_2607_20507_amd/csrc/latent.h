@@ -17,12 +17,13 @@
 
 namespace spec {
 
-// Query vectors [qv0, qv0 + nqv) of one sequence, whose first row (of all
-// sequences' rows) is row0 at position pos0 and whose page ids start at entry
-// page0 of the page list, against its keys [t0, t1), t0 a multiple of 32.
+// Query vectors [qv0, qv0 + nqv) of one sequence, whose first row (of the rows that
+// take the form) is row0 at position pos0 and whose page ids start at entry page0
+// of the page list, against its keys [t0, t1), t0 a multiple of 32.  Its rows are qoff
+// rows further on among all rows of the call.
 // part >= 0: an unnormalised partial; part < 0: the normalised output.
 struct LatentItem {
-  int32_t qv0, nqv, row0, pos0, page0, t0, t1, part;
+  int32_t qv0, nqv, row0, pos0, page0, t0, t1, part, qoff;
 };
 
 // The parts of one tile's query vectors.
@@ -30,9 +31,10 @@ struct LatentGroup {
   int32_t qv0, nqv, part0, nparts;
 };
 
-// A sequence's rows [row0, row0 + nrows) at positions pos0.. .
+// A sequence's rows [row0, row0 + nrows), of those that take the form, at positions
+// pos0.. .
 struct LatentSegment {
-  int32_t row0, nrows, pos0, page0;
+  int32_t row0, nrows, pos0, page0, qoff;
 };
 
 struct LatentPlan {
@@ -45,19 +47,28 @@ struct LatentPlan {
 // Tiles and key splits of the absorbed form; at most max_parts partials.
 LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_parts, bool fp32);
 
+// Items of the expanded form (below): blocks of kPromptRows rows, those with most keys
+// first.
+std::vector<LatentItem> plan_latent_prompt(const std::vector<LatentSegment>& segs);
+
+// Whether a sequence of nrows rows behind pos0 others takes the expanded form.
+bool latent_expands(int nrows, int pos0);
+
 struct LatentArgs {
   int dtype;  // 0 fp32, 1 bf16 (q, pages, weights, out, q_lat, o_lat)
-  int R, H, nope, rope, rank, vdim;
+  int H, nope, rope, rank, vdim;
+  int R = 0;                          // rows that take the absorbed form
+  const int32_t* row_list = nullptr;  // which of all rows they are (null: the first R)
   float scale;             // of the scores, times log2 e
-  const void* q;           // [R, H, nope + rope]
+  const void* q;           // [rows, H, nope + rope]
   const void* pages;       // [P][16][rank + rope]
   const void* w_k;         // [H][nope][rank], k_stride elements between heads
   const void* w_v;         // [H][vdim][rank], v_stride elements between heads
   int64_t k_stride, v_stride;
   const int32_t* page_list;
-  void* out;               // [R, H, vdim]
-  void* q_lat;             // [R, H, rank]: the queries in the latents' space
-  void* o_lat;             // [R, H, rank]: the weighted sums of latents
+  void* out;               // [rows, H, vdim]
+  void* q_lat;             // [R, H, rank]: the absorbed rows' queries in the latents' space
+  void* o_lat;             // [R, H, rank]: their weighted sums of latents
   float* part_o;           // [parts][tile][rank]
   float* part_ml;          // [parts][tile][2]: raw maximum and sum
 };
@@ -73,5 +84,17 @@ hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st);
 hipError_t launch_latent_attention(const LatentArgs& a, const LatentItem* items, int n_items, int tile, hipStream_t st);
 hipError_t launch_latent_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int tile, hipStream_t st);
 hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st);
+
+// The expanded form (bf16): every head's keys [n_pages][H][16 x nope] and values
+// [n_pages][H][16 x vdim] of the listed pages, and the shared keys [n_pages][16 x
+// rope], in kv_layout.h's order; then items of at most kPromptRows rows (qv0, nqv: a
+// row and rows; page0: the sequence's first expanded page; t0 = 0, part < 0), each of
+// which is one workgroup a head.
+constexpr int kPromptRows = 256;
+struct LatentExpanded {
+  void *k = nullptr, *v = nullptr, *key = nullptr;
+};
+hipError_t launch_latent_expand(const LatentArgs& a, const int32_t* list, int n_pages, const LatentExpanded& x, hipStream_t st);
+hipError_t launch_latent_prompt(const LatentArgs& a, const LatentItem* items, int n_items, const LatentExpanded& x, hipStream_t st);
 
 }  // namespace spec

@@ -143,6 +143,9 @@ __global__ __launch_bounds__(256) void rope_latent_kernel(int H, int nope, int r
   }
 }
 
+// The row, among all, of absorbed row i.
+__device__ __forceinline__ int row_of(const LatentArgs& a, int i) { return a.row_list ? a.row_list[i] : i; }
+
 // ---------------------------------------------------------------------------
 // Queries into the latents' space: q' [row, h, c] = sum_n q[row, h, n] w_k[h, n, c].
 // A workgroup holds w_k's columns 64 cb .. of one head, one wave 16 of them as MFMA
@@ -180,12 +183,12 @@ __global__ __launch_bounds__(256) void latent_absorb_bf16_kernel(LatentArgs a) {
   bf16_t* to = static_cast<bf16_t*>(a.q_lat);
   const int hq = NOPE + a.rope;
   for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += 16 * gridDim.y) {
-    const int r = r0 + l16;
-    const size_t qv = static_cast<size_t>(min(r, a.R - 1)) * a.H + h;
+    const int r = r0 + l16, i = min(r, a.R - 1);
+    const size_t qv = static_cast<size_t>(i) * a.H + h, from = (static_cast<size_t>(row_of(a, i)) * a.H + h) * hq;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     uint4 qf[KS];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const uint4*>(q + qv * hq + 32 * s + 8 * g);
+    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const uint4*>(q + from + 32 * s + 8 * g);
 #pragma unroll
     for (int s = 0; s < KS; ++s) acc = mfma16x16x32(wf[s], qf[s], acc);
     if (r < a.R) put4(to + qv * a.rank + c0 + 16 * wave + 4 * g, acc[0], acc[1], acc[2], acc[3]);
@@ -209,12 +212,12 @@ __global__ __launch_bounds__(256) void latent_absorb_f32_kernel(LatentArgs a) {
   float* to = static_cast<float*>(a.q_lat);
   const int hq = NOPE + a.rope;
   for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += 16 * gridDim.y) {
-    const int r = r0 + l16;
-    const size_t qv = static_cast<size_t>(min(r, a.R - 1)) * a.H + h;
+    const int r = r0 + l16, i0 = min(r, a.R - 1);
+    const size_t qv = static_cast<size_t>(i0) * a.H + h, from = (static_cast<size_t>(row_of(a, i0)) * a.H + h) * hq;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     f32x4 qf[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) qf[j] = *reinterpret_cast<const f32x4*>(q + qv * hq + 16 * j + 4 * g);
+    for (int j = 0; j < J; ++j) qf[j] = *reinterpret_cast<const f32x4*>(q + from + 16 * j + 4 * g);
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -255,7 +258,7 @@ __global__ __launch_bounds__(256) void latent_values_bf16_kernel(LatentArgs a) {
     __syncthreads();
     if (wave == 0 && r < a.R) {
       acc = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
-      put4(out + qv * a.vdim + d0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+      put4(out + (static_cast<size_t>(row_of(a, r)) * a.H + h) * a.vdim + d0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
     }
     __syncthreads();
   }
@@ -291,7 +294,7 @@ __global__ __launch_bounds__(256) void latent_values_f32_kernel(LatentArgs a) {
     __syncthreads();
     if (wave == 0 && r < a.R) {
       acc = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
-      put4(out + qv * a.vdim + d0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+      put4(out + (static_cast<size_t>(row_of(a, r)) * a.H + h) * a.vdim + d0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
     }
     __syncthreads();
   }
@@ -456,7 +459,7 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
     klim[nt] = ok ? min(pos_of(m), it.t1 - 1) : -1;
     const size_t qv = static_cast<size_t>(it.qv0 + (ok ? m : 0));
     const bf16_t* ql = static_cast<const bf16_t*>(a.q_lat) + qv * RANK + 8 * g;
-    const bf16_t* qr = static_cast<const bf16_t*>(a.q) + qv * (a.nope + ROPE) + a.nope + 8 * g;
+    const bf16_t* qr = static_cast<const bf16_t*>(a.q) + (qv + static_cast<size_t>(it.qoff) * a.H) * (a.nope + ROPE) + a.nope + 8 * g;
 #pragma unroll
     for (int s = 0; s < DL + DR; ++s)
       qf[nt][s] = ok ? *reinterpret_cast<const uint4*>(s < DL ? ql + 32 * s : qr + 32 * (s - DL)) : make_uint4(0, 0, 0, 0);
@@ -680,7 +683,7 @@ __global__ __launch_bounds__(256, 1) void attn_latent_f32_kernel(LatentArgs a, c
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const float* src = 16 * j < RANK ? static_cast<const float*>(a.q_lat) + qv * RANK + 16 * j
-                                     : static_cast<const float*>(a.q) + qv * (a.nope + ROPE) + a.nope + 16 * j - RANK;
+                                     : static_cast<const float*>(a.q) + (qv + static_cast<size_t>(it.qoff) * a.H) * (a.nope + ROPE) + a.nope + 16 * j - RANK;
     qf[j] = ok ? *reinterpret_cast<const f32x4*>(src + 4 * g) : f32x4{0.f, 0.f, 0.f, 0.f};
   }
   float mneg = FLT_MAX, mlim = -INFINITY, lrun = 0.f;
@@ -818,6 +821,7 @@ hipError_t launch_rope_latent(int dtype, int R, int H, int nope, int rope, int r
 }
 
 hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st) {
+  if (a.R <= 0) return hipSuccess;
   const unsigned columns = static_cast<unsigned>(a.H) * (a.rank / 64);
   const dim3 grid(columns, row_blocks(a.R, columns));
   if (a.nope == 64 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<64>, grid, dim3(256), 0, st, a);
@@ -829,6 +833,7 @@ hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st) {
+  if (a.R <= 0) return hipSuccess;
   const unsigned columns = static_cast<unsigned>(a.H) * (a.vdim / 16);
   const dim3 grid(columns, row_blocks(a.R, columns));
   if (a.rank == 256 && a.dtype == 0) launch_kernel(latent_values_f32_kernel<256>, grid, dim3(256), 0, st, a);

@@ -12,7 +12,7 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_pa
   for (const LatentSegment& s : segs) most = std::max<int64_t>(most, static_cast<int64_t>(s.nrows) * H);
   p.tile = fp32 || most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 128;
   struct Tile {
-    int32_t qv0, nqv, row0, pos0, page0, kend;
+    int32_t qv0, nqv, row0, pos0, page0, kend, qoff;
   };
   std::vector<Tile> tiles;
   int64_t keys = 0;
@@ -21,7 +21,7 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_pa
     for (int64_t m = 0; m < n; m += p.tile) {
       const int64_t c = std::min<int64_t>(p.tile, n - m);
       const int kend = static_cast<int>(s.pos0 + (m + c - 1) / H + 1);  // keys 0 .. its last row's position
-      tiles.push_back(Tile{static_cast<int32_t>(first + m), static_cast<int32_t>(c), s.row0, s.pos0, s.page0, kend});
+      tiles.push_back(Tile{static_cast<int32_t>(first + m), static_cast<int32_t>(c), s.row0, s.pos0, s.page0, kend, s.qoff});
       keys += kend;
     }
   }
@@ -37,13 +37,13 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_pa
   for (const Tile& t : tiles) {
     const int c = static_cast<int>((t.kend + split - 1) / split);
     if (c <= 1) {
-      p.items.push_back(LatentItem{t.qv0, t.nqv, t.row0, t.pos0, t.page0, 0, t.kend, -1});
+      p.items.push_back(LatentItem{t.qv0, t.nqv, t.row0, t.pos0, t.page0, 0, t.kend, -1, t.qoff});
       continue;
     }
     p.groups.push_back(LatentGroup{t.qv0, t.nqv, p.n_parts, c});
     for (int i = 0; i < c; ++i)
       p.items.push_back(LatentItem{t.qv0, t.nqv, t.row0, t.pos0, t.page0, static_cast<int32_t>(i * split),
-                                   static_cast<int32_t>(std::min<int64_t>(t.kend, (i + 1) * split)), p.n_parts + i});
+                                   static_cast<int32_t>(std::min<int64_t>(t.kend, (i + 1) * split)), p.n_parts + i, t.qoff});
     p.n_parts += c;
   }
   // longest key ranges first, so that the short ones fill in behind them
@@ -51,5 +51,18 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_pa
                    [](const LatentItem& x, const LatentItem& y) { return x.t1 - x.t0 > y.t1 - y.t0; });
   return p;
 }
+
+std::vector<LatentItem> plan_latent_prompt(const std::vector<LatentSegment>& segs) {
+  std::vector<LatentItem> items;
+  for (const LatentSegment& s : segs)
+    for (int64_t r = 0; r < s.nrows; r += kPromptRows) {
+      const int n = static_cast<int>(std::min<int64_t>(kPromptRows, s.nrows - r)), first = static_cast<int>(r);
+      items.push_back(LatentItem{s.row0 + s.qoff + first, n, 0, s.pos0 + first, s.page0, 0, s.pos0 + first + n, -1, 0});
+    }
+  std::stable_sort(items.begin(), items.end(), [](const LatentItem& x, const LatentItem& y) { return x.t1 > y.t1; });
+  return items;
+}
+
+bool latent_expands(int nrows, int pos0) { return nrows >= 256; }
 
 }  // namespace spec

@@ -1,0 +1,429 @@
+// The expanded form of the attention over a latent cache, for long runs of rows:
+// every head's keys and values are made from the latents once, then attended to.
+
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
+
+#include "common.h"
+#include "kv_layout.h"
+#include "latent.h"
+
+namespace spec {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Expansion: keys and values of the listed pages, k[t, h, n] = sum_c c[t, c] w_k[h, n, c]
+// and v likewise, in the operand order of kv_layout.h, a block of 16 tokens per (page,
+// head); the shared keys in the same order, a block per page.
+// A workgroup makes 128 tokens x 128 features (two units of 64, each of one head's keys
+// or values), four waves 64 x 64 each, 64 of the sum at a time through LDS (direct
+// loads, two buffers).  Of every 32 rows, tile 0 takes rows 8 i + 0..3 and tile 1 rows
+// 8 i + 4..7, on both sides, so that a lane's two tiles hold 8 consecutive dims of a
+// token (keys: the weight's rows are the product's rows) or 8 consecutive tokens of a
+// dim (values: the tokens are), one 16-byte unit.  Chunk c of row r sits at c ^ key(r):
+// the 8 rows that 8 lanes read take every bank once.
+
+__global__ __launch_bounds__(256, 2) void latent_expand_kernel(LatentArgs a, const int32_t* __restrict__ list, int n_pages,
+                                                               int col_blocks, bf16_t* __restrict__ kx,
+                                                               bf16_t* __restrict__ vx, bf16_t* __restrict__ rx) {
+  constexpr int KB = 64;
+  __shared__ uint4 st[2][128 * 8], sw[2][128 * 8];
+  const int cb = blockIdx.x % col_blocks, tb = blockIdx.x / col_blocks;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, l16 = lane & 15;
+  const int uk = a.nope / 64, units = uk + a.vdim / 64;  // of a head: keys', all
+  const int entry = a.rank + a.rope;
+  const bf16_t* pool = static_cast<const bf16_t*>(a.pages);
+  auto key = [](int r) { return (r & 3) | (r >> 3 & 1) << 2; };
+  auto page_at = [&](int i) { return list[min(8 * tb + i, n_pages - 1)]; };
+
+  auto issue = [&](int k0, int b) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {  // 8 rows of each operand a load
+      const int i = 4 * wave + j, r = 8 * i + (lane >> 3), c = (lane & 7) ^ key(r);
+      const size_t page = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(page_at(i >> 1)));
+      load_lds16(pool + page * 16 * entry, ((r & 15) * entry + k0 + 8 * c) * 2, lds_addr(&st[b][64 * i]));
+      const int u = min(2 * cb + (i >> 3), a.H * units - 1), h = u / units, hu = u % units;
+      const bf16_t* w = hu < uk ? static_cast<const bf16_t*>(a.w_k) + h * a.k_stride + static_cast<size_t>(64) * hu * a.rank
+                                : static_cast<const bf16_t*>(a.w_v) + h * a.v_stride + static_cast<size_t>(64) * (hu - uk) * a.rank;
+      load_lds16(w, ((r & 63) * a.rank + k0 + 8 * c) * 2, lds_addr(&sw[b][64 * i]));
+    }
+  };
+
+  // the wave's 64 tokens and its unit
+  const int wt = wave >> 1, wu = wave & 1;
+  const int u = 2 * cb + wu, h = u / units, hu = u % units;
+  const bool values = hu >= uk;
+  // rows of the product: the weight's for keys, the tokens for values
+  int off[2];  // of a lane's chunk-0 unit in tile 0 and 1 of a 32-row pair
+#pragma unroll
+  for (int t = 0; t < 2; ++t) off[t] = (8 * (l16 >> 2) + (l16 & 3) + 4 * t) * 8;
+  const int kk = key(8 * (l16 >> 2) + (l16 & 3));  // (tile 1's rows and other pairs have the same)
+  f32x4 acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int nk = a.rank / KB;
+  issue(0, 0);
+  for (int k = 0; k < nk; ++k) {
+    SPEC_WAIT_VM_LDS(0);
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_s_barrier();
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    if (k + 1 < nk) issue(KB * (k + 1), (k + 1) & 1);
+    const uint4* tok = &st[k & 1][wt * 512];
+    const uint4* wgt = &sw[k & 1][wu * 512];
+    const uint4* rows = values ? tok : wgt;
+    const uint4* cols = values ? wgt : tok;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      uint4 x[4], y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = (i >> 1) * 256 + off[i & 1] + ((4 * s + g) ^ kk);
+        x[i] = rows[at];
+        y[i] = cols[at];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = mfma16x16x32(x[i], y[j], acc[i][j]);
+    }
+  }
+  if (u < a.H * units) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 lo = acc[2 * i][j], hi = acc[2 * i + 1][j];
+        const uint4 v = make_uint4(cvt_pk_bf16(lo[0], lo[1]), cvt_pk_bf16(lo[2], lo[3]), cvt_pk_bf16(hi[0], hi[1]),
+                                   cvt_pk_bf16(hi[2], hi[3]));
+        const int row = 32 * i + 8 * g;                                                 // .. + 7
+        const int col = 32 * (j >> 1) + 8 * (l16 >> 2) + (l16 & 3) + 4 * (j & 1);
+        const int t = 64 * wt + (values ? row : col);
+        const int page = 8 * tb + (t >> 4);
+        if (page >= n_pages) continue;
+        if (values) {
+          const int d = 64 * (hu - uk) + col;
+          *reinterpret_cast<uint4*>(vx + (static_cast<size_t>(page) * a.H + h) * 16 * a.vdim + kv_v_off(t & 15, d)) = v;
+        } else {
+          const int d = 64 * hu + row;
+          *reinterpret_cast<uint4*>(kx + (static_cast<size_t>(page) * a.H + h) * 16 * a.nope + kv_k_off(t & 15, d)) = v;
+        }
+      }
+  }
+  if (cb == 0) {
+    const int cr = a.rope / 8;
+    for (int e = threadIdx.x; e < 128 * cr; e += 256) {
+      const int t = e / cr, c = e % cr, page = 8 * tb + (t >> 4);
+      if (page >= n_pages) break;
+      const bf16_t* src = pool + static_cast<size_t>(static_cast<uint32_t>(list[page])) * 16 * entry + (t & 15) * entry + a.rank;
+      *reinterpret_cast<uint4*>(rx + static_cast<size_t>(page) * 16 * a.rope + kv_k_off(t & 15, 8 * c)) =
+          *reinterpret_cast<const uint4*>(src + 8 * c);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention to the expanded pages: one workgroup of 8 waves (two per SIMD) per (block
+// of 256 consecutive rows, head).  The structure is the K / V cache's prompt kernel's
+// (attention.hip): 64 keys at a time in LDS, three buffers; each wave both products for
+// its own 32 rows; a 32-key chunk is a matrix phase and a vector phase, and waves 4..7
+// run one phase behind waves 0..3, with which they share the SIMDs.  A key's score has
+// the head's own dims and the shared ones, whose block every head reads.
+// Differences to the maximum are taken before the scale.  Values that are not finite are
+// dropped from chunks in which some row does not see their key, and added after the
+// walk for the rows that do.
+
+constexpr float kPromptRescaleLog2 = 8.f;
+
+__device__ __forceinline__ uint32_t keep_pair(uint32_t w, int valid) {
+  return valid >= 2 ? w : valid == 1 ? w & 0xFFFFu : 0u;
+}
+
+template <int NOPE, int ROPE, int VD>
+__global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a, const LatentItem* __restrict__ items,
+                                                                    const bf16_t* __restrict__ kx,
+                                                                    const bf16_t* __restrict__ vx,
+                                                                    const bf16_t* __restrict__ rx) {
+  constexpr int DN = NOPE / 32, DS = DN + ROPE / 32;  // k-steps of the scores: own dims, all
+  constexpr int DT = VD / 16;
+  constexpr int NT = 2, NW = 8, NB = 3;
+  constexpr int KU = 2 * NOPE, RU = 2 * ROPE, VU = 2 * VD;  // 16-byte units of a page's block
+  constexpr int LK = KU / 64, LV = VU / 64, LR = RU / 64;   // loads of one
+  constexpr int NL = 4 * (LK + LV + LR);                    // loads of a stage
+  constexpr int LPW = NL / NW;                              // a wave's at least
+  __shared__ uint4 sk[NB][4 * KU], sv[NB][4 * VU], sr[NB][4 * RU];
+  const int h = blockIdx.x % a.H;
+  const LatentItem it = items[blockIdx.x / a.H];  // (qv0: its first row, nqv: rows)
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, l16 = lane & 15;
+  const int t1 = it.t1, np = (t1 + 15) >> 4, ns = (t1 + 63) >> 6;
+
+  auto issue = [&](int j, int b) {
+#pragma unroll
+    for (int n = 0; n < (NL + NW - 1) / NW; ++n) {
+      const int i = NW * n + wave;
+      if (i >= NL) break;
+      const bool k = i < 4 * LK, v = !k && i < 4 * (LK + LV);
+      const int e = k ? i : v ? i - 4 * LK : i - 4 * (LK + LV);
+      const int per = k ? LK : v ? LV : LR;
+      const int p = e / per, part = e % per;
+      const size_t page = static_cast<size_t>(it.page0) + min(4 * j + p, np - 1);
+      const bf16_t* blk = k ? kx + (page * a.H + h) * (16 * NOPE) : v ? vx + (page * a.H + h) * (16 * VD) : rx + page * (16 * ROPE);
+      const uint32_t dst = k ? lds_addr(&sk[b][p * KU]) : v ? lds_addr(&sv[b][p * VU]) : lds_addr(&sr[b][p * RU]);
+      load_lds16(blk, (part * 64 + lane) * 16, dst + part * 1024);
+    }
+  };
+
+  uint4 qf[NT][DS];
+  int klim[NT];  // the last key each row sees (-1: none, padding)
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int m = 32 * wave + 16 * nt + l16;
+    const bool ok = m < it.nqv;
+    klim[nt] = ok ? min(it.pos0 + m, t1 - 1) : -1;
+    const bf16_t* base = static_cast<const bf16_t*>(a.q) + (static_cast<size_t>(it.qv0 + (ok ? m : 0)) * a.H + h) * (NOPE + ROPE) + 8 * g;
+#pragma unroll
+    for (int s = 0; s < DS; ++s) qf[nt][s] = ok ? *reinterpret_cast<const uint4*>(base + 32 * s) : make_uint4(0, 0, 0, 0);
+  }
+  const int pos_lo = it.pos0 + 32 * wave;
+  const int pos_hi = it.pos0 + min(32 * wave + 31, it.nqv - 1);
+  const float scale = a.scale;
+  float mneg[NT], mlim[NT], lrun[NT][2];
+  f32x4 acc[DT][NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    mlim[nt] = -INFINITY;
+    mneg[nt] = FLT_MAX;
+    lrun[nt][0] = lrun[nt][1] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // the head's own dims of the next chunk's keys, read a phase ahead
+  uint4 kf[2][DN], vf[DT];
+  auto read_k = [&](int b, int hf) {
+    const uint4* kb = &sk[b][(2 * hf + (l16 >> 3)) * KU];
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+      for (int s = 0; s < DN; ++s) kf[hh][s] = kb[((s * 2 + hh) * 4 + g) * 8 + (l16 & 7)];
+  };
+  auto read_v = [&](int b, int hf, int q) {
+    const uint4* vb = &sv[b][(2 * hf + (g >> 1)) * VU];
+#pragma unroll
+    for (int dt = q * DT / 4; dt < (q + 1) * DT / 4; ++dt) vf[dt] = vb[(dt * 2 + (g & 1)) * 16 + l16];
+  };
+  f32x4 sc[NT][2];
+  uint4 pf[NT];
+  // (the shared keys are read here, under the own dims' products: a phase ahead they
+  // cost 16 registers more than there are)
+  auto scores = [&](int b, int hf) {
+    const uint4* rb = &sr[b][(2 * hf + (l16 >> 3)) * RU];
+    uint4 kr[2][DS - DN];
+#pragma unroll
+    for (int s = 0; s < DS - DN; ++s)
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) kr[hh][s] = rb[((s * 2 + hh) * 4 + g) * 8 + (l16 & 7)];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < DS; ++s)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+          sc[nt][hh] = mfma16x16x32(s < DN ? kf[hh][s] : kr[hh][s - DN], qf[nt][s], sc[nt][hh]);
+  };
+  bool dropped = false;
+  auto output = [&](int c0) {
+    if (c0 + 32 > t1) {
+      asm volatile("");
+      const int nvalid = min(max(t1 - (c0 + 8 * g), 0), 8);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        vf[dt].x = keep_pair(vf[dt].x, nvalid);
+        vf[dt].y = keep_pair(vf[dt].y, nvalid - 2);
+        vf[dt].z = keep_pair(vf[dt].z, nvalid - 4);
+        vf[dt].w = keep_pair(vf[dt].w, nvalid - 6);
+      }
+    }
+    if (c0 + 31 > pos_lo) {
+      asm volatile("");
+      uint32_t bad = 0;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        bad |= nonfinite_bits(vf[dt].x) | nonfinite_bits(vf[dt].y) | nonfinite_bits(vf[dt].z) | nonfinite_bits(vf[dt].w);
+      if (__any(bad != 0)) {
+        dropped = true;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vf[dt] = drop_nonfinite(vf[dt]);
+      }
+    }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) acc[dt][nt] = mfma16x16x32(vf[dt], pf[nt], acc[dt][nt]);
+  };
+  auto softmax = [&](int c0, int b, int hf) {
+    read_v(b, hf, 0);
+    read_v(b, hf, 1);
+    if (c0 + 31 > pos_lo || c0 + 31 >= t1) {
+      asm volatile("");
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (c0 + 8 * g + j > klim[nt]) sc[nt][j / 4][j % 4] = -INFINITY;
+    }
+    float mx[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      mx[nt] = sc[nt][0][0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) mx[nt] = fmaxf(mx[nt], sc[nt][j / 4][j % 4]);
+    }
+    if (__any(mx[0] > mlim[0] || mx[1] > mlim[1])) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float m = mx[nt];
+        m = fmaxf(m, __shfl_xor(m, 16, kWave));
+        m = fmaxf(m, __shfl_xor(m, 32, kWave));
+        if (m > mlim[nt]) {
+          const float alpha = __builtin_amdgcn_exp2f((-mneg[nt] - m) * scale);
+          mneg[nt] = -m;
+          mlim[nt] = m + kPromptRescaleLog2 / scale;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) lrun[nt][i] *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= alpha;
+        }
+      }
+    }
+    read_v(b, hf, 2);
+    read_v(b, hf, 3);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float p[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f((sc[nt][j / 4][j % 4] + mneg[nt]) * scale);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) lrun[nt][j % 2] += p[j];
+      pf[nt] = make_uint4(cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7]));
+    }
+  };
+  auto phase_end = [&] {
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    __atomic_signal_fence(__ATOMIC_SEQ_CST);
+  };
+
+  issue(0, 0);
+  if (ns > 1) {
+    issue(1, 1);
+    SPEC_WAIT_VM_LDS(LPW);
+  } else {
+    SPEC_WAIT_VM_LDS(0);
+  }
+  phase_end();  // stage 0 has landed
+  read_k(0, 0);
+  if (wave >= 4) phase_end();  // waves 4..7 run one phase behind
+  for (int j = 0; j < ns; ++j) {
+    const int b = j % NB, bn = (j + 1) % NB;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int c0 = 64 * j + 32 * hf;
+      // matrix phase (chunks above every row of this wave are left out)
+      if (c0 <= pos_hi) scores(b, hf);
+      if (hf == 0) read_k(b, 1);
+      else if (j + 1 < ns) read_k(bn, 0);
+      if (c0 >= 32 && c0 - 32 <= pos_hi) output(c0 - 32);
+      // stage j + 1 has landed before any wave reads it, a phase on
+      if (hf == 0) __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+      phase_end();
+      // vector phase.  Every wave is past its reads of stage j - 1, so its buffer takes stage j + 2
+      if (hf == 0 && j + 2 < ns) issue(j + 2, (j + 2) % NB);
+      __builtin_amdgcn_s_setprio(1);
+      if (c0 <= pos_hi) softmax(c0, b, hf);
+      __builtin_amdgcn_s_setprio(0);
+      SPEC_WAIT_VM_LDS(63);  // (LDS reads only)
+      phase_end();
+    }
+  }
+  if (64 * ns - 32 <= pos_hi) output(64 * ns - 32);
+  if (wave < 4) phase_end();
+  if (dropped)
+    for (int c0 = max(pos_lo - 31, 0) / 32 * 32; c0 <= pos_hi; c0 += 32) {
+      if (c0 + 31 <= pos_lo) continue;
+      const uint4* vb = reinterpret_cast<const uint4*>(
+          vx + ((static_cast<size_t>(it.page0) + min((c0 + 8 * g) >> 4, np - 1)) * a.H + h) * (16 * VD));
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const uint4 marks = nonfinite_marks(vb[(dt * 2 + (g & 1)) * 16 + l16]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          acc[dt][nt] += nonfinite_sum(mfma16x16x32(marks, seen_keys(klim[nt] - (c0 + 8 * g)), f32x4{0.f, 0.f, 0.f, 0.f}));
+      }
+    }
+
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    float l = lrun[nt][0] + lrun[nt][1];
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    const int m = 32 * wave + 16 * nt + l16;
+    if (m >= it.nqv) continue;
+    const float inv = 1.f / l;
+    bf16_t* o = static_cast<bf16_t*>(a.out) + (static_cast<size_t>(it.qv0 + m) * a.H + h) * VD + 4 * g;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const f32x4 v = acc[dt][nt] * inv;
+      *reinterpret_cast<uint2*>(o + 16 * dt) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
+    }
+  }
+}
+
+template <int NOPE, int ROPE, int VD>
+hipError_t launch_prompt(const LatentArgs& a, const LatentItem* items, unsigned n, const LatentExpanded& x, hipStream_t st) {
+  launch_kernel(attn_latent_prompt_kernel<NOPE, ROPE, VD>, dim3(n), dim3(512), 0, st, a, items, static_cast<const bf16_t*>(x.k),
+                static_cast<const bf16_t*>(x.v), static_cast<const bf16_t*>(x.key));
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_latent_expand(const LatentArgs& a, const int32_t* list, int n_pages, const LatentExpanded& x, hipStream_t st) {
+  const int units = a.H * (a.nope + a.vdim) / 64;
+  const size_t cols = (static_cast<size_t>(units) + 1) / 2, rows = (static_cast<size_t>(n_pages) + 7) / 8;
+  if (cols * rows > kMaxGrid256) return hipErrorInvalidValue;
+  launch_kernel(latent_expand_kernel, dim3(static_cast<unsigned>(cols * rows)), dim3(256), 0, st, a, list, n_pages,
+                static_cast<int>(cols), static_cast<bf16_t*>(x.k), static_cast<bf16_t*>(x.v), static_cast<bf16_t*>(x.key));
+  return hipGetLastError();
+}
+
+hipError_t launch_latent_prompt(const LatentArgs& a, const LatentItem* items, int n_items, const LatentExpanded& x, hipStream_t st) {
+  const size_t n = static_cast<size_t>(n_items) * a.H;
+  if (n == 0) return hipSuccess;
+  if (n > kMaxGrid256 / 2) return hipErrorInvalidValue;
+  const int sizes = (a.nope == 128 ? 4 : 0) + (a.rope == 64 ? 2 : 0) + (a.vdim == 128 ? 1 : 0);
+  const unsigned g = static_cast<unsigned>(n);
+  switch (sizes) {
+    case 0: return launch_prompt<64, 32, 64>(a, items, g, x, st);
+    case 1: return launch_prompt<64, 32, 128>(a, items, g, x, st);
+    case 2: return launch_prompt<64, 64, 64>(a, items, g, x, st);
+    case 3: return launch_prompt<64, 64, 128>(a, items, g, x, st);
+    case 4: return launch_prompt<128, 32, 64>(a, items, g, x, st);
+    case 5: return launch_prompt<128, 32, 128>(a, items, g, x, st);
+    case 6: return launch_prompt<128, 64, 64>(a, items, g, x, st);
+    default: return launch_prompt<128, 64, 128>(a, items, g, x, st);
+  }
+}
+
+}  // namespace spec

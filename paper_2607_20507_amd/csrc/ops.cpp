@@ -651,11 +651,19 @@ namespace {
 struct LatentCall {
   spec_status status = SPEC_E_INVALID;
   const char* why = "";
-  int R = 0;
-  int64_t pages = 0;  // of all sequences with rows
+  int64_t rows = 0;
+  int64_t pages = 0, x_pages = 0;  // of the sequences in the absorbed and the expanded form
+  std::vector<int> first, second;  // those sequences
+  std::vector<int32_t> row_list;   // the absorbed form's rows, where both are taken
+  int R = 0;                       // their number
   LatentPlan plan;
-  size_t o_q = 0, o_o = 0, o_part = 0, o_ml = 0, bytes = 0;
+  std::vector<LatentItem> x_items;
+  size_t o_q = 0, o_o = 0, o_part = 0, o_ml = 0, o_k = 0, o_v = 0, o_key = 0, bytes = 0;
 };
+
+// Most bytes of expanded keys and values: beyond it (131072 keys of 32 heads of 128
+// dims take 2 GiB) the absorbed form reads the cache itself.
+constexpr int64_t kLatentMaxExpanded = int64_t{1} << 32;
 
 LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const int32_t* pos0, int32_t max_pages,
                        int32_t n_heads, int32_t nope_dim, int32_t rope_dim, int32_t rank, int32_t v_dim) {
@@ -671,31 +679,47 @@ LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const
     return fail(SPEC_E_UNSUPPORTED,
                 "spec_op_attention_latent: nope_dim and v_dim must be 64 or 128, rope_dim 32 or 64, rank 256 or 512");
   if (n_seqs > 0 && (!rows || !pos0)) return fail(SPEC_E_INVALID, "spec_op_attention_latent: null pointer");
-  std::vector<LatentSegment> segs;
-  int64_t R = 0;
+  const int64_t x_page = int64_t{32} * (static_cast<int64_t>(n_heads) * (nope_dim + v_dim) + rope_dim);  // bytes
+  std::vector<LatentSegment> segs, x_segs;
   for (int i = 0; i < n_seqs; ++i) {
-    const int64_t len = static_cast<int64_t>(pos0[i]) + rows[i];
-    if (rows[i] < 0 || pos0[i] < 0 || len > kMaxExtent || (len + 15) / 16 > max_pages)
+    const int64_t len = static_cast<int64_t>(pos0[i]) + rows[i], pages = (len + 15) / 16;
+    if (rows[i] < 0 || pos0[i] < 0 || len > kMaxExtent || pages > max_pages)
       return fail(SPEC_E_INVALID, "spec_op_attention_latent: rows beyond the page table or 2^30 positions, or a negative length");
-    if ((R + rows[i]) * n_heads > kMaxExtent) return fail(SPEC_E_INVALID, "spec_op_attention_latent: more than 2^30 rows x heads");
-    if (rows[i] > 0) {
-      if (c.pages > kMaxExtent) return fail(SPEC_E_INVALID, "spec_op_attention_latent: too many pages");
-      segs.push_back(LatentSegment{static_cast<int32_t>(R), rows[i], pos0[i], static_cast<int32_t>(c.pages)});
-      c.pages += (len + 15) / 16;
+    if ((c.rows + rows[i]) * n_heads > kMaxExtent)
+      return fail(SPEC_E_INVALID, "spec_op_attention_latent: more than 2^30 rows x heads");
+    if (rows[i] == 0) continue;
+    if (c.pages + pages > kMaxExtent) return fail(SPEC_E_INVALID, "spec_op_attention_latent: too many pages");
+    const int32_t row = static_cast<int32_t>(c.rows);
+    if (dtype == SPEC_BF16 && latent_expands(rows[i], pos0[i]) && (c.x_pages + pages) * x_page <= kLatentMaxExpanded) {
+      x_segs.push_back(LatentSegment{0, rows[i], pos0[i], static_cast<int32_t>(c.x_pages), row});
+      c.second.push_back(i);
+      c.x_pages += pages;
+    } else {
+      segs.push_back(LatentSegment{c.R, rows[i], pos0[i], static_cast<int32_t>(c.pages), row - c.R});
+      c.first.push_back(i);
+      c.pages += pages;
+      c.R += rows[i];
     }
-    R += rows[i];
+    c.rows += rows[i];
   }
-  c.R = static_cast<int>(R);
   c.status = SPEC_OK;
-  if (R == 0) return c;
-  c.plan = plan_latent(segs, n_heads, kOpMaxParts, dtype == SPEC_F32);
-  const size_t elem = dtype == SPEC_F32 ? 4 : 2, lat = align_up(elem * R * n_heads * rank);
-  c.o_q = align_up(sizeof(int32_t) * c.pages) + align_up(sizeof(LatentItem) * c.plan.items.size()) +
-          align_up(sizeof(LatentGroup) * c.plan.groups.size());
+  if (c.rows == 0) return c;
+  if (c.R) c.plan = plan_latent(segs, n_heads, kOpMaxParts, dtype == SPEC_F32);
+  c.x_items = plan_latent_prompt(x_segs);
+  if (c.R && c.R < c.rows)
+    for (const LatentSegment& s : segs)
+      for (int r = 0; r < s.nrows; ++r) c.row_list.push_back(s.row0 + s.qoff + r);
+  const size_t elem = dtype == SPEC_F32 ? 4 : 2, lat = align_up(elem * c.R * n_heads * rank);
+  c.o_q = align_up(sizeof(int32_t) * (c.pages + c.x_pages)) + align_up(sizeof(LatentItem) * c.plan.items.size()) +
+          align_up(sizeof(LatentGroup) * c.plan.groups.size()) + align_up(sizeof(LatentItem) * c.x_items.size()) +
+          align_up(sizeof(int32_t) * c.row_list.size());
   c.o_o = c.o_q + lat;
   c.o_part = c.o_o + lat;
   c.o_ml = c.o_part + align_up(sizeof(float) * static_cast<size_t>(c.plan.n_parts) * c.plan.tile * rank);
-  c.bytes = c.o_ml + align_up(sizeof(float) * static_cast<size_t>(c.plan.n_parts) * c.plan.tile * 2);
+  c.o_k = c.o_ml + align_up(sizeof(float) * static_cast<size_t>(c.plan.n_parts) * c.plan.tile * 2);
+  c.o_v = c.o_k + align_up(size_t{32} * c.x_pages * n_heads * nope_dim);
+  c.o_key = c.o_v + align_up(size_t{32} * c.x_pages * n_heads * v_dim);
+  c.bytes = c.o_key + align_up(size_t{32} * c.x_pages * rope_dim);
   return c;
 }
 
@@ -721,7 +745,7 @@ spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_
   const LatentCall c = latent_call(dtype, n_seqs, rows, pos0, max_pages, n_heads, nope_dim, rope_dim, rank, v_dim);
   if (c.status != SPEC_OK) return refuse(c.status, c.why);
   if (!(scale > 0.f) || !(scale <= 1e30f)) return refuse(SPEC_E_INVALID, "spec_op_attention_latent: scale must be positive and finite");
-  if (c.R == 0) return SPEC_OK;
+  if (c.rows == 0) return SPEC_OK;
   if (!page_table || !q || !pages || !w_k || !w_v || !out || !workspace)
     return refuse(SPEC_E_INVALID, "spec_op_attention_latent: null pointer");
   const int64_t unit = dtype == SPEC_F32 ? 4 : 8;  // elements in 16 bytes
@@ -732,30 +756,34 @@ spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_
       misaligned(workspace, 256) || workspace_bytes < c.bytes)
     return refuse(SPEC_E_INVALID,
                   "spec_op_attention_latent: buffers must be 16-byte aligned, the workspace 256-byte aligned and large enough");
+  // the page ids that the call reads, one sequence after the other: the absorbed form's, then the expanded one's
   std::vector<int32_t> table;
-  table.reserve(c.pages);
-  for (int i = 0; i < n_seqs; ++i) {
-    const int n = rows[i] > 0 ? static_cast<int>((static_cast<int64_t>(pos0[i]) + rows[i] + 15) / 16) : 0;
-    const int32_t* from = page_table + static_cast<size_t>(i) * max_pages;
-    for (int j = 0; j < n; ++j)
-      if (from[j] < 0 || from[j] >= num_pages)
-        return refuse(SPEC_E_INVALID, "spec_op_attention_latent: page outside the pool");
-    table.insert(table.end(), from, from + n);
-  }
+  table.reserve(c.pages + c.x_pages);
+  for (const std::vector<int>* seqs : {&c.first, &c.second})
+    for (const int i : *seqs) {
+      const int n = static_cast<int>((static_cast<int64_t>(pos0[i]) + rows[i] + 15) / 16);
+      const int32_t* from = page_table + static_cast<size_t>(i) * max_pages;
+      for (int j = 0; j < n; ++j)
+        if (from[j] < 0 || from[j] >= num_pages)
+          return refuse(SPEC_E_INVALID, "spec_op_attention_latent: page outside the pool");
+      table.insert(table.end(), from, from + n);
+    }
   MetaBlock mb;
-  const size_t opt = mb.add(table), oit = mb.add(c.plan.items), ogr = mb.add(c.plan.groups);
+  const size_t opt = mb.add(table), oit = mb.add(c.plan.items), ogr = mb.add(c.plan.groups), oxi = mb.add(c.x_items),
+               orl = mb.add(c.row_list);
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const spec_status up = upload_tables(ws, mb, "spec_op_attention_latent: larger tables than a captured call takes", st);
   if (up != SPEC_OK) return up;
   LatentArgs a;
   a.dtype = dtype == SPEC_F32 ? 0 : 1;
-  a.R = c.R;
   a.H = n_heads;
   a.nope = nope_dim;
   a.rope = rope_dim;
   a.rank = rank;
   a.vdim = v_dim;
+  a.R = c.R;
+  a.row_list = c.row_list.empty() ? nullptr : reinterpret_cast<const int32_t*>(ws + orl);
   a.scale = scale * 1.4426950408889634f;
   a.q = q;
   a.pages = pages;
@@ -769,14 +797,23 @@ spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_
   a.o_lat = ws + c.o_o;
   a.part_o = reinterpret_cast<float*>(ws + c.o_part);
   a.part_ml = reinterpret_cast<float*>(ws + c.o_ml);
-  hipError_t e = launch_latent_absorb(a, st);
-  if (e == hipSuccess)
-    e = launch_latent_attention(a, reinterpret_cast<const LatentItem*>(ws + oit), static_cast<int>(c.plan.items.size()),
+  hipError_t e = hipSuccess;
+  if (!c.x_items.empty()) {
+    const LatentExpanded x{ws + c.o_k, ws + c.o_v, ws + c.o_key};
+    e = launch_latent_expand(a, a.page_list + c.pages, static_cast<int>(c.x_pages), x, st);
+    if (e == hipSuccess)
+      e = launch_latent_prompt(a, reinterpret_cast<const LatentItem*>(ws + oxi), static_cast<int>(c.x_items.size()), x, st);
+  }
+  if (c.R) {
+    if (e == hipSuccess) e = launch_latent_absorb(a, st);
+    if (e == hipSuccess)
+      e = launch_latent_attention(a, reinterpret_cast<const LatentItem*>(ws + oit), static_cast<int>(c.plan.items.size()),
+                                  c.plan.tile, st);
+    if (e == hipSuccess)
+      e = launch_latent_combine(a, reinterpret_cast<const LatentGroup*>(ws + ogr), static_cast<int>(c.plan.groups.size()),
                                 c.plan.tile, st);
-  if (e == hipSuccess)
-    e = launch_latent_combine(a, reinterpret_cast<const LatentGroup*>(ws + ogr), static_cast<int>(c.plan.groups.size()),
-                              c.plan.tile, st);
-  if (e == hipSuccess) e = launch_latent_values(a, st);
+    if (e == hipSuccess) e = launch_latent_values(a, st);
+  }
   return launched(e, "spec_op_attention_latent");
 } catch (const std::exception&) {
   return refuse(SPEC_E_UNSUPPORTED, "spec_op_attention_latent: out of host memory");
