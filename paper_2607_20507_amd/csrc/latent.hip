@@ -27,6 +27,30 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
+// A product whose sum stays in accumulation registers, in place: left to itself the
+// compiler keeps a second copy of the sums, and there are no registers for one.  It
+// does not see that this is an MFMA, so the waits that one needs are written out:
+// two states after a vector instruction that wrote an operand, sums_ready() before
+// anything but such a product reads the sums.
+__device__ __forceinline__ void mfma_in_place(const uint4& a, const uint4& b, f32x4& c) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0"
+               : "+a"(c)
+               : "v"(__builtin_bit_cast(u32x4, a)), "v"(__builtin_bit_cast(u32x4, b)));
+}
+// c *= x for such a sum, which stays where it is.
+__device__ __forceinline__ void scale_in_place(f32x4& c, float x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float v = c[i], w;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(w) : "a"(v));
+    w *= x;
+    asm volatile("v_accvgpr_write_b32 %0, %1" : "=a"(v) : "v"(w));
+    c[i] = v;
+  }
+}
+__device__ __forceinline__ void operands_ready() { asm volatile("s_nop 1"); }
+__device__ __forceinline__ void sums_ready() { asm volatile("s_nop 15\n\ts_nop 7"); }
+
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 
 __device__ __forceinline__ void wave_fence() {
@@ -403,6 +427,7 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
   constexpr int DL = RANK / 32, DR = ROPE / 32;  // k-steps of the scores
   constexpr int DT = RANK / 16;                  // 16-dim output tiles
   constexpr int NB = WK == 4 ? 1 : 2;            // chunk buffers of a key share
+  constexpr int PD = NT == 1 ? 8 : 5;            // operands read ahead
   constexpr int BU = 32 * (CL + CR);             // units of one
   constexpr int Q = 16 * NT * WQ;
   constexpr int TP = 64 / CL, RT = 64 / CR;      // tokens a load covers: latents, keys
@@ -467,7 +492,10 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
     mlim[nt] = -INFINITY;
     lrun[nt][0] = lrun[nt][1] = 0.f;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int dt = 0; dt < DT; ++dt) {
+      acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      asm volatile("" : "+a"(acc[dt][nt]));
+    }
   }
   const bool active = m0 < it.nqv;
   const int pos_lo = active ? pos_of(m0) : -1;
@@ -492,20 +520,28 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
       const uint2 x = read_tr(at), y = read_tr(at + 16 * RANK * 2);
       return make_uint4(x.x, x.y, y.x, y.y);
     };
+    auto read_k = [&](int u) {  // k-step u / 2 of key tile u % 2
+      const int s = u >> 1, hh = u & 1;
+      if (s < DL) return kb[16 * hh * CL + (s & 1 ? k_off1 : k_off0) + 8 * (s >> 1)];
+      if (CR == 8) return rb[(16 * hh + l16) * 8 + ((4 * (s - DL) + g) ^ fk)];
+      return rb[(16 * hh + l16) * 4 + (g ^ (l16 >> 1 & 3))];
+    };
+    // operands are read PD ahead of their product, in this order: read earlier they
+    // take registers that there are not
+    uint4 ring[PD];
     f32x4 sc[NT][2];
 #pragma unroll
+    for (int u = 0; u < PD; ++u) ring[u] = read_k(u);
+#pragma unroll
     for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int s = 0; s < DL + DR; ++s)
+    for (int u = 0; u < 2 * (DL + DR); ++u) {
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh) {
-        uint4 k;
-        if (s < DL) k = kb[16 * hh * CL + (s & 1 ? k_off1 : k_off0) + 8 * (s >> 1)];
-        else if (CR == 8) k = rb[(16 * hh + l16) * 8 + ((4 * (s - DL) + g) ^ fk)];
-        else k = rb[(16 * hh + l16) * 4 + (g ^ (l16 >> 1 & 3))];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) sc[nt][hh] = mfma16x16x32(k, qf[nt][s], sc[nt][hh]);
-      }
+      for (int nt = 0; nt < NT; ++nt) sc[nt][u & 1] = mfma16x16x32(ring[u % PD], qf[nt][u >> 1], sc[nt][u & 1]);
+      if (u + PD < 2 * (DL + DR)) ring[u % PD] = read_k(u + PD);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     bool bad = false;
     if (t0 + 31 > pos_lo || t0 + 31 >= it.t1) {  // some key that some row does not see
       asm volatile("");
@@ -551,20 +587,22 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
       raise |= mx[nt] > mlim[nt];
     }
     if (__any(raise)) {
+      sums_ready();
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float m = mx[nt];
         m = fmaxf(m, __shfl_xor(m, 16, kWave));
         m = fmaxf(m, __shfl_xor(m, 32, kWave));
+        float alpha = 1.f;
         if (m > mlim[nt]) {
-          const float alpha = __builtin_amdgcn_exp2f((-mneg[nt] - m) * a.scale);
+          alpha = __builtin_amdgcn_exp2f((-mneg[nt] - m) * a.scale);
           mneg[nt] = -m;
           mlim[nt] = m + kLatentRescaleLog2 / a.scale;
-#pragma unroll
-          for (int i = 0; i < 2; ++i) lrun[nt][i] *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= alpha;
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) lrun[nt][i] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) scale_in_place(acc[dt][nt], alpha);
       }
     }
     uint4 pf[NT];
@@ -578,40 +616,42 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
       // bf16, as the values that it weights: its rounding stays below the output's
       pf[nt] = make_uint4(cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7]));
     }
-    if (bad) {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const uint4 v = drop_nonfinite(read_v(dt));
+    for (int u = 0; u < PD; ++u) ring[u] = read_v(u);
+    operands_ready();
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[dt][nt] = mfma16x16x32(v, pf[nt], acc[dt][nt]);
+    for (int dt = 0; dt < DT; ++dt) {
+      if (bad) {
+        ring[dt % PD] = drop_nonfinite(ring[dt % PD]);
+        operands_ready();
       }
-    } else {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const uint4 v = read_v(dt);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) acc[dt][nt] = mfma16x16x32(v, pf[nt], acc[dt][nt]);
-      }
+      for (int nt = 0; nt < NT; ++nt) mfma_in_place(ring[dt % PD], pf[nt], acc[dt][nt]);
+      if (dt + PD < DT) ring[dt % PD] = read_v(dt + PD);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
 
-  if (NB == 2 && wk < nch) issue(c0 + wk, 0);
+  // (a share's chunk past the last is loaded from the last page, and masked)
+  if (NB == 2) issue(c0 + wk, 0);
   for (int j = 0; j < nit; ++j) {
-    const int i = j * WK + wk, c = c0 + i;
+    const int c = c0 + j * WK + wk;
     if (NB == 2) {
       SPEC_WAIT_VM_LDS(0);
       block_sync();  // chunk j has landed, and every wave is done with the one before
-      if (i + WK < nch) issue(c + WK, (j + 1) & 1);
+      if (j + 1 < nit) issue(c + WK, (j + 1) & 1);
     } else {  // a buffer of the wave's own
       SPEC_WAIT_VM_LDS(0);
       wave_fence();
-      if (i < nch) issue(c, 0);
+      issue(c, 0);
       SPEC_WAIT_VM_LDS(0);
       wave_fence();
     }
-    if (i < nch && 32 * c <= pos_hi) chunk(c, NB == 2 ? j & 1 : 0);
+    chunk(c, NB == 2 ? j & 1 : 0);
   }
 
+  sums_ready();
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     float l = lrun[nt][0] + lrun[nt][1];
