@@ -37,6 +37,25 @@ __device__ __forceinline__ void mfma_in_place(const uint4& a, const uint4& b, f3
                : "+a"(c)
                : "v"(__builtin_bit_cast(u32x4, a)), "v"(__builtin_bit_cast(u32x4, b)));
 }
+// The same on vector registers, and a first product (sum 0).
+__device__ __forceinline__ void mfma_in_place_v(const uint4& a, const uint4& b, f32x4& c) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0"
+               : "+v"(c)
+               : "v"(__builtin_bit_cast(u32x4, a)), "v"(__builtin_bit_cast(u32x4, b)));
+}
+__device__ __forceinline__ f32x4 mfma_first_v(const uint4& a, const uint4& b) {
+  f32x4 c;
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0"
+               : "=v"(c)
+               : "v"(__builtin_bit_cast(u32x4, a)), "v"(__builtin_bit_cast(u32x4, b)));
+  return c;
+}
+// x ^ k, computed where it stands: the compiler would have every step's address ready
+// ahead, and there are no registers for that.
+__device__ __forceinline__ uint32_t xor_here(uint32_t x, uint32_t k) {
+  asm volatile("v_xor_b32 %0, %1, %2" : "=v"(x) : "s"(k), "v"(x));
+  return x;
+}
 // c *= x for such a sum, which stays where it is.
 __device__ __forceinline__ void scale_in_place(f32x4& c, float x) {
 #pragma unroll
@@ -412,14 +431,14 @@ __global__ __launch_bounds__(RANK / 4) void latent_combine_kernel(LatentArgs a, 
 // the keys in the order in which a lane's score accumulators hold them, so the
 // probabilities go from one product to the other in registers.
 // Chunks of 16 bytes of token t's latent sit at c ^ f(t): the 8 lanes of a row read
-// (8 tokens, one chunk) and the 16 of a transposed one (4 tokens, two chunks) take
-// every bank once.
+// (8 tokens, one chunk: 128 bytes) and the 32 of a transposed one (8 tokens, two
+// chunks: 256 bytes) take every bank once.
 // The running maximum (of raw scores) is raised only when a score exceeds it by more
 // than 2^8; differences are taken before the scale, so scores of any size keep theirs.
-// A key that some row of the wave does not see may hold a value that is not finite
-// (a slot past the sequence anything at all).  Its scores are not finite then, which
-// sends the wave through a form that drops such values from the second product and
-// gives the rows that see the key a NaN score.
+// A key that some row does not see may hold a value that is not finite (a slot past the
+// sequence anything at all), whose product with the row's probability 0 would be NaN.
+// So chunks with such keys are cleaned in LDS between the two products: values that
+// are not finite become 0, and the rows that do see their key get a NaN score.
 
 template <int RANK, int ROPE, int NT, int WQ, int WK>
 __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, const LatentItem* __restrict__ items) {
@@ -427,7 +446,7 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
   constexpr int DL = RANK / 32, DR = ROPE / 32;  // k-steps of the scores
   constexpr int DT = RANK / 16;                  // 16-dim output tiles
   constexpr int NB = WK == 4 ? 1 : 2;            // chunk buffers of a key share
-  constexpr int PD = NT == 1 ? 8 : 5;            // operands read ahead
+  constexpr int PD = NT == 1 ? 8 : 4;            // operands read ahead
   constexpr int BU = 32 * (CL + CR);             // units of one
   constexpr int Q = 16 * NT * WQ;
   constexpr int TP = 64 / CL, RT = 64 / CR;      // tokens a load covers: latents, keys
@@ -435,8 +454,9 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
   constexpr int kJoin = WK > 1 ? WK * Q * (RANK + 4) * 4 / 16 : 0;
   constexpr int kUnits = WK * NB * BU > kJoin ? WK * NB * BU : kJoin;
   static_assert(WQ * WK == 4 && (WK == 1 || NT == 1));
-  __shared__ uint4 buf[kUnits];
+  __shared__ __attribute__((aligned(256))) uint4 buf[kUnits];
   __shared__ float s_ml[WK > 1 ? 2 * WK * Q : 1];
+  __shared__ uint32_t s_flag[4];
   const LatentItem it = items[blockIdx.x];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -447,26 +467,38 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
   const int np = (it.t1 + 15) >> 4;
   const int c0 = it.t0 >> 5, nch = (it.t1 - it.t0 + 31) >> 5;
   const int nit = (nch + WK - 1) / WK;
-  auto f = [](int t) { return (t & 3) << 1 | (t >> 2 & 1); };
-  auto fr = [&](int t) { return CR == 8 ? f(t) : t >> 1 & 3; };
+  auto f = [](int t) { return (t & 7) << 1 | (t >> 2 & 1); };
+  auto fr = [&](int t) { return CR == 8 ? (t & 3) << 1 | (t >> 2 & 1) : t >> 1 & 3; };
 
-  // the wave's loads of chunk c into buffer b
-  auto issue = [&](int c, int b) {
+  // lane offsets of the loads
+  const uint32_t ld_lat = (lane % CL ^ (TP == 2 ? (lane >> 5) * 2 : 0)) * 16;
+  const uint32_t ld_key = lane / CR * ((CL + CR) * 16) + (CL + (lane % CR ^ fr(lane / CR))) * 16;
+  // the pages of chunk c (past the last: the last's), asked for a chunk before they are needed
+  int32_t page_id[2];
+  auto ask = [&](int c) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) page_id[i] = list[min(2 * c + i, np - 1)];
+  };
+  // the wave's loads of the chunk asked for into buffer b
+  auto issue = [&](int b) {
     size_t page[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      page[i] = static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(list[min(2 * c + i, np - 1)])));
+    for (int i = 0; i < 2; ++i) page[i] = static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(page_id[i])));
     const uint32_t dst = lds_addr(&buf[(wk * NB + b) * BU]);
+    constexpr int kEntry = (CL + CR) * 16;
 #pragma unroll
     for (int j = 0; j < (NL + WQ - 1) / WQ; ++j) {
       const int i = WQ * j + wq;
       if (i >= NL) break;
       const bool key = i >= NLL;
       const int first = key ? (i - NLL) * RT : i * TP;
-      const int t = key ? first + lane / CR : first + lane / CL;
-      const int ch = key ? CL + (lane % CR ^ fr(t)) : lane % CL ^ f(t);
-      const char* base = pool + (first >> 4 ? page[1] : page[0]) * (16 * (CL + CR) * 16);
-      load_lds16(base, ((t & 15) * (CL + CR) + ch) * 16, dst + i * 1024);
+      const char* base = pool + (first >> 4 ? page[1] : page[0]) * (16 * kEntry) + (first & 15) * kEntry;
+      // (f of a load's second token, first + 1, is f(first) ^ 2)
+      uint32_t at;
+      if (key) at = ld_key;
+      else if (TP == 1) at = xor_here(ld_lat, f(first) * 16);
+      else at = xor_here(ld_lat, f(first) * 16) + (lane >> 5) * kEntry;
+      load_lds16(base, at, dst + i * 1024);
     }
   };
 
@@ -497,34 +529,31 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
       asm volatile("" : "+a"(acc[dt][nt]));
     }
   }
-  const bool active = m0 < it.nqv;
-  const int pos_lo = active ? pos_of(m0) : -1;
-  const int pos_hi = active ? min(pos_of(min(m0 + 16 * NT, it.nqv) - 1), it.t1 - 1) : -1;
+  const int pos_lo = pos_of(0);
 
   // lane constants of the reads
-  const int fk = f(l16);
-  const int k_off0 = l16 * CL + (g ^ fk), k_off1 = l16 * CL + ((4 + g) ^ fk);
-  const int fv = (l16 >> 2) << 1 | (g & 1);
-  uint32_t v_off[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    v_off[i] = (4 * g + (l16 >> 2)) * (RANK * 2) + ((2 * i + (l16 >> 1 & 1)) ^ fv) * 16 + (l16 & 1) * 8;
+  // (of a k-step's or output tile's number, the bits that f changes are an exclusive or of the address)
+  const uint32_t k_off = l16 * (CL * 16) + ((g ^ f(l16)) * 16);
+  const int tv = 4 * g + (l16 >> 2);
+  const uint32_t v_off = tv * (CL * 16) + (((l16 >> 1 & 1) ^ f(tv)) * 16) + (l16 & 1) * 8;
+  const uint32_t r_off = l16 * (CR * 16) + (g ^ fr(l16)) * 16;
+  typedef __attribute__((address_space(3))) const u32x4* lds_units;
+  auto unit_at = [](uint32_t lds) { return __builtin_bit_cast(uint4, *(lds_units)(uintptr_t)lds); };
 
-  auto chunk = [&](int c, int b) {
-    const uint4* kb = &buf[(wk * NB + b) * BU];
-    const uint4* rb = kb + 32 * CL;
-    const uint32_t vb = lds_addr(kb);
+  // masked: some row of the workgroup does not see some key of the step's chunks
+  auto chunk = [&](int c, int b, bool masked) {
+    const uint32_t vb = lds_addr(&buf[(wk * NB + b) * BU]);  // (a multiple of 256)
+    const uint32_t vv = vb + v_off, kb = vb + k_off, rb = vb + 32 * CL * 16 + r_off;
     const int t0 = 32 * c;
     auto read_v = [&](int dt) {
-      const uint32_t at = vb + v_off[dt & 3] + (dt >> 2) * 128;
+      const uint32_t at = (dt & 7 ? xor_here(vv, (dt & 7) * 32) : vv) + (dt >> 3) * 256;
       const uint2 x = read_tr(at), y = read_tr(at + 16 * RANK * 2);
       return make_uint4(x.x, x.y, y.x, y.y);
     };
     auto read_k = [&](int u) {  // k-step u / 2 of key tile u % 2
       const int s = u >> 1, hh = u & 1;
-      if (s < DL) return kb[16 * hh * CL + (s & 1 ? k_off1 : k_off0) + 8 * (s >> 1)];
-      if (CR == 8) return rb[(16 * hh + l16) * 8 + ((4 * (s - DL) + g) ^ fk)];
-      return rb[(16 * hh + l16) * 4 + (g ^ (l16 >> 1 & 3))];
+      if (s < DL) return unit_at((s & 3 ? xor_here(kb, (s & 3) * 64) : kb) + (s >> 2) * 256 + hh * (16 * CL * 16));
+      return unit_at((s > DL ? xor_here(rb, 64) : rb) + hh * (16 * CR * 16));
     };
     // operands are read PD ahead of their product, in this order: read earlier they
     // take registers that there are not
@@ -532,51 +561,53 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
     f32x4 sc[NT][2];
 #pragma unroll
     for (int u = 0; u < PD; ++u) ring[u] = read_k(u);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int u = 0; u < 2 * (DL + DR); ++u) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) sc[nt][u & 1] = mfma16x16x32(ring[u % PD], qf[nt][u >> 1], sc[nt][u & 1]);
+      for (int nt = 0; nt < NT; ++nt) {
+        if (u < 2) sc[nt][u & 1] = mfma_first_v(ring[u % PD], qf[nt][u >> 1]);
+        else mfma_in_place_v(ring[u % PD], qf[nt][u >> 1], sc[nt][u & 1]);
+      }
       if (u + PD < 2 * (DL + DR)) ring[u % PD] = read_k(u + PD);
       __builtin_amdgcn_sched_barrier(0);
     }
-    bool bad = false;
-    if (t0 + 31 > pos_lo || t0 + 31 >= it.t1) {  // some key that some row does not see
+    sums_ready();
+    if (masked) {
       asm volatile("");
-      bool odd = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) odd |= !finite(sc[nt][j / 4][j % 4]);
-      bad = __any(odd);
-      uint32_t flags = 0;  // of the lane's 8 keys: a latent that is not finite
-      if (bad) {
+      uint4* lat = &buf[(wk * NB + b) * BU];
+      if (WQ > 1) {
+        SPEC_WAIT_VM_LDS(63);
+        block_sync();  // every wave of the share has its scores
+      }
+      uint32_t flags = 0;
 #pragma unroll 1
-        for (int i = 0; i < DT / 4; ++i)
+      for (int i = wq; i < NLL; i += WQ) {
+        const uint4 v = lat[64 * i + lane];
+        const uint64_t m = __ballot((nonfinite_bits(v.x) | nonfinite_bits(v.y) | nonfinite_bits(v.z) | nonfinite_bits(v.w)) != 0);
+        if (m == 0) continue;
+        lat[64 * i + lane] = drop_nonfinite(v);
+        if (TP == 1) flags |= 1u << i;
+        else flags |= (static_cast<uint32_t>(m) ? 1u : 0u) << (2 * i) | (m >> 32 ? 2u : 0u) << (2 * i);
+      }
+      if (WQ > 1) {
+        if (lane == 0) s_flag[wave] = flags;
+        SPEC_WAIT_VM_LDS(63);
+        block_sync();
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t at = vb + v_off[j] + i * 128;
-            const uint2 x = read_tr(at), y = read_tr(at + 16 * RANK * 2);
-            const uint32_t w[4] = {x.x, x.y, y.x, y.y};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t n = nonfinite_bits(w[e]);
-              flags |= (n >> 15 & 1u) << (2 * e) | (n >> 31) << (2 * e + 1);
-            }
-          }
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) flags |= __shfl_xor(flags, o, kWave);
+        for (int i = 0; i < WQ; ++i) flags |= s_flag[wk * WQ + i];
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          if (t0 + 16 * (j / 4) + 4 * g + j % 4 > klim[nt]) sc[nt][j / 4][j % 4] = -INFINITY;
-          else if (flags >> j & 1) sc[nt][j / 4][j % 4] = __builtin_nanf("");
+          const int k = 16 * (j / 4) + 4 * g + j % 4;
+          if (t0 + k > klim[nt]) sc[nt][j / 4][j % 4] = -INFINITY;
+          else if (flags >> k & 1) sc[nt][j / 4][j % 4] = __builtin_nanf("");
         }
     }
+#pragma unroll
+    for (int u = 0; u < PD; ++u) ring[u] = read_v(u);
     float mx[NT];
     bool raise = false;
 #pragma unroll
@@ -616,16 +647,10 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
       // bf16, as the values that it weights: its rounding stays below the output's
       pf[nt] = make_uint4(cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7]));
     }
-#pragma unroll
-    for (int u = 0; u < PD; ++u) ring[u] = read_v(u);
     operands_ready();
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      if (bad) {
-        ring[dt % PD] = drop_nonfinite(ring[dt % PD]);
-        operands_ready();
-      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) mfma_in_place(ring[dt % PD], pf[nt], acc[dt][nt]);
       if (dt + PD < DT) ring[dt % PD] = read_v(dt + PD);
@@ -634,21 +659,28 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
   };
 
   // (a share's chunk past the last is loaded from the last page, and masked)
-  if (NB == 2) issue(c0 + wk, 0);
+  ask(c0 + wk);
+  if (NB == 2) {
+    issue(0);
+    ask(c0 + WK + wk);
+  }
   for (int j = 0; j < nit; ++j) {
     const int c = c0 + j * WK + wk;
     if (NB == 2) {
       SPEC_WAIT_VM_LDS(0);
       block_sync();  // chunk j has landed, and every wave is done with the one before
-      if (j + 1 < nit) issue(c + WK, (j + 1) & 1);
+      if (j + 1 < nit) issue((j + 1) & 1);
+      ask(c + 2 * WK);
     } else {  // a buffer of the wave's own
       SPEC_WAIT_VM_LDS(0);
       wave_fence();
-      issue(c, 0);
+      issue(0);
+      ask(c + WK);
       SPEC_WAIT_VM_LDS(0);
       wave_fence();
     }
-    chunk(c, NB == 2 ? j & 1 : 0);
+    const int last = 32 * (c0 + (j + 1) * WK) - 1;
+    chunk(c, NB == 2 ? j & 1 : 0, last > pos_lo || last >= it.t1);
   }
 
   sums_ready();
