@@ -82,7 +82,9 @@ hipError_t launch_rope_latent(int dtype, int R, int H, int nope, int rope, int r
 
 hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st);
 hipError_t launch_latent_attention(const LatentArgs& a, const LatentItem* items, int n_items, int tile, hipStream_t st);
-hipError_t launch_latent_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int tile, hipStream_t st);
+// (max_parts: the most parts of a group)
+hipError_t launch_latent_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int tile, int max_parts,
+                                 hipStream_t st);
 hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st);
 
 // The expanded form (bf16): every head's keys [n_pages][H][16 x nope] and values

@@ -386,38 +386,62 @@ __device__ __forceinline__ void join_waves(const LatentArgs& a, const LatentItem
   }
 }
 
-// One workgroup per query vector of a group: four values a thread.
-template <typename T, int RANK>
-__global__ __launch_bounds__(RANK / 4) void latent_combine_kernel(LatentArgs a, const LatentGroup* __restrict__ groups,
-                                                                  int tile) {
+// One workgroup per query vector of a group and block of 1024 / PG columns: four columns
+// a thread, the parts dealt to PG shares, whose sums are added in their order.
+constexpr int kCombineMaxParts = 4096;
+
+template <typename T, int RANK, int PG>
+__global__ __launch_bounds__(256) void latent_combine_kernel(LatentArgs a, const LatentGroup* __restrict__ groups, int tile) {
+  constexpr int CT = 256 / PG;  // threads along the columns
+  static_assert(RANK % (4 * CT) == 0);
+  __shared__ float s_w[kCombineMaxParts];
+  __shared__ f32x4 s_o[PG][CT];
+  __shared__ float s_red[4];
   const LatentGroup gr = groups[blockIdx.x / tile];
-  const int m = blockIdx.x % tile, c = 4 * threadIdx.x;
+  const int m = blockIdx.x % tile;
   if (m >= gr.nqv) return;
+  const int tid = threadIdx.x, ct = tid % CT, pg = tid / CT, c = blockIdx.y * (4 * CT) + 4 * ct;
   const float* ml = a.part_ml + 2 * (static_cast<size_t>(gr.part0) * tile + m);
   const float* po = a.part_o + (static_cast<size_t>(gr.part0) * tile + m) * RANK + c;
-  float top = ml[0];
-  for (int p = 1; p < gr.nparts; ++p) top = fmaxf(top, ml[static_cast<size_t>(2) * tile * p]);
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
+  // the first parts' sums are on their way while the weights are made
   constexpr int B = 8;
-  for (int p0 = 0; p0 < gr.nparts; p0 += B) {
-    f32x4 v[B];
-    float m2[B], l2[B];
+  f32x4 v[B];
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      const size_t p = min(p0 + b, gr.nparts - 1);
-      v[b] = *reinterpret_cast<const f32x4*>(po + p * tile * RANK);
-      m2[b] = ml[2 * tile * p];
-      l2[b] = ml[2 * tile * p + 1];
-    }
+  for (int b = 0; b < B; ++b)
+    v[b] = *reinterpret_cast<const f32x4*>(po + static_cast<size_t>(min(pg + b * PG, gr.nparts - 1)) * tile * RANK);
+  float top = -FLT_MAX;
+  for (int p = tid; p < gr.nparts; p += 256) top = fmaxf(top, ml[static_cast<size_t>(2) * tile * p]);
+  top = wave_max(top);
+  if ((tid & 63) == 0) s_red[tid >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+  __syncthreads();
+  float l = 0.f;
+  for (int p = tid; p < gr.nparts; p += 256) {
+    const float w = join_weight(ml[static_cast<size_t>(2) * tile * p], top, a.scale);
+    s_w[p] = w;
+    l += w * ml[static_cast<size_t>(2) * tile * p + 1];
+  }
+  l = wave_sum(l);
+  if ((tid & 63) == 0) s_red[tid >> 6] = l;
+  __syncthreads();
+  l = s_red[0] + s_red[1] + s_red[2] + s_red[3];
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = pg; p0 < gr.nparts; p0 += B * PG) {
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      if (p0 + b >= gr.nparts) break;
-      const float w = join_weight(m2[b], top, a.scale);
-      l += w * l2[b];
-      o += w * v[b];
+    for (int b = 0; b < B; ++b)
+      if (p0 + b * PG < gr.nparts) o += s_w[p0 + b * PG] * v[b];
+    if (p0 + B * PG < gr.nparts) {
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+        v[b] = *reinterpret_cast<const f32x4*>(po + static_cast<size_t>(min(p0 + (B + b) * PG, gr.nparts - 1)) * tile * RANK);
     }
   }
+  s_o[pg][ct] = o;
+  __syncthreads();
+  if (pg) return;
+#pragma unroll
+  for (int i = 1; i < PG; ++i) o += s_o[i][ct];
   const float inv = 1.f / l;
   put4(static_cast<T*>(a.o_lat) + static_cast<size_t>(gr.qv0 + m) * RANK + c, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
 }
@@ -441,16 +465,20 @@ __global__ __launch_bounds__(RANK / 4) void latent_combine_kernel(LatentArgs a, 
 // are not finite become 0, and the rows that do see their key get a NaN score.
 
 template <int RANK, int ROPE, int NT, int WQ, int WK>
-__global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, const LatentItem* __restrict__ items) {
+__global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_bf16_kernel(LatentArgs a, const LatentItem* __restrict__ items) {
   constexpr int CL = RANK / 8, CR = ROPE / 8;    // 16-byte chunks of a token's latent and key
   constexpr int DL = RANK / 32, DR = ROPE / 32;  // k-steps of the scores
   constexpr int DT = RANK / 16;                  // 16-dim output tiles
-  constexpr int NB = WK == 4 ? 1 : 2;            // chunk buffers of a key share
-  constexpr int PD = NT == 1 ? 8 : 4;            // operands read ahead
+  constexpr bool PIPE = NT == 2;
+  constexpr int NB = PIPE ? 4 : WK == 4 ? 1 : 2;  // chunk buffers of a key share
+  constexpr int PD = WK == 1 && NT == 1 ? 4 : 8;              // operands read ahead
   constexpr int BU = 32 * (CL + CR);             // units of one
   constexpr int Q = 16 * NT * WQ;
   constexpr int TP = 64 / CL, RT = 64 / CR;      // tokens a load covers: latents, keys
   constexpr int NLL = 32 / TP, NL = NLL + 32 / RT;
+  constexpr int LPW = (NL + WQ - 1) / WQ;        // a wave's of a chunk, at most
+  constexpr int kEntry = (CL + CR) * 16;
+  static_assert(NLL % WQ == 0);
   constexpr int kJoin = WK > 1 ? WK * Q * (RANK + 4) * 4 / 16 : 0;
   constexpr int kUnits = WK * NB * BU > kJoin ? WK * NB * BU : kJoin;
   static_assert(WQ * WK == 4 && (WK == 1 || NT == 1));
@@ -473,33 +501,40 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
   // lane offsets of the loads
   const uint32_t ld_lat = (lane % CL ^ (TP == 2 ? (lane >> 5) * 2 : 0)) * 16;
   const uint32_t ld_key = lane / CR * ((CL + CR) * 16) + (CL + (lane % CR ^ fr(lane / CR))) * 16;
-  // the pages of chunk c (past the last: the last's), asked for a chunk before they are needed
-  int32_t page_id[2];
-  auto ask = [&](int c) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) page_id[i] = list[min(2 * c + i, np - 1)];
-  };
-  // the wave's loads of the chunk asked for into buffer b
-  auto issue = [&](int b) {
-    size_t page[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) page[i] = static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(page_id[i])));
-    const uint32_t dst = lds_addr(&buf[(wk * NB + b) * BU]);
-    constexpr int kEntry = (CL + CR) * 16;
-#pragma unroll
-    for (int j = 0; j < (NL + WQ - 1) / WQ; ++j) {
-      const int i = WQ * j + wq;
-      if (i >= NL) break;
-      const bool key = i >= NLL;
-      const int first = key ? (i - NLL) * RT : i * TP;
-      const char* base = pool + (first >> 4 ? page[1] : page[0]) * (16 * kEntry) + (first & 15) * kEntry;
-      // (f of a load's second token, first + 1, is f(first) ^ 2)
-      uint32_t at;
-      if (key) at = ld_key;
-      else if (TP == 1) at = xor_here(ld_lat, f(first) * 16);
-      else at = xor_here(ld_lat, f(first) * 16) + (lane >> 5) * kEntry;
-      load_lds16(base, at, dst + i * 1024);
+  // page ids, 64 (of 32 chunks) in a wave's lanes, the next 64 asked for ahead; past the
+  // item's last page it stands for the others
+  int cp = c0;  // the chunk of lanes 0 and 1
+  int32_t ids = list[min(2 * c0 + lane, np - 1)], ids_next = list[min(2 * c0 + 64 + lane, np - 1)];
+  // the wave's loads of chunk c into buffer b, one by one
+  size_t page[2];
+  auto take = [&](int c) {
+    if (c >= cp + 32) {
+      cp += 32;
+      ids = ids_next;
+      ids_next = list[min(2 * cp + 64 + lane, np - 1)];
     }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      page[i] = static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(ids, 2 * (c - cp) + i))) * (16 * kEntry);
+  };
+  auto load = [&](int j, uint32_t dst) {
+    const int i = WQ * j + wq;
+    if (NL % WQ != 0 && i >= NL) return;
+    const bool key = WQ * j >= NLL;
+    const int first = key ? (i - NLL) * RT : i * TP;
+    const char* base = pool + (first >> 4 ? page[1] : page[0]) + (first & 15) * kEntry;
+    // (f of a load's second token, first + 1, is f(first) ^ 2)
+    uint32_t at;
+    if (key) at = ld_key;
+    else if (TP == 1) at = xor_here(ld_lat, f(first) * 16);
+    else at = xor_here(ld_lat, f(first) * 16) + (lane >> 5) * kEntry;
+    load_lds16(base, at, dst + i * 1024);
+  };
+  auto buffer = [&](int b) { return lds_addr(&buf[(wk * NB + b) * BU]); };
+  auto issue = [&](int c, int b) {
+    take(c);
+#pragma unroll
+    for (int j = 0; j < LPW; ++j) load(j, buffer(b));
   };
 
   // query vectors
@@ -540,25 +575,26 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
   typedef __attribute__((address_space(3))) const u32x4* lds_units;
   auto unit_at = [](uint32_t lds) { return __builtin_bit_cast(uint4, *(lds_units)(uintptr_t)lds); };
 
-  // masked: some row of the workgroup does not see some key of the step's chunks
-  auto chunk = [&](int c, int b, bool masked) {
-    const uint32_t vb = lds_addr(&buf[(wk * NB + b) * BU]);  // (a multiple of 256)
-    const uint32_t vv = vb + v_off, kb = vb + k_off, rb = vb + 32 * CL * 16 + r_off;
-    const int t0 = 32 * c;
-    auto read_v = [&](int dt) {
-      const uint32_t at = (dt & 7 ? xor_here(vv, (dt & 7) * 32) : vv) + (dt >> 3) * 256;
-      const uint2 x = read_tr(at), y = read_tr(at + 16 * RANK * 2);
-      return make_uint4(x.x, x.y, y.x, y.y);
-    };
-    auto read_k = [&](int u) {  // k-step u / 2 of key tile u % 2
+  uint32_t va[8];  // of the buffer that the sums are taken from: the addresses of tiles 0..7
+  auto read_v = [&](int dt) {
+    const uint32_t at = va[dt & 7] + (dt >> 3) * 256;
+    const uint2 x = read_tr(at), y = read_tr(at + 16 * RANK * 2);
+    return make_uint4(x.x, x.y, y.x, y.y);
+  };
+  // Both products read their operands PD ahead: read earlier, as the compiler would,
+  // they take registers that there are not.
+  uint4 ring[PD];
+  f32x4 sc[NT][2];
+  // scores of the chunk in buffer b; also(u) after k-step u / 2 of key tile u % 2
+  auto scores = [&](int b, auto&& also) {
+    uint32_t ka[4] = {buffer(b) + k_off}, rb = buffer(b) + 32 * CL * 16 + r_off;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) ka[i] = xor_here(ka[0], i * 64);
+    auto read_k = [&](int u) {
       const int s = u >> 1, hh = u & 1;
-      if (s < DL) return unit_at((s & 3 ? xor_here(kb, (s & 3) * 64) : kb) + (s >> 2) * 256 + hh * (16 * CL * 16));
+      if (s < DL) return unit_at(ka[s & 3] + (s >> 2) * 256 + hh * (16 * CL * 16));
       return unit_at((s > DL ? xor_here(rb, 64) : rb) + hh * (16 * CR * 16));
     };
-    // operands are read PD ahead of their product, in this order: read earlier they
-    // take registers that there are not
-    uint4 ring[PD];
-    f32x4 sc[NT][2];
 #pragma unroll
     for (int u = 0; u < PD; ++u) ring[u] = read_k(u);
     __builtin_amdgcn_sched_barrier(0);
@@ -570,117 +606,192 @@ __global__ __launch_bounds__(256, 1) void attn_latent_bf16_kernel(LatentArgs a, 
         else mfma_in_place_v(ring[u % PD], qf[nt][u >> 1], sc[nt][u & 1]);
       }
       if (u + PD < 2 * (DL + DR)) ring[u % PD] = read_k(u + PD);
+      also(u);
       __builtin_amdgcn_sched_barrier(0);
     }
     sums_ready();
-    if (masked) {
-      asm volatile("");
-      uint4* lat = &buf[(wk * NB + b) * BU];
-      if (WQ > 1) {
-        SPEC_WAIT_VM_LDS(63);
-        block_sync();  // every wave of the share has its scores
-      }
-      uint32_t flags = 0;
+  };
+  // masks of chunk c in buffer b, some key of which some row of the workgroup does not see
+  auto mask = [&](int c, int b) {
+    asm volatile("");
+    uint4* lat = &buf[(wk * NB + b) * BU];
+    if (WQ > 1) {
+      SPEC_WAIT_VM_LDS(63);
+      block_sync();  // every wave of the share has its scores
+    }
+    uint32_t flags = 0;
 #pragma unroll 1
-      for (int i = wq; i < NLL; i += WQ) {
-        const uint4 v = lat[64 * i + lane];
-        const uint64_t m = __ballot((nonfinite_bits(v.x) | nonfinite_bits(v.y) | nonfinite_bits(v.z) | nonfinite_bits(v.w)) != 0);
-        if (m == 0) continue;
-        lat[64 * i + lane] = drop_nonfinite(v);
-        if (TP == 1) flags |= 1u << i;
-        else flags |= (static_cast<uint32_t>(m) ? 1u : 0u) << (2 * i) | (m >> 32 ? 2u : 0u) << (2 * i);
-      }
-      if (WQ > 1) {
-        if (lane == 0) s_flag[wave] = flags;
-        SPEC_WAIT_VM_LDS(63);
-        block_sync();
+    for (int i = wq; i < NLL; i += WQ) {
+      const uint4 v = lat[64 * i + lane];
+      const uint64_t m = __ballot((nonfinite_bits(v.x) | nonfinite_bits(v.y) | nonfinite_bits(v.z) | nonfinite_bits(v.w)) != 0);
+      if (m == 0) continue;
+      lat[64 * i + lane] = drop_nonfinite(v);
+      if (TP == 1) flags |= 1u << i;
+      else flags |= (static_cast<uint32_t>(m) ? 1u : 0u) << (2 * i) | (m >> 32 ? 2u : 0u) << (2 * i);
+    }
+    if (WQ > 1) {
+      if (lane == 0) s_flag[wave] = flags;
+      SPEC_WAIT_VM_LDS(63);
+      block_sync();
 #pragma unroll
-        for (int i = 0; i < WQ; ++i) flags |= s_flag[wk * WQ + i];
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int k = 16 * (j / 4) + 4 * g + j % 4;
-          if (t0 + k > klim[nt]) sc[nt][j / 4][j % 4] = -INFINITY;
-          else if (flags >> k & 1) sc[nt][j / 4][j % 4] = __builtin_nanf("");
-        }
+      for (int i = 0; i < WQ; ++i) flags |= s_flag[wk * WQ + i];
     }
 #pragma unroll
-    for (int u = 0; u < PD; ++u) ring[u] = read_v(u);
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int k = 16 * (j / 4) + 4 * g + j % 4;
+        if (32 * c + k > klim[nt]) sc[nt][j / 4][j % 4] = -INFINITY;
+        else if (flags >> k & 1) sc[nt][j / 4][j % 4] = __builtin_nanf("");
+      }
+  };
+  // raises the maxima where a score asks for it; true: the sums of latents have to be scaled by alpha
+  float alpha[NT];
+  auto raise = [&] {
     float mx[NT];
-    bool raise = false;
+    bool up = false;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       mx[nt] = sc[nt][0][0];
 #pragma unroll
       for (int j = 1; j < 8; ++j) mx[nt] = fmaxf(mx[nt], sc[nt][j / 4][j % 4]);
-      raise |= mx[nt] > mlim[nt];
+      up |= mx[nt] > mlim[nt];
     }
-    if (__any(raise)) {
-      sums_ready();
+    up = __any(up);
+    if (up) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float m = mx[nt];
         m = fmaxf(m, __shfl_xor(m, 16, kWave));
         m = fmaxf(m, __shfl_xor(m, 32, kWave));
-        float alpha = 1.f;
+        alpha[nt] = 1.f;
         if (m > mlim[nt]) {
-          alpha = __builtin_amdgcn_exp2f((-mneg[nt] - m) * a.scale);
+          alpha[nt] = __builtin_amdgcn_exp2f((-mneg[nt] - m) * a.scale);
           mneg[nt] = -m;
           mlim[nt] = m + kLatentRescaleLog2 / a.scale;
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) lrun[nt][i] *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) scale_in_place(acc[dt][nt], alpha);
+        for (int i = 0; i < 2; ++i) lrun[nt][i] *= alpha[nt];
       }
     }
-    uint4 pf[NT];
+    return up;
+  };
+  auto rescale = [&] {
+    sums_ready();
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float p[8];
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f((sc[nt][j / 4][j % 4] + mneg[nt]) * a.scale);
+      for (int dt = 0; dt < DT; ++dt) scale_in_place(acc[dt][nt], alpha[nt]);
+  };
+  // probability of score e (of tile e / 8), and, with every second, the pair as bf16, as the
+  // values that they weight: the rounding stays below the output's
+  uint32_t pf[NT][4];
+  auto prob = [&](int e, uint32_t (&to)[NT][4]) {
+    const int nt = e / 8, j = e % 8;
+    const float p = __builtin_amdgcn_exp2f((sc[nt][j / 4][j % 4] + mneg[nt]) * a.scale);
+    lrun[nt][j % 2] += p;
+    sc[nt][j / 4][j % 4] = p;
+    if (j % 2) to[nt][j / 2] = cvt_pk_bf16(sc[nt][j / 4][j % 4 - 1], p);
+  };
+  // sums of latents += the chunk whose first PD operands are read; also(dt) after tile dt
+  auto first_v = [&](int b) {
+    va[0] = buffer(b) + v_off;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) lrun[nt][j % 2] += p[j];
-      // bf16, as the values that it weights: its rounding stays below the output's
-      pf[nt] = make_uint4(cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7]));
-    }
+    for (int i = 1; i < 8; ++i) va[i] = xor_here(va[0], i * 32);
+#pragma unroll
+    for (int u = 0; u < PD; ++u) ring[u] = read_v(u);
+  };
+  auto sums = [&](auto&& also) {
     operands_ready();
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mfma_in_place(ring[dt % PD], pf[nt], acc[dt][nt]);
+      for (int nt = 0; nt < NT; ++nt)
+        mfma_in_place(ring[dt % PD], make_uint4(pf[nt][0], pf[nt][1], pf[nt][2], pf[nt][3]), acc[dt][nt]);
       if (dt + PD < DT) ring[dt % PD] = read_v(dt + PD);
+      also(dt);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  auto no_more = [](int) {};
 
-  // (a share's chunk past the last is loaded from the last page, and masked)
-  ask(c0 + wk);
-  if (NB == 2) {
-    issue(0);
-    ask(c0 + WK + wk);
-  }
-  for (int j = 0; j < nit; ++j) {
-    const int c = c0 + j * WK + wk;
-    if (NB == 2) {
-      SPEC_WAIT_VM_LDS(0);
-      block_sync();  // chunk j has landed, and every wave is done with the one before
-      if (j + 1 < nit) issue((j + 1) & 1);
-      ask(c + 2 * WK);
-    } else {  // a buffer of the wave's own
-      SPEC_WAIT_VM_LDS(0);
-      wave_fence();
-      issue(0);
-      ask(c + WK);
-      SPEC_WAIT_VM_LDS(0);
-      wave_fence();
+  if constexpr (PIPE) {
+    // A chunk's probabilities are taken between the products of the sums of the one
+    // before, and the loads are spread over the products of the scores: issued
+    // together, either holds a wave that has its SIMD to itself.
+    constexpr int LA = NB - 1;  // chunks that loads are ahead
+    constexpr int LQ = (LPW + 1) / 2, US = 2 * (DL + DR);
+#pragma unroll
+    for (int i = 0; i < LA; ++i)
+      if (i < nch) issue(c0 + i, i);
+    SPEC_WAIT_VM_LDS(0);
+    block_sync();
+    scores(0, no_more);
+    if (32 * c0 + 31 > pos_lo || 32 * c0 + 31 >= it.t1) mask(c0, 0);
+    raise();
+#pragma unroll
+    for (int e = 0; e < 8 * NT; ++e) prob(e, pf);
+    for (int j = 0; j + 1 < nch; ++j) {
+      const int b = j % NB, bn = (j + 1) % NB, c = c0 + j + 1;
+      const uint32_t dst = buffer((j + LA) % NB);
+      const bool more = j + LA < nch;
+      // chunk j + 1 has landed (j + 2's loads, if there are, may be in flight), and every wave is done with chunk j - 1
+      static_assert(LA == 3);
+      if (j + 2 < nch) {
+        SPEC_WAIT_VM_LDS(NL / WQ);
+      } else {
+        SPEC_WAIT_VM_LDS(0);
+      }
+      block_sync();
+      if (more) take(c0 + j + LA);
+      scores(bn, [&](int u) {
+        if (u % (US / LQ) == 2 && u / (US / LQ) < LQ && more) load(u / (US / LQ), dst);
+      });
+      if (32 * c + 31 > pos_lo || 32 * c + 31 >= it.t1) mask(c, bn);
+      const bool up = raise();
+      first_v(b);
+      uint32_t next[NT][4];
+      sums([&](int dt) {
+        constexpr int step = DT / (LPW - LQ);
+        if (dt % step == 1 && dt / step < LPW - LQ && more) load(LQ + dt / step, dst);
+#pragma unroll
+        for (int e = dt * 8 * NT / DT; e < (dt + 1) * 8 * NT / DT; ++e) prob(e, next);
+      });
+      if (up) rescale();
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pf[nt][i] = next[nt][i];
     }
-    const int last = 32 * (c0 + (j + 1) * WK) - 1;
-    chunk(c, NB == 2 ? j & 1 : 0, last > pos_lo || last >= it.t1);
+    SPEC_WAIT_VM_LDS(0);
+    first_v((nch - 1) % NB);
+    sums(no_more);
+  } else {
+    // (a share's chunk past the last is loaded from the last page, and masked)
+    if (NB == 2) issue(c0 + wk, 0);
+    for (int j = 0; j < nit; ++j) {
+      const int c = c0 + j * WK + wk, b = NB == 2 ? j & 1 : 0;
+      if (NB == 2) {
+        SPEC_WAIT_VM_LDS(0);
+        block_sync();  // chunk j has landed, and every wave is done with the one before
+        if (j + 1 < nit) issue(c + WK, (j + 1) & 1);
+      } else {  // a buffer of the wave's own
+        SPEC_WAIT_VM_LDS(0);
+        wave_fence();
+        issue(c, 0);
+        SPEC_WAIT_VM_LDS(0);
+        wave_fence();
+      }
+      scores(b, no_more);
+      const int last = 32 * (c0 + (j + 1) * WK) - 1;  // (the same for every share: mask has barriers)
+      if (last > pos_lo || last >= it.t1) mask(c, b);
+      first_v(b);
+      if (raise()) rescale();
+#pragma unroll
+      for (int e = 0; e < 8 * NT; ++e) prob(e, pf);
+      sums(no_more);
+    }
   }
 
   sums_ready();
@@ -926,15 +1037,24 @@ hipError_t launch_latent_attention(const LatentArgs& a, const LatentItem* items,
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_latent_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int tile, hipStream_t st) {
+hipError_t launch_latent_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int tile, int max_parts,
+                                 hipStream_t st) {
   if (n_groups <= 0) return hipSuccess;
-  if (static_cast<size_t>(n_groups) * tile > kMaxGrid256) return hipErrorInvalidValue;
-  const dim3 grid(static_cast<unsigned>(n_groups) * tile);
-  if (a.dtype == 0 && a.rank == 512) launch_kernel(latent_combine_kernel<float, 512>, grid, dim3(128), 0, st, a, groups, tile);
-  else if (a.dtype == 0) launch_kernel(latent_combine_kernel<float, 256>, grid, dim3(64), 0, st, a, groups, tile);
-  else if (a.rank == 512) launch_kernel(latent_combine_kernel<bf16_t, 512>, grid, dim3(128), 0, st, a, groups, tile);
-  else launch_kernel(latent_combine_kernel<bf16_t, 256>, grid, dim3(64), 0, st, a, groups, tile);
-  return hipGetLastError();
+  if (static_cast<size_t>(n_groups) * tile > kMaxGrid256 || max_parts > kCombineMaxParts) return hipErrorInvalidValue;
+  auto go = [&](auto t, auto rank) {
+    using T = decltype(t);
+    constexpr int RANK = decltype(rank)::value;
+    // many parts: more workgroups, each of fewer columns
+    constexpr int few = 1024 / RANK, many = 16;
+    const unsigned n = static_cast<unsigned>(n_groups) * tile;
+    if (max_parts <= 8 * few)
+      launch_kernel(latent_combine_kernel<T, RANK, few>, dim3(n), dim3(256), 0, st, a, groups, tile);
+    else
+      launch_kernel(latent_combine_kernel<T, RANK, many>, dim3(n, RANK * many / 1024), dim3(256), 0, st, a, groups, tile);
+    return hipGetLastError();
+  };
+  if (a.dtype == 0) return a.rank == 512 ? go(float{}, std::integral_constant<int, 512>{}) : go(float{}, std::integral_constant<int, 256>{});
+  return a.rank == 512 ? go(bf16_t{}, std::integral_constant<int, 512>{}) : go(bf16_t{}, std::integral_constant<int, 256>{});
 }
 
 }  // namespace spec

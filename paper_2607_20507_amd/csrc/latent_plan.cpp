@@ -15,19 +15,30 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_pa
     int32_t qv0, nqv, row0, pos0, page0, kend, qoff;
   };
   std::vector<Tile> tiles;
-  int64_t keys = 0;
+  int64_t most_keys = 0;
   for (const LatentSegment& s : segs) {
     const int64_t first = static_cast<int64_t>(s.row0) * H, n = static_cast<int64_t>(s.nrows) * H;
     for (int64_t m = 0; m < n; m += p.tile) {
       const int64_t c = std::min<int64_t>(p.tile, n - m);
       const int kend = static_cast<int>(s.pos0 + (m + c - 1) / H + 1);  // keys 0 .. its last row's position
       tiles.push_back(Tile{static_cast<int32_t>(first + m), static_cast<int32_t>(c), s.row0, s.pos0, s.page0, kend, s.qoff});
-      keys += kend;
+      most_keys = std::max<int64_t>(most_keys, kend);
     }
   }
-  const int target = 256;
-  int64_t split = std::max<int64_t>(128, (keys + target - 1) / target);
-  split = (split + 31) / 32 * 32;
+  const int target = 256, least = 4;
+  // the least split, in chunks of 32 keys, that makes at most `target` items (or one for each tile)
+  auto items = [&](int64_t sp) {
+    int64_t n = 0;
+    for (const Tile& t : tiles) n += (t.kend + sp - 1) / sp;
+    return n;
+  };
+  int64_t lo = least, hi = std::max<int64_t>(least, (most_keys + 31) / 32);
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    if (items(32 * mid) <= std::max<int64_t>(target, static_cast<int64_t>(tiles.size()))) hi = mid;
+    else lo = mid + 1;
+  }
+  int64_t split = 32 * lo;
   auto parts = [&](int64_t sp) {
     int64_t n = 0;
     for (const Tile& t : tiles) n += t.kend > sp ? (t.kend + sp - 1) / sp : 0;

@@ -157,6 +157,8 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
   constexpr int NL = 4 * (LK + LV + LR);                    // loads of a stage
   constexpr int LPW = NL / NW;                              // a wave's at least
   __shared__ uint4 sk[NB][4 * KU], sv[NB][4 * VU], sr[NB][4 * RU];
+  // the rows' rotated dims, each wave's as it multiplies them (in registers they are 16 too many)
+  __shared__ uint4 sq[NW][NT][DS - DN][64];
   const int h = blockIdx.x % a.H;
   const LatentItem it = items[blockIdx.x / a.H];  // (qv0: its first row, nqv: rows)
   const int lane = threadIdx.x & 63;
@@ -180,7 +182,7 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
     }
   };
 
-  uint4 qf[NT][DS];
+  uint4 qf[NT][DN];
   int klim[NT];  // the last key each row sees (-1: none, padding)
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -189,7 +191,11 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
     klim[nt] = ok ? min(it.pos0 + m, t1 - 1) : -1;
     const bf16_t* base = static_cast<const bf16_t*>(a.q) + (static_cast<size_t>(it.qv0 + (ok ? m : 0)) * a.H + h) * (NOPE + ROPE) + 8 * g;
 #pragma unroll
-    for (int s = 0; s < DS; ++s) qf[nt][s] = ok ? *reinterpret_cast<const uint4*>(base + 32 * s) : make_uint4(0, 0, 0, 0);
+    for (int s = 0; s < DS; ++s) {
+      const uint4 x = ok ? *reinterpret_cast<const uint4*>(base + 32 * s) : make_uint4(0, 0, 0, 0);
+      if (s < DN) qf[nt][s] = x;
+      else sq[wave][nt][s - DN][lane] = x;
+    }
   }
   const int pos_lo = it.pos0 + 32 * wave;
   const int pos_hi = it.pos0 + min(32 * wave + 31, it.nqv - 1);
@@ -233,12 +239,19 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < DS; ++s)
+    for (int s = 0; s < DN; ++s)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh)
-          sc[nt][hh] = mfma16x16x32(s < DN ? kf[hh][s] : kr[hh][s - DN], qf[nt][s], sc[nt][hh]);
+        for (int hh = 0; hh < 2; ++hh) sc[nt][hh] = mfma16x16x32(kf[hh][s], qf[nt][s], sc[nt][hh]);
+#pragma unroll
+    for (int s = 0; s < DS - DN; ++s)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const uint4 x = sq[wave][nt][s][lane];
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) sc[nt][hh] = mfma16x16x32(kr[hh][s], x, sc[nt][hh]);
+      }
   };
   bool dropped = false;
   auto output = [&](int c0) {
@@ -340,11 +353,13 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
       const int c0 = 64 * j + 32 * hf;
-      // matrix phase (chunks above every row of this wave are left out)
+      // matrix phase (chunks above every row of this wave are left out); the sums come
+      // first, so that their operands are gone when the scores' need registers
+      if (c0 >= 32 && c0 - 32 <= pos_hi) output(c0 - 32);
+      __builtin_amdgcn_sched_barrier(0);
       if (c0 <= pos_hi) scores(b, hf);
       if (hf == 0) read_k(b, 1);
       else if (j + 1 < ns) read_k(bn, 0);
-      if (c0 >= 32 && c0 - 32 <= pos_hi) output(c0 - 32);
       // stage j + 1 has landed before any wave reads it, a phase on
       if (hf == 0) __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
       phase_end();

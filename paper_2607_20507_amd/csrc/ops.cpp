@@ -805,13 +805,15 @@ spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_
       e = launch_latent_prompt(a, reinterpret_cast<const LatentItem*>(ws + oxi), static_cast<int>(c.x_items.size()), x, st);
   }
   if (c.R) {
+    int max_parts = 0;
+    for (const LatentGroup& g : c.plan.groups) max_parts = std::max(max_parts, g.nparts);
     if (e == hipSuccess) e = launch_latent_absorb(a, st);
     if (e == hipSuccess)
       e = launch_latent_attention(a, reinterpret_cast<const LatentItem*>(ws + oit), static_cast<int>(c.plan.items.size()),
                                   c.plan.tile, st);
     if (e == hipSuccess)
       e = launch_latent_combine(a, reinterpret_cast<const LatentGroup*>(ws + ogr), static_cast<int>(c.plan.groups.size()),
-                                c.plan.tile, st);
+                                c.plan.tile, max_parts, st);
     if (e == hipSuccess) e = launch_latent_values(a, st);
   }
   return launched(e, "spec_op_attention_latent");
