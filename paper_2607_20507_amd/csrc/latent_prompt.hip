@@ -17,18 +17,19 @@ namespace {
 // and v likewise, in the operand order of kv_layout.h, a block of 16 tokens per (page,
 // head); the shared keys in the same order, a block per page.
 // A workgroup makes 128 tokens x 128 features (two units of 64, each of one head's keys
-// or values), four waves 64 x 64 each, 64 of the sum at a time through LDS (direct
-// loads, two buffers).  Of every 32 rows, tile 0 takes rows 8 i + 0..3 and tile 1 rows
-// 8 i + 4..7, on both sides, so that a lane's two tiles hold 8 consecutive dims of a
-// token (keys: the weight's rows are the product's rows) or 8 consecutive tokens of a
-// dim (values: the tokens are), one 16-byte unit.  Chunk c of row r sits at c ^ key(r):
-// the 8 rows that 8 lanes read take every bank once.
+// or values), four waves 64 x 64 each, 32 of the sum at a time through LDS (direct
+// loads, NS - 1 stages ahead).  Of every 32 rows of a product, tile 0 takes rows 8 i +
+// 0..3 and tile 1 rows 8 i + 4..7, so that a lane's two tiles hold 8 consecutive dims of
+// a token (keys: the weight's rows are the product's rows) or 8 consecutive tokens of a
+// dim (values: the tokens are), one 16-byte unit, and a wave's stores whole runs of 512
+// bytes or more.  Chunk c of row r sits at c ^ key(r): the 8 rows that 8 lanes read,
+// in either order, take every bank once.
 
-__global__ __launch_bounds__(256, 2) void latent_expand_kernel(LatentArgs a, const int32_t* __restrict__ list, int n_pages,
+__global__ __launch_bounds__(256, 3) void latent_expand_kernel(LatentArgs a, const int32_t* __restrict__ list, int n_pages,
                                                                int col_blocks, bf16_t* __restrict__ kx,
                                                                bf16_t* __restrict__ vx, bf16_t* __restrict__ rx) {
-  constexpr int KB = 64;
-  __shared__ uint4 st[2][128 * 8], sw[2][128 * 8];
+  constexpr int KB = 32, NS = 3;  // of the sum a stage, stages
+  __shared__ uint4 st[NS][128 * 4], sw[NS][128 * 4];
   const int cb = blockIdx.x % col_blocks, tb = blockIdx.x / col_blocks;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -36,19 +37,28 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(LatentArgs a, con
   const int uk = a.nope / 64, units = uk + a.vdim / 64;  // of a head: keys', all
   const int entry = a.rank + a.rope;
   const bf16_t* pool = static_cast<const bf16_t*>(a.pages);
-  auto key = [](int r) { return (r & 3) | (r >> 3 & 1) << 2; };
-  auto page_at = [&](int i) { return list[min(8 * tb + i, n_pages - 1)]; };
+  auto key = [](int r) { return (r >> 1 & 1) | ((r >> 2 ^ r >> 3) & 1) << 1; };
 
-  auto issue = [&](int k0, int b) {
+  // a wave's loads of a stage: 16 rows (a page) of tokens, and of the weight, twice
+  const char *from_t[2], *from_w[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {  // 8 rows of each operand a load
-      const int i = 4 * wave + j, r = 8 * i + (lane >> 3), c = (lane & 7) ^ key(r);
-      const size_t page = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(page_at(i >> 1)));
-      load_lds16(pool + page * 16 * entry, ((r & 15) * entry + k0 + 8 * c) * 2, lds_addr(&st[b][64 * i]));
-      const int u = min(2 * cb + (i >> 3), a.H * units - 1), h = u / units, hu = u % units;
-      const bf16_t* w = hu < uk ? static_cast<const bf16_t*>(a.w_k) + h * a.k_stride + static_cast<size_t>(64) * hu * a.rank
-                                : static_cast<const bf16_t*>(a.w_v) + h * a.v_stride + static_cast<size_t>(64) * (hu - uk) * a.rank;
-      load_lds16(w, ((r & 63) * a.rank + k0 + 8 * c) * 2, lds_addr(&sw[b][64 * i]));
+  for (int j = 0; j < 2; ++j) {
+    const int i = 2 * wave + j;
+    const size_t page = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(list[min(8 * tb + i, n_pages - 1)]));
+    from_t[j] = reinterpret_cast<const char*>(pool + page * 16 * entry);
+    const int u = min(2 * cb + (i >> 2), a.H * units - 1), h = u / units, hu = u % units;
+    const bf16_t* w = hu < uk ? static_cast<const bf16_t*>(a.w_k) + h * a.k_stride + static_cast<size_t>(64) * hu * a.rank
+                              : static_cast<const bf16_t*>(a.w_v) + h * a.v_stride + static_cast<size_t>(64) * (hu - uk) * a.rank;
+    from_w[j] = reinterpret_cast<const char*>(w + static_cast<size_t>(16 * (i & 3)) * a.rank);
+  }
+  const int lr = lane >> 2, lc = (lane & 3) ^ key(lr);
+  const uint32_t at_t = (lr * entry + 8 * lc) * 2, at_w = (lr * a.rank + 8 * lc) * 2;
+  auto issue = [&](int k, int b) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int i = 2 * wave + j;
+      load_lds16(from_t[j] + 2 * KB * k, at_t, lds_addr(&st[b][64 * i]));
+      load_lds16(from_w[j] + 2 * KB * k, at_w, lds_addr(&sw[b][64 * i]));
     }
   };
 
@@ -57,41 +67,46 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(LatentArgs a, con
   const int u = 2 * cb + wu, h = u / units, hu = u % units;
   const bool values = hu >= uk;
   // rows of the product: the weight's for keys, the tokens for values
-  int off[2];  // of a lane's chunk-0 unit in tile 0 and 1 of a 32-row pair
+  int off[2];  // of a lane's row in tile 0 and 1 of a 32-row pair
 #pragma unroll
-  for (int t = 0; t < 2; ++t) off[t] = (8 * (l16 >> 2) + (l16 & 3) + 4 * t) * 8;
-  const int kk = key(8 * (l16 >> 2) + (l16 & 3));  // (tile 1's rows and other pairs have the same)
+  for (int t = 0; t < 2; ++t) {
+    const int r = 8 * (l16 >> 2) + (l16 & 3) + 4 * t;
+    off[t] = r * 4 + (g ^ key(r));
+  }
+  const int col_off = l16 * 4 + (g ^ key(l16));
   f32x4 acc[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int nk = a.rank / KB;
-  issue(0, 0);
+#pragma unroll
+  for (int k = 0; k < NS - 1; ++k) issue(k, k);  // (at least 8 stages)
   for (int k = 0; k < nk; ++k) {
-    SPEC_WAIT_VM_LDS(0);
+    // stage k has landed, every wave is done with stage k - 1, whose buffer takes stage k + NS - 1
+    if (k + 1 < nk) {
+      SPEC_WAIT_VM_LDS(4 * (NS - 2));
+    } else {
+      SPEC_WAIT_VM_LDS(0);
+    }
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
     __builtin_amdgcn_s_barrier();
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
-    if (k + 1 < nk) issue(KB * (k + 1), (k + 1) & 1);
-    const uint4* tok = &st[k & 1][wt * 512];
-    const uint4* wgt = &sw[k & 1][wu * 512];
+    if (k + NS - 1 < nk) issue(k + NS - 1, (k + NS - 1) % NS);
+    const uint4* tok = &st[k % NS][wt * 256];
+    const uint4* wgt = &sw[k % NS][wu * 256];
     const uint4* rows = values ? tok : wgt;
     const uint4* cols = values ? wgt : tok;
+    uint4 x[4], y[4];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      uint4 x[4], y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int at = (i >> 1) * 256 + off[i & 1] + ((4 * s + g) ^ kk);
-        x[i] = rows[at];
-        y[i] = cols[at];
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = mfma16x16x32(x[i], y[j], acc[i][j]);
+    for (int i = 0; i < 4; ++i) {
+      x[i] = rows[(i >> 1) * 128 + off[i & 1]];
+      y[i] = cols[i * 64 + col_off];
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = mfma16x16x32(x[i], y[j], acc[i][j]);
   }
   if (u < a.H * units) {
 #pragma unroll
@@ -102,7 +117,7 @@ __global__ __launch_bounds__(256, 2) void latent_expand_kernel(LatentArgs a, con
         const uint4 v = make_uint4(cvt_pk_bf16(lo[0], lo[1]), cvt_pk_bf16(lo[2], lo[3]), cvt_pk_bf16(hi[0], hi[1]),
                                    cvt_pk_bf16(hi[2], hi[3]));
         const int row = 32 * i + 8 * g;                                                 // .. + 7
-        const int col = 32 * (j >> 1) + 8 * (l16 >> 2) + (l16 & 3) + 4 * (j & 1);
+        const int col = 16 * j + l16;
         const int t = 64 * wt + (values ? row : col);
         const int page = 8 * tb + (t >> 4);
         if (page >= n_pages) continue;
@@ -154,8 +169,9 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
   constexpr int NT = 2, NW = 8, NB = 3;
   constexpr int KU = 2 * NOPE, RU = 2 * ROPE, VU = 2 * VD;  // 16-byte units of a page's block
   constexpr int LK = KU / 64, LV = VU / 64, LR = RU / 64;   // loads of one
-  constexpr int NL = 4 * (LK + LV + LR);                    // loads of a stage
-  constexpr int LPW = NL / NW;                              // a wave's at least
+  // a wave's loads of a stage: of the four pages' keys, values and (LR = 1: waves 0..3) shared keys
+  constexpr int WK = 4 * LK / NW, WV = 4 * LV / NW, LPW = WK + WV;
+  static_assert(4 * LK % NW == 0 && 4 * LV % NW == 0 && 4 * LR <= NW);
   __shared__ uint4 sk[NB][4 * KU], sv[NB][4 * VU], sr[NB][4 * RU];
   // the rows' rotated dims, each wave's as it multiplies them (in registers they are 16 too many)
   __shared__ uint4 sq[NW][NT][DS - DN][64];
@@ -164,22 +180,28 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, l16 = lane & 15;
-  const int t1 = it.t1, np = (t1 + 15) >> 4, ns = (t1 + 63) >> 6;
+  const int t1 = it.t1, ns = (t1 + 63) >> 6;
 
-  auto issue = [&](int j, int b) {
+  // the next stage into buffer b.  Pages past the sequence's last are other pages, or what
+  // the workspace has behind them (their keys are masked, and their values not used)
+  const char* next_k = reinterpret_cast<const char*>(kx) + (static_cast<size_t>(it.page0) * a.H + h) * (32 * NOPE);
+  const char* next_v = reinterpret_cast<const char*>(vx) + (static_cast<size_t>(it.page0) * a.H + h) * (32 * VD);
+  const char* next_r = reinterpret_cast<const char*>(rx) + static_cast<size_t>(it.page0) * (32 * ROPE);
+  const size_t page_k = static_cast<size_t>(a.H) * (32 * NOPE), page_v = static_cast<size_t>(a.H) * (32 * VD);
+  size_t of_k[WK], of_v[WV];
 #pragma unroll
-    for (int n = 0; n < (NL + NW - 1) / NW; ++n) {
-      const int i = NW * n + wave;
-      if (i >= NL) break;
-      const bool k = i < 4 * LK, v = !k && i < 4 * (LK + LV);
-      const int e = k ? i : v ? i - 4 * LK : i - 4 * (LK + LV);
-      const int per = k ? LK : v ? LV : LR;
-      const int p = e / per, part = e % per;
-      const size_t page = static_cast<size_t>(it.page0) + min(4 * j + p, np - 1);
-      const bf16_t* blk = k ? kx + (page * a.H + h) * (16 * NOPE) : v ? vx + (page * a.H + h) * (16 * VD) : rx + page * (16 * ROPE);
-      const uint32_t dst = k ? lds_addr(&sk[b][p * KU]) : v ? lds_addr(&sv[b][p * VU]) : lds_addr(&sr[b][p * RU]);
-      load_lds16(blk, (part * 64 + lane) * 16, dst + part * 1024);
-    }
+  for (int n = 0; n < WK; ++n) of_k[n] = (NW * n + wave) / LK * page_k + (NW * n + wave) % LK * 1024;
+#pragma unroll
+  for (int n = 0; n < WV; ++n) of_v[n] = (NW * n + wave) / LV * page_v + (NW * n + wave) % LV * 1024;
+  auto issue = [&](int b) {
+#pragma unroll
+    for (int n = 0; n < WK; ++n) load_lds16(next_k + of_k[n], lane * 16, lds_addr(&sk[b][(NW * n + wave) * 64]));
+#pragma unroll
+    for (int n = 0; n < WV; ++n) load_lds16(next_v + of_v[n], lane * 16, lds_addr(&sv[b][(NW * n + wave) * 64]));
+    if (4 * LR == NW || wave < 4 * LR) load_lds16(next_r + wave * 1024, lane * 16, lds_addr(&sr[b][wave * 64]));
+    next_k += 4 * page_k;
+    next_v += 4 * page_v;
+    next_r += 4 * 32 * ROPE;
   };
 
   uint4 qf[NT][DN];
@@ -227,31 +249,29 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
   };
   f32x4 sc[NT][2];
   uint4 pf[NT];
-  // (the shared keys are read here, under the own dims' products: a phase ahead they
-  // cost 16 registers more than there are)
-  auto scores = [&](int b, int hf) {
+  // the shared keys and the rows' rotated dims, read under the own dims' products
+  uint4 kr[2][DS - DN], qr[NT][DS - DN];
+  auto read_r = [&](int b, int hf) {
     const uint4* rb = &sr[b][(2 * hf + (l16 >> 3)) * RU];
-    uint4 kr[2][DS - DN];
 #pragma unroll
     for (int s = 0; s < DS - DN; ++s)
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) kr[hh][s] = rb[((s * 2 + hh) * 4 + g) * 8 + (l16 & 7)];
 #pragma unroll
+    for (int s = 0; s < DS - DN; ++s)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) qr[nt][s] = sq[wave][nt][s][lane];
+  };
+  auto scores = [&] {
+#pragma unroll
     for (int nt = 0; nt < NT; ++nt) sc[nt][0] = sc[nt][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < DN; ++s)
+    for (int s = 0; s < DS; ++s)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) sc[nt][hh] = mfma16x16x32(kf[hh][s], qf[nt][s], sc[nt][hh]);
-#pragma unroll
-    for (int s = 0; s < DS - DN; ++s)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const uint4 x = sq[wave][nt][s][lane];
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) sc[nt][hh] = mfma16x16x32(kr[hh][s], x, sc[nt][hh]);
-      }
+        for (int hh = 0; hh < 2; ++hh)
+          sc[nt][hh] = mfma16x16x32(s < DN ? kf[hh][s] : kr[hh][s - DN], s < DN ? qf[nt][s] : qr[nt][s - DN], sc[nt][hh]);
   };
   bool dropped = false;
   auto output = [&](int c0) {
@@ -338,9 +358,9 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
     __atomic_signal_fence(__ATOMIC_SEQ_CST);
   };
 
-  issue(0, 0);
+  issue(0);
   if (ns > 1) {
-    issue(1, 1);
+    issue(1);
     SPEC_WAIT_VM_LDS(LPW);
   } else {
     SPEC_WAIT_VM_LDS(0);
@@ -357,14 +377,17 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
       // first, so that their operands are gone when the scores' need registers
       if (c0 >= 32 && c0 - 32 <= pos_hi) output(c0 - 32);
       __builtin_amdgcn_sched_barrier(0);
-      if (c0 <= pos_hi) scores(b, hf);
+      if (c0 <= pos_hi) {
+        read_r(b, hf);
+        scores();
+      }
       if (hf == 0) read_k(b, 1);
       else if (j + 1 < ns) read_k(bn, 0);
       // stage j + 1 has landed before any wave reads it, a phase on
       if (hf == 0) __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
       phase_end();
       // vector phase.  Every wave is past its reads of stage j - 1, so its buffer takes stage j + 2
-      if (hf == 0 && j + 2 < ns) issue(j + 2, (j + 2) % NB);
+      if (hf == 0 && j + 2 < ns) issue((j + 2) % NB);
       __builtin_amdgcn_s_setprio(1);
       if (c0 <= pos_hi) softmax(c0, b, hf);
       __builtin_amdgcn_s_setprio(0);
@@ -378,7 +401,7 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
     for (int c0 = max(pos_lo - 31, 0) / 32 * 32; c0 <= pos_hi; c0 += 32) {
       if (c0 + 31 <= pos_lo) continue;
       const uint4* vb = reinterpret_cast<const uint4*>(
-          vx + ((static_cast<size_t>(it.page0) + min((c0 + 8 * g) >> 4, np - 1)) * a.H + h) * (16 * VD));
+          vx + ((static_cast<size_t>(it.page0) + min((c0 + 8 * g) >> 4, (t1 - 1) >> 4)) * a.H + h) * (16 * VD));
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         const uint4 marks = nonfinite_marks(vb[(dt * 2 + (g & 1)) * 16 + l16]);

@@ -719,7 +719,8 @@ LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const
   c.o_k = c.o_ml + align_up(sizeof(float) * static_cast<size_t>(c.plan.n_parts) * c.plan.tile * 2);
   c.o_v = c.o_k + align_up(size_t{32} * c.x_pages * n_heads * nope_dim);
   c.o_key = c.o_v + align_up(size_t{32} * c.x_pages * n_heads * v_dim);
-  c.bytes = c.o_key + align_up(size_t{32} * c.x_pages * rope_dim);
+  // (the prompt kernel loads four pages at a time: up to three past the last)
+  c.bytes = c.o_key + align_up(size_t{32} * c.x_pages * rope_dim) + (c.x_pages ? size_t{96} * n_heads * std::max(nope_dim, v_dim) : 0);
   return c;
 }
 
