@@ -47,9 +47,13 @@ struct LatentPlan {
 // Tiles and key splits of the absorbed form; at most max_parts partials.
 LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_parts, bool fp32);
 
-// Items of the expanded form (below): blocks of kPromptRows rows, those with most keys
-// first.
-std::vector<LatentItem> plan_latent_prompt(const std::vector<LatentSegment>& segs);
+// Items of the expanded form (below): blocks of `rows` (256 or 128) rows, those with
+// most keys first.
+struct LatentPromptPlan {
+  int rows = 256;
+  std::vector<LatentItem> items;
+};
+LatentPromptPlan plan_latent_prompt(const std::vector<LatentSegment>& segs, int H);
 
 // Whether a sequence of nrows rows behind pos0 others takes the expanded form.
 bool latent_expands(int nrows, int pos0);
@@ -89,14 +93,14 @@ hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st);
 
 // The expanded form (bf16): every head's keys [n_pages][H][16 x nope] and values
 // [n_pages][H][16 x vdim] of the listed pages, and the shared keys [n_pages][16 x
-// rope], in kv_layout.h's order; then items of at most kPromptRows rows (qv0, nqv: a
-// row and rows; page0: the sequence's first expanded page; t0 = 0, part < 0), each of
-// which is one workgroup a head.
-constexpr int kPromptRows = 256;
+// rope], in kv_layout.h's order; then items of at most `rows` rows (qv0, nqv: a row and
+// rows; page0: the sequence's first expanded page; t0 = 0, part < 0), each of which is
+// one workgroup a head.
 struct LatentExpanded {
   void *k = nullptr, *v = nullptr, *key = nullptr;
 };
 hipError_t launch_latent_expand(const LatentArgs& a, const int32_t* list, int n_pages, const LatentExpanded& x, hipStream_t st);
-hipError_t launch_latent_prompt(const LatentArgs& a, const LatentItem* items, int n_items, const LatentExpanded& x, hipStream_t st);
+hipError_t launch_latent_prompt(const LatentArgs& a, const LatentItem* items, int n_items, int rows, const LatentExpanded& x,
+                                hipStream_t st);
 
 }  // namespace spec

@@ -8,6 +8,7 @@
 
 #include "common.h"
 #include "latent.h"
+#include "latent_dev.h"
 
 namespace spec {
 namespace {
@@ -27,60 +28,7 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-// A product whose sum stays in accumulation registers, in place: left to itself the
-// compiler keeps a second copy of the sums, and there are no registers for one.  It
-// does not see that this is an MFMA, so the waits that one needs are written out:
-// two states after a vector instruction that wrote an operand, sums_ready() before
-// anything but such a product reads the sums.
-__device__ __forceinline__ void mfma_in_place(const uint4& a, const uint4& b, f32x4& c) {
-  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0"
-               : "+a"(c)
-               : "v"(__builtin_bit_cast(u32x4, a)), "v"(__builtin_bit_cast(u32x4, b)));
-}
-// The same on vector registers, and a first product (sum 0).
-__device__ __forceinline__ void mfma_in_place_v(const uint4& a, const uint4& b, f32x4& c) {
-  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0"
-               : "+v"(c)
-               : "v"(__builtin_bit_cast(u32x4, a)), "v"(__builtin_bit_cast(u32x4, b)));
-}
-__device__ __forceinline__ f32x4 mfma_first_v(const uint4& a, const uint4& b) {
-  f32x4 c;
-  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0"
-               : "=v"(c)
-               : "v"(__builtin_bit_cast(u32x4, a)), "v"(__builtin_bit_cast(u32x4, b)));
-  return c;
-}
-// x ^ k, computed where it stands: the compiler would have every step's address ready
-// ahead, and there are no registers for that.
-__device__ __forceinline__ uint32_t xor_here(uint32_t x, uint32_t k) {
-  asm volatile("v_xor_b32 %0, %1, %2" : "=v"(x) : "s"(k), "v"(x));
-  return x;
-}
-// c *= x for such a sum, which stays where it is.
-__device__ __forceinline__ void scale_in_place(f32x4& c, float x) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float v = c[i], w;
-    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(w) : "a"(v));
-    w *= x;
-    asm volatile("v_accvgpr_write_b32 %0, %1" : "=a"(v) : "v"(w));
-    c[i] = v;
-  }
-}
-__device__ __forceinline__ void operands_ready() { asm volatile("s_nop 1"); }
-__device__ __forceinline__ void sums_ready() { asm volatile("s_nop 15\n\ts_nop 7"); }
-
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
-
-__device__ __forceinline__ void wave_fence() {
-  __atomic_signal_fence(__ATOMIC_SEQ_CST);
-  __builtin_amdgcn_sched_barrier(0);
-}
-__device__ __forceinline__ void block_sync() {
-  wave_fence();
-  __builtin_amdgcn_s_barrier();
-  wave_fence();
-}
 
 template <typename T>
 __device__ __forceinline__ void put4(T* p, float a, float b, float c, float d) {
@@ -585,7 +533,7 @@ __global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_b
   // they take registers that there are not.
   uint4 ring[PD];
   f32x4 sc[NT][2];
-  // scores of the chunk in buffer b; also(u) after k-step u / 2 of key tile u % 2
+  // scores of the chunk in buffer b; also(i) after product i
   auto scores = [&](int b, auto&& also) {
     uint32_t ka[4] = {buffer(b) + k_off}, rb = buffer(b) + 32 * CL * 16 + r_off;
 #pragma unroll
@@ -595,6 +543,7 @@ __global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_b
       if (s < DL) return unit_at(ka[s & 3] + (s >> 2) * 256 + hh * (16 * CL * 16));
       return unit_at((s > DL ? xor_here(rb, 64) : rb) + hh * (16 * CR * 16));
     };
+    f32x4 x[NT][2];
 #pragma unroll
     for (int u = 0; u < PD; ++u) ring[u] = read_k(u);
     __builtin_amdgcn_sched_barrier(0);
@@ -602,14 +551,21 @@ __global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_b
     for (int u = 0; u < 2 * (DL + DR); ++u) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        if (u < 2) sc[nt][u & 1] = mfma_first_v(ring[u % PD], qf[nt][u >> 1]);
-        else mfma_in_place_v(ring[u % PD], qf[nt][u >> 1], sc[nt][u & 1]);
+        if (u < 2) x[nt][u & 1] = mfma_first_v(ring[u % PD], qf[nt][u >> 1]);
+        else mfma_in_place_v(ring[u % PD], qf[nt][u >> 1], x[nt][u & 1]);
+        if (nt == NT - 1 && u + PD < 2 * (DL + DR)) ring[u % PD] = read_k(u + PD);
+        also(u * NT + nt);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      if (u + PD < 2 * (DL + DR)) ring[u % PD] = read_k(u + PD);
-      also(u);
-      __builtin_amdgcn_sched_barrier(0);
     }
     sums_ready();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh) {
+        asm volatile("" : "+v"(x[nt][hh]));  // (in its place until here)
+        sc[nt][hh] = x[nt][hh];
+      }
   };
   // masks of chunk c in buffer b, some key of which some row of the workgroup does not see
   auto mask = [&](int c, int b) {
@@ -683,17 +639,24 @@ __global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_b
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) scale_in_place(acc[dt][nt], alpha[nt]);
   };
-  // probability of score e (of tile e / 8), and, with every second, the pair as bf16, as the
-  // values that they weight: the rounding stays below the output's
+  // Probability of score e / 3 (of tile e / 24), in three pieces: the exponent, the power, and
+  // the sum with every second pair as bf16, as the values that they weight: the rounding
+  // stays below the output's.  A product takes the matrix unit 16 cycles and the wave's
+  // issue 4: about a piece fits behind each.
   uint32_t pf[NT][4];
+  constexpr int E = 24 * NT;
   auto prob = [&](int e, uint32_t (&to)[NT][4]) {
-    const int nt = e / 8, j = e % 8;
-    const float p = __builtin_amdgcn_exp2f((sc[nt][j / 4][j % 4] + mneg[nt]) * a.scale);
-    lrun[nt][j % 2] += p;
-    sc[nt][j / 4][j % 4] = p;
-    if (j % 2) to[nt][j / 2] = cvt_pk_bf16(sc[nt][j / 4][j % 4 - 1], p);
+    const int nt = e / 24, j = e / 3 % 8;
+    float x = sc[nt][j / 4][j % 4];
+    if (e % 3 == 0) x = (x + mneg[nt]) * a.scale;
+    else if (e % 3 == 1) x = __builtin_amdgcn_exp2f(x);
+    else lrun[nt][j % 2] += x;
+    if (e % 3 < 2) stay_here(x);
+    else stay_here(lrun[nt][j % 2]);
+    sc[nt][j / 4][j % 4] = x;
+    if (e % 3 == 2 && j % 2) to[nt][j / 2] = cvt_pk_bf16(sc[nt][j / 4][j % 4 - 1], x);
   };
-  // sums of latents += the chunk whose first PD operands are read; also(dt) after tile dt
+  // sums of latents += the chunk whose first PD operands are read; also(i) after product i
   auto first_v = [&](int b) {
     va[0] = buffer(b) + v_off;
 #pragma unroll
@@ -707,11 +670,12 @@ __global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_b
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt) {
         mfma_in_place(ring[dt % PD], make_uint4(pf[nt][0], pf[nt][1], pf[nt][2], pf[nt][3]), acc[dt][nt]);
-      if (dt + PD < DT) ring[dt % PD] = read_v(dt + PD);
-      also(dt);
-      __builtin_amdgcn_sched_barrier(0);
+        if (nt == NT - 1 && dt + PD < DT) ring[dt % PD] = read_v(dt + PD);
+        also(dt * NT + nt);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   };
   auto no_more = [](int) {};
@@ -721,42 +685,37 @@ __global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_b
     // before, and the loads are spread over the products of the scores: issued
     // together, either holds a wave that has its SIMD to itself.
     constexpr int LA = NB - 1;  // chunks that loads are ahead
-    constexpr int LQ = (LPW + 1) / 2, US = 2 * (DL + DR);
+    constexpr int LQ = (LPW + 1) / 2, MS = 2 * (DL + DR) * NT, MV = DT * NT;  // products of the scores and of the sums
+    // (loads past the item's last chunk are of its last page: a branch around them would let
+    // the compiler gather up what is to be between the products)
 #pragma unroll
-    for (int i = 0; i < LA; ++i)
-      if (i < nch) issue(c0 + i, i);
-    SPEC_WAIT_VM_LDS(0);
+    for (int i = 0; i < LA; ++i) issue(c0 + i, i);
+    SPEC_WAIT_VM_LDS((LA - 1) * (NL / WQ));
     block_sync();
     scores(0, no_more);
     if (32 * c0 + 31 > pos_lo || 32 * c0 + 31 >= it.t1) mask(c0, 0);
     raise();
 #pragma unroll
-    for (int e = 0; e < 8 * NT; ++e) prob(e, pf);
+    for (int e = 0; e < E; ++e) prob(e, pf);
     for (int j = 0; j + 1 < nch; ++j) {
       const int b = j % NB, bn = (j + 1) % NB, c = c0 + j + 1;
       const uint32_t dst = buffer((j + LA) % NB);
-      const bool more = j + LA < nch;
-      // chunk j + 1 has landed (j + 2's loads, if there are, may be in flight), and every wave is done with chunk j - 1
-      static_assert(LA == 3);
-      if (j + 2 < nch) {
-        SPEC_WAIT_VM_LDS(NL / WQ);
-      } else {
-        SPEC_WAIT_VM_LDS(0);
-      }
+      // chunk j + 1 has landed (those behind it may be in flight), and every wave is done with chunk j - 1
+      SPEC_WAIT_VM_LDS((LA - 2) * (NL / WQ));
       block_sync();
-      if (more) take(c0 + j + LA);
-      scores(bn, [&](int u) {
-        if (u % (US / LQ) == 2 && u / (US / LQ) < LQ && more) load(u / (US / LQ), dst);
+      take(c0 + j + LA);
+      scores(bn, [&](int i) {
+        if (i % (MS / LQ) == 2 && i / (MS / LQ) < LQ) load(i / (MS / LQ), dst);
       });
       if (32 * c + 31 > pos_lo || 32 * c + 31 >= it.t1) mask(c, bn);
       const bool up = raise();
       first_v(b);
       uint32_t next[NT][4];
-      sums([&](int dt) {
-        constexpr int step = DT / (LPW - LQ);
-        if (dt % step == 1 && dt / step < LPW - LQ && more) load(LQ + dt / step, dst);
+      sums([&](int i) {
+        constexpr int step = MV / (LPW - LQ);
+        if (i % step == 1 && i / step < LPW - LQ) load(LQ + i / step, dst);
 #pragma unroll
-        for (int e = dt * 8 * NT / DT; e < (dt + 1) * 8 * NT / DT; ++e) prob(e, next);
+        for (int e = i * E / MV; e < (i + 1) * E / MV; ++e) prob(e, next);
       });
       if (up) rescale();
 #pragma unroll
@@ -764,9 +723,9 @@ __global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_b
 #pragma unroll
         for (int i = 0; i < 4; ++i) pf[nt][i] = next[nt][i];
     }
-    SPEC_WAIT_VM_LDS(0);
     first_v((nch - 1) % NB);
     sums(no_more);
+    SPEC_WAIT_VM_LDS(0);  // (no load outlives the buffers)
   } else {
     // (a share's chunk past the last is loaded from the last page, and masked)
     if (NB == 2) issue(c0 + wk, 0);
@@ -789,7 +748,7 @@ __global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_b
       first_v(b);
       if (raise()) rescale();
 #pragma unroll
-      for (int e = 0; e < 8 * NT; ++e) prob(e, pf);
+      for (int e = 0; e < E; ++e) prob(e, pf);
       sums(no_more);
     }
   }

@@ -63,15 +63,21 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_pa
   return p;
 }
 
-std::vector<LatentItem> plan_latent_prompt(const std::vector<LatentSegment>& segs) {
-  std::vector<LatentItem> items;
+LatentPromptPlan plan_latent_prompt(const std::vector<LatentSegment>& segs, int H) {
+  LatentPromptPlan p;
+  auto blocks = [&](int rows) {
+    int64_t n = 0;
+    for (const LatentSegment& s : segs) n += (static_cast<int64_t>(s.nrows) + rows - 1) / rows;
+    return n * H;
+  };
+  if (blocks(256) < 256) p.rows = 128;
   for (const LatentSegment& s : segs)
-    for (int64_t r = 0; r < s.nrows; r += kPromptRows) {
-      const int n = static_cast<int>(std::min<int64_t>(kPromptRows, s.nrows - r)), first = static_cast<int>(r);
-      items.push_back(LatentItem{s.row0 + s.qoff + first, n, 0, s.pos0 + first, s.page0, 0, s.pos0 + first + n, -1, 0});
+    for (int64_t r = 0; r < s.nrows; r += p.rows) {
+      const int n = static_cast<int>(std::min<int64_t>(p.rows, s.nrows - r)), first = static_cast<int>(r);
+      p.items.push_back(LatentItem{s.row0 + s.qoff + first, n, 0, s.pos0 + first, s.page0, 0, s.pos0 + first + n, -1, 0});
     }
-  std::stable_sort(items.begin(), items.end(), [](const LatentItem& x, const LatentItem& y) { return x.t1 > y.t1; });
-  return items;
+  std::stable_sort(p.items.begin(), p.items.end(), [](const LatentItem& x, const LatentItem& y) { return x.t1 > y.t1; });
+  return p;
 }
 
 bool latent_expands(int nrows, int pos0) { return nrows >= 256; }

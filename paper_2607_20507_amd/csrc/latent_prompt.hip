@@ -144,29 +144,33 @@ __global__ __launch_bounds__(256, 3) void latent_expand_kernel(LatentArgs a, con
 
 // ---------------------------------------------------------------------------
 // Attention to the expanded pages: one workgroup of 8 waves (two per SIMD) per (block
-// of 256 consecutive rows, head).  The structure is the K / V cache's prompt kernel's
+// of 128 NT consecutive rows, head).  The structure is the K / V cache's prompt kernel's
 // (attention.hip): 64 keys at a time in LDS, three buffers; each wave both products for
-// its own 32 rows; a 32-key chunk is a matrix phase and a vector phase, and waves 4..7
+// its own 16 NT rows; a 32-key chunk is a matrix phase and a vector phase, and waves 4..7
 // run one phase behind waves 0..3, with which they share the SIMDs.  A key's score has
 // the head's own dims and the shared ones, whose block every head reads.
-// Differences to the maximum are taken before the scale.  Values that are not finite are
+// p = 2^(score scale - max scale), one FMA a score; the rounding of max scale is one factor
+// for all of a row, and divides out.  Where a row's logits reach 2^16 that factor could
+// matter (and from 2^30 on overflow): there a chunk's scores become their differences to
+// the maximum first.  Values that are not finite are
 // dropped from chunks in which some row does not see their key, and added after the
 // walk for the rows that do.
 
 constexpr float kPromptRescaleLog2 = 8.f;
+constexpr float kPromptLargeLogit = 65536.f;
 
 __device__ __forceinline__ uint32_t keep_pair(uint32_t w, int valid) {
   return valid >= 2 ? w : valid == 1 ? w & 0xFFFFu : 0u;
 }
 
-template <int NOPE, int ROPE, int VD>
+template <int NOPE, int ROPE, int VD, int NT>
 __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a, const LatentItem* __restrict__ items,
                                                                     const bf16_t* __restrict__ kx,
                                                                     const bf16_t* __restrict__ vx,
                                                                     const bf16_t* __restrict__ rx) {
   constexpr int DN = NOPE / 32, DS = DN + ROPE / 32;  // k-steps of the scores: own dims, all
   constexpr int DT = VD / 16;
-  constexpr int NT = 2, NW = 8, NB = 3;
+  constexpr int NW = 8, NB = 3;
   constexpr int KU = 2 * NOPE, RU = 2 * ROPE, VU = 2 * VD;  // 16-byte units of a page's block
   constexpr int LK = KU / 64, LV = VU / 64, LR = RU / 64;   // loads of one
   // a wave's loads of a stage: of the four pages' keys, values and (LR = 1: waves 0..3) shared keys
@@ -208,7 +212,7 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
   int klim[NT];  // the last key each row sees (-1: none, padding)
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int m = 32 * wave + 16 * nt + l16;
+    const int m = 16 * (NT * wave + nt) + l16;
     const bool ok = m < it.nqv;
     klim[nt] = ok ? min(it.pos0 + m, t1 - 1) : -1;
     const bf16_t* base = static_cast<const bf16_t*>(a.q) + (static_cast<size_t>(it.qv0 + (ok ? m : 0)) * a.H + h) * (NOPE + ROPE) + 8 * g;
@@ -219,15 +223,18 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
       else sq[wave][nt][s - DN][lane] = x;
     }
   }
-  const int pos_lo = it.pos0 + 32 * wave;
-  const int pos_hi = it.pos0 + min(32 * wave + 31, it.nqv - 1);
+  const int pos_lo = it.pos0 + 16 * NT * wave;
+  const int pos_hi = it.pos0 + min(16 * NT * (wave + 1), it.nqv) - 1;
   const float scale = a.scale;
-  float mneg[NT], mlim[NT], lrun[NT][2];
+  // minus the running maximum, minus its logit (-inf: no key yet, every p is 0; 0 where logits
+  // are large), the score above which it is raised (-inf: no key yet), two partial sums of p
+  float mneg[NT], add[NT], mlim[NT], lrun[NT][2];
+  bool large = false;  // some logit of the wave is
   f32x4 acc[DT][NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    mlim[nt] = -INFINITY;
-    mneg[nt] = FLT_MAX;
+    mlim[nt] = add[nt] = -INFINITY;
+    mneg[nt] = 0.f;
     lrun[nt][0] = lrun[nt][1] = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -321,15 +328,23 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
 #pragma unroll
       for (int j = 1; j < 8; ++j) mx[nt] = fmaxf(mx[nt], sc[nt][j / 4][j % 4]);
     }
-    if (__any(mx[0] > mlim[0] || mx[1] > mlim[1])) {
+    bool up = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) up |= mx[nt] > mlim[nt];
+    if (__any(up)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float m = mx[nt];
         m = fmaxf(m, __shfl_xor(m, 16, kWave));
         m = fmaxf(m, __shfl_xor(m, 32, kWave));
         if (m > mlim[nt]) {
-          const float alpha = __builtin_amdgcn_exp2f((-mneg[nt] - m) * scale);
+          const float logit = m * scale;
+          const bool big = !(fabsf(logit) < kPromptLargeLogit);
+          const float to = big ? 0.f : -logit;
+          const float alpha = mlim[nt] == -INFINITY ? 0.f
+                              : __builtin_amdgcn_exp2f(big || add[nt] == 0.f ? (-mneg[nt] - m) * scale : to - add[nt]);
           mneg[nt] = -m;
+          add[nt] = to;
           mlim[nt] = m + kPromptRescaleLog2 / scale;
 #pragma unroll
           for (int i = 0; i < 2; ++i) lrun[nt][i] *= alpha;
@@ -337,6 +352,15 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
           for (int dt = 0; dt < DT; ++dt) acc[dt][nt] *= alpha;
         }
       }
+      large = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) large |= __any(!(fabsf(mneg[nt] * scale) < kPromptLargeLogit));
+    }
+    if (large) {
+      asm volatile("");
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+        if (!(fabsf(mneg[nt] * scale) < kPromptLargeLogit)) sc[nt][0] += mneg[nt], sc[nt][1] += mneg[nt];
     }
     read_v(b, hf, 2);
     read_v(b, hf, 3);
@@ -344,7 +368,7 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
     for (int nt = 0; nt < NT; ++nt) {
       float p[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f((sc[nt][j / 4][j % 4] + mneg[nt]) * scale);
+      for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(sc[nt][j / 4][j % 4], scale, add[nt]));
 #pragma unroll
       for (int j = 0; j < 8; ++j) lrun[nt][j % 2] += p[j];
       pf[nt] = make_uint4(cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7]));
@@ -416,7 +440,7 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
     float l = lrun[nt][0] + lrun[nt][1];
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
-    const int m = 32 * wave + 16 * nt + l16;
+    const int m = 16 * (NT * wave + nt) + l16;
     if (m >= it.nqv) continue;
     const float inv = 1.f / l;
     bf16_t* o = static_cast<bf16_t*>(a.out) + (static_cast<size_t>(it.qv0 + m) * a.H + h) * VD + 4 * g;
@@ -429,9 +453,10 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
 }
 
 template <int NOPE, int ROPE, int VD>
-hipError_t launch_prompt(const LatentArgs& a, const LatentItem* items, unsigned n, const LatentExpanded& x, hipStream_t st) {
-  launch_kernel(attn_latent_prompt_kernel<NOPE, ROPE, VD>, dim3(n), dim3(512), 0, st, a, items, static_cast<const bf16_t*>(x.k),
-                static_cast<const bf16_t*>(x.v), static_cast<const bf16_t*>(x.key));
+hipError_t launch_prompt(const LatentArgs& a, const LatentItem* items, unsigned n, int rows, const LatentExpanded& x, hipStream_t st) {
+  const bf16_t *k = static_cast<const bf16_t*>(x.k), *v = static_cast<const bf16_t*>(x.v), *key = static_cast<const bf16_t*>(x.key);
+  if (rows == 256) launch_kernel(attn_latent_prompt_kernel<NOPE, ROPE, VD, 2>, dim3(n), dim3(512), 0, st, a, items, k, v, key);
+  else launch_kernel(attn_latent_prompt_kernel<NOPE, ROPE, VD, 1>, dim3(n), dim3(512), 0, st, a, items, k, v, key);
   return hipGetLastError();
 }
 
@@ -446,21 +471,23 @@ hipError_t launch_latent_expand(const LatentArgs& a, const int32_t* list, int n_
   return hipGetLastError();
 }
 
-hipError_t launch_latent_prompt(const LatentArgs& a, const LatentItem* items, int n_items, const LatentExpanded& x, hipStream_t st) {
+hipError_t launch_latent_prompt(const LatentArgs& a, const LatentItem* items, int n_items, int rows, const LatentExpanded& x,
+                                hipStream_t st) {
+  if (rows != 128 && rows != 256) return hipErrorInvalidValue;
   const size_t n = static_cast<size_t>(n_items) * a.H;
   if (n == 0) return hipSuccess;
   if (n > kMaxGrid256 / 2) return hipErrorInvalidValue;
   const int sizes = (a.nope == 128 ? 4 : 0) + (a.rope == 64 ? 2 : 0) + (a.vdim == 128 ? 1 : 0);
   const unsigned g = static_cast<unsigned>(n);
   switch (sizes) {
-    case 0: return launch_prompt<64, 32, 64>(a, items, g, x, st);
-    case 1: return launch_prompt<64, 32, 128>(a, items, g, x, st);
-    case 2: return launch_prompt<64, 64, 64>(a, items, g, x, st);
-    case 3: return launch_prompt<64, 64, 128>(a, items, g, x, st);
-    case 4: return launch_prompt<128, 32, 64>(a, items, g, x, st);
-    case 5: return launch_prompt<128, 32, 128>(a, items, g, x, st);
-    case 6: return launch_prompt<128, 64, 64>(a, items, g, x, st);
-    default: return launch_prompt<128, 64, 128>(a, items, g, x, st);
+    case 0: return launch_prompt<64, 32, 64>(a, items, g, rows, x, st);
+    case 1: return launch_prompt<64, 32, 128>(a, items, g, rows, x, st);
+    case 2: return launch_prompt<64, 64, 64>(a, items, g, rows, x, st);
+    case 3: return launch_prompt<64, 64, 128>(a, items, g, rows, x, st);
+    case 4: return launch_prompt<128, 32, 64>(a, items, g, rows, x, st);
+    case 5: return launch_prompt<128, 32, 128>(a, items, g, rows, x, st);
+    case 6: return launch_prompt<128, 64, 64>(a, items, g, rows, x, st);
+    default: return launch_prompt<128, 64, 128>(a, items, g, rows, x, st);
   }
 }
 

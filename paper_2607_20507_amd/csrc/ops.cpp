@@ -657,7 +657,7 @@ struct LatentCall {
   std::vector<int32_t> row_list;   // the absorbed form's rows, where both are taken
   int R = 0;                       // their number
   LatentPlan plan;
-  std::vector<LatentItem> x_items;
+  LatentPromptPlan x;
   size_t o_q = 0, o_o = 0, o_part = 0, o_ml = 0, o_k = 0, o_v = 0, o_key = 0, bytes = 0;
 };
 
@@ -705,13 +705,13 @@ LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const
   c.status = SPEC_OK;
   if (c.rows == 0) return c;
   if (c.R) c.plan = plan_latent(segs, n_heads, kOpMaxParts, dtype == SPEC_F32);
-  c.x_items = plan_latent_prompt(x_segs);
+  c.x = plan_latent_prompt(x_segs, n_heads);
   if (c.R && c.R < c.rows)
     for (const LatentSegment& s : segs)
       for (int r = 0; r < s.nrows; ++r) c.row_list.push_back(s.row0 + s.qoff + r);
   const size_t elem = dtype == SPEC_F32 ? 4 : 2, lat = align_up(elem * c.R * n_heads * rank);
   c.o_q = align_up(sizeof(int32_t) * (c.pages + c.x_pages)) + align_up(sizeof(LatentItem) * c.plan.items.size()) +
-          align_up(sizeof(LatentGroup) * c.plan.groups.size()) + align_up(sizeof(LatentItem) * c.x_items.size()) +
+          align_up(sizeof(LatentGroup) * c.plan.groups.size()) + align_up(sizeof(LatentItem) * c.x.items.size()) +
           align_up(sizeof(int32_t) * c.row_list.size());
   c.o_o = c.o_q + lat;
   c.o_part = c.o_o + lat;
@@ -770,7 +770,7 @@ spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_
       table.insert(table.end(), from, from + n);
     }
   MetaBlock mb;
-  const size_t opt = mb.add(table), oit = mb.add(c.plan.items), ogr = mb.add(c.plan.groups), oxi = mb.add(c.x_items),
+  const size_t opt = mb.add(table), oit = mb.add(c.plan.items), ogr = mb.add(c.plan.groups), oxi = mb.add(c.x.items),
                orl = mb.add(c.row_list);
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -799,11 +799,11 @@ spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_
   a.part_o = reinterpret_cast<float*>(ws + c.o_part);
   a.part_ml = reinterpret_cast<float*>(ws + c.o_ml);
   hipError_t e = hipSuccess;
-  if (!c.x_items.empty()) {
+  if (!c.x.items.empty()) {
     const LatentExpanded x{ws + c.o_k, ws + c.o_v, ws + c.o_key};
     e = launch_latent_expand(a, a.page_list + c.pages, static_cast<int>(c.x_pages), x, st);
     if (e == hipSuccess)
-      e = launch_latent_prompt(a, reinterpret_cast<const LatentItem*>(ws + oxi), static_cast<int>(c.x_items.size()), x, st);
+      e = launch_latent_prompt(a, reinterpret_cast<const LatentItem*>(ws + oxi), static_cast<int>(c.x.items.size()), c.x.rows, x, st);
   }
   if (c.R) {
     int max_parts = 0;
