@@ -38,25 +38,29 @@ struct LatentSegment {
 };
 
 struct LatentPlan {
-  int tile = 16;  // query vectors an item holds at most: 16, 32, 64 or 128 (fp32: 16)
+  int tile = 16;  // query vectors an item holds at most: 16, 32 or 64 (fp32: 16)
   std::vector<LatentItem> items;
   std::vector<LatentGroup> groups;
   int n_parts = 0;
 };
 
-// Tiles and key splits of the absorbed form; at most max_parts partials.
-LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_parts, bool fp32);
+// Tiles and key splits of the absorbed form (at most kLatentMaxParts parts in all).
+constexpr int kLatentMaxParts = 512;
+LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, bool fp32);
 
 // Items of the expanded form (below): blocks of `rows` (256 or 128) rows, those with
 // most keys first.
 struct LatentPromptPlan {
   int rows = 256;
   std::vector<LatentItem> items;
+  std::vector<LatentGroup> groups;  // (qv0, nqv: a row and rows)
+  int n_parts = 0;
 };
 LatentPromptPlan plan_latent_prompt(const std::vector<LatentSegment>& segs, int H);
 
-// Whether a sequence of nrows rows behind pos0 others takes the expanded form.
-bool latent_expands(int nrows, int pos0);
+// Whether a sequence of nrows rows behind pos0 others takes the expanded form; weights:
+// elements of w_k and w_v.
+bool latent_expands(int nrows, int pos0, int64_t weights);
 
 struct LatentArgs {
   int dtype;  // 0 fp32, 1 bf16 (q, pages, weights, out, q_lat, o_lat)
@@ -94,13 +98,18 @@ hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st);
 // The expanded form (bf16): every head's keys [n_pages][H][16 x nope] and values
 // [n_pages][H][16 x vdim] of the listed pages, and the shared keys [n_pages][16 x
 // rope], in kv_layout.h's order; then items of at most `rows` rows (qv0, nqv: a row and
-// rows; page0: the sequence's first expanded page; t0 = 0, part < 0), each of which is
-// one workgroup a head.
+// rows; page0: the sequence's first expanded page; t0 a multiple of 64), each of which is
+// one workgroup a head; then the parts' join.
 struct LatentExpanded {
   void *k = nullptr, *v = nullptr, *key = nullptr;
+  float* part_o = nullptr;   // [parts][rows][H][vdim]
+  float* part_ml = nullptr;  // [parts][rows][H][2]
 };
 hipError_t launch_latent_expand(const LatentArgs& a, const int32_t* list, int n_pages, const LatentExpanded& x, hipStream_t st);
 hipError_t launch_latent_prompt(const LatentArgs& a, const LatentItem* items, int n_items, int rows, const LatentExpanded& x,
                                 hipStream_t st);
+
+hipError_t launch_latent_prompt_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int rows,
+                                        const LatentExpanded& x, hipStream_t st);
 
 }  // namespace spec

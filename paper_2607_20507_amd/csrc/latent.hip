@@ -172,17 +172,24 @@ __global__ __launch_bounds__(256) void latent_absorb_bf16_kernel(LatentArgs a) {
   }
   const bf16_t* q = static_cast<const bf16_t*>(a.q);
   bf16_t* to = static_cast<bf16_t*>(a.q_lat);
-  const int hq = NOPE + a.rope;
-  for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += 16 * gridDim.y) {
-    const int r = r0 + l16, i = min(r, a.R - 1);
-    const size_t qv = static_cast<size_t>(i) * a.H + h, from = (static_cast<size_t>(row_of(a, i)) * a.H + h) * hq;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    uint4 qf[KS];
+  const int hq = NOPE + a.rope, step = 16 * gridDim.y;
+  uint4 qf[KS], qn[KS];
+  auto read = [&](int r0, uint4 (&x)[KS]) {
+    const size_t from = (static_cast<size_t>(row_of(a, min(r0 + l16, a.R - 1))) * a.H + h) * hq;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const uint4*>(q + from + 32 * s + 8 * g);
+    for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const uint4*>(q + from + 32 * s + 8 * g);
+  };
+  read(16 * blockIdx.y, qf);
+  for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += step) {
+    read(r0 + step, qn);  // (past the last row: that row)
+    const int r = r0 + l16;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < KS; ++s) acc = mfma16x16x32(wf[s], qf[s], acc);
-    if (r < a.R) put4(to + qv * a.rank + c0 + 16 * wave + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+    if (r < a.R)
+      put4(to + (static_cast<size_t>(r) * a.H + h) * a.rank + c0 + 16 * wave + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = qn[s];
   }
 }
 
@@ -219,16 +226,18 @@ __global__ __launch_bounds__(256) void latent_absorb_f32_kernel(LatentArgs a) {
 
 // ---------------------------------------------------------------------------
 // Sums of latents to values: out[row, h, d] = sum_c o'[row, h, c] w_v[h, d, c].  A
-// workgroup makes 16 dims of one head, its four waves a quarter of the sum each.
+// workgroup makes 16 dims of one head.  For few rows its four waves take a quarter of
+// the sum each (SPLIT: all 256 CUs stream the weight); for more, every wave holds all 16
+// rows of the weight and takes its own row tiles.
 
-template <int RANK>
+template <int RANK, bool SPLIT>
 __global__ __launch_bounds__(256) void latent_values_bf16_kernel(LatentArgs a) {
-  constexpr int KS = RANK / 128;
-  __shared__ f32x4 part[4][64];
+  constexpr int KS = SPLIT ? RANK / 128 : RANK / 32;
+  __shared__ f32x4 part[SPLIT ? 4 : 1][64];
   const int tiles = a.vdim / 16;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
   const int h = blockIdx.x / tiles, d0 = blockIdx.x % tiles * 16;
-  const int c0 = wave * (RANK / 4) + 8 * g;
+  const int c0 = (SPLIT ? wave * (RANK / 4) : 0) + 8 * g;
   const bf16_t* w = static_cast<const bf16_t*>(a.w_v) + static_cast<int64_t>(h) * a.v_stride +
                     static_cast<size_t>(d0 + l16) * RANK + c0;
   uint4 wf[KS];
@@ -236,7 +245,8 @@ __global__ __launch_bounds__(256) void latent_values_bf16_kernel(LatentArgs a) {
   for (int s = 0; s < KS; ++s) wf[s] = *reinterpret_cast<const uint4*>(w + 32 * s);
   const bf16_t* o = static_cast<const bf16_t*>(a.o_lat);
   bf16_t* out = static_cast<bf16_t*>(a.out);
-  for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += 16 * gridDim.y) {
+  const int step = (SPLIT ? 16 : 64) * gridDim.y;
+  for (int r0 = SPLIT ? 16 * blockIdx.y : 64 * blockIdx.y + 16 * wave; r0 < a.R; r0 += step) {
     const int r = r0 + l16;
     const size_t qv = static_cast<size_t>(min(r, a.R - 1)) * a.H + h;
     uint4 of[KS];
@@ -245,13 +255,14 @@ __global__ __launch_bounds__(256) void latent_values_bf16_kernel(LatentArgs a) {
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < KS; ++s) acc = mfma16x16x32(wf[s], of[s], acc);
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (wave == 0 && r < a.R) {
-      acc = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
-      put4(out + (static_cast<size_t>(row_of(a, r)) * a.H + h) * a.vdim + d0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+    if constexpr (SPLIT) {
+      part[wave][lane] = acc;
+      __syncthreads();
+      if (wave == 0) acc = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
     }
-    __syncthreads();
+    if ((!SPLIT || wave == 0) && r < a.R)
+      put4(out + (static_cast<size_t>(row_of(a, r)) * a.H + h) * a.vdim + d0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+    if constexpr (SPLIT) __syncthreads();
   }
 }
 
@@ -336,13 +347,11 @@ __device__ __forceinline__ void join_waves(const LatentArgs& a, const LatentItem
 
 // One workgroup per query vector of a group and block of 1024 / PG columns: four columns
 // a thread, the parts dealt to PG shares, whose sums are added in their order.
-constexpr int kCombineMaxParts = 4096;
-
 template <typename T, int RANK, int PG>
 __global__ __launch_bounds__(256) void latent_combine_kernel(LatentArgs a, const LatentGroup* __restrict__ groups, int tile) {
   constexpr int CT = 256 / PG;  // threads along the columns
   static_assert(RANK % (4 * CT) == 0);
-  __shared__ float s_w[kCombineMaxParts];
+  __shared__ float s_w[kLatentMaxParts];
   __shared__ f32x4 s_o[PG][CT];
   __shared__ float s_red[4];
   const LatentGroup gr = groups[blockIdx.x / tile];
@@ -395,7 +404,7 @@ __global__ __launch_bounds__(256) void latent_combine_kernel(LatentArgs a, const
 }
 
 // ---------------------------------------------------------------------------
-// Absorbed attention, bf16.  A workgroup holds 16 NT WQ query vectors of one
+// Absorbed attention, bf16.  A workgroup holds 16 WQ query vectors of one
 // sequence; its four waves are WQ shares of them times WK shares of the keys.  32
 // keys at a time go to LDS (direct loads of their two pages), where the waves of a
 // share read them twice: as rows for S^T = C Q'^T (A = 16 keys x 32 dims), and
@@ -412,24 +421,21 @@ __global__ __launch_bounds__(256) void latent_combine_kernel(LatentArgs a, const
 // So chunks with such keys are cleaned in LDS between the two products: values that
 // are not finite become 0, and the rows that do see their key get a NaN score.
 
-template <int RANK, int ROPE, int NT, int WQ, int WK>
-__global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_bf16_kernel(LatentArgs a, const LatentItem* __restrict__ items) {
+template <int RANK, int ROPE, int WQ, int WK>
+__global__ __launch_bounds__(256, WK == 1 ? 2 : 1) void attn_latent_bf16_kernel(LatentArgs a, const LatentItem* __restrict__ items) {
   constexpr int CL = RANK / 8, CR = ROPE / 8;    // 16-byte chunks of a token's latent and key
   constexpr int DL = RANK / 32, DR = ROPE / 32;  // k-steps of the scores
   constexpr int DT = RANK / 16;                  // 16-dim output tiles
-  constexpr bool PIPE = NT == 2;
-  constexpr int NB = PIPE ? 4 : WK == 4 ? 1 : 2;  // chunk buffers of a key share
-  constexpr int PD = WK == 1 && NT == 1 ? 4 : 8;              // operands read ahead
-  constexpr int BU = 32 * (CL + CR);             // units of one
-  constexpr int Q = 16 * NT * WQ;
+  constexpr int NB = WK == 4 ? 1 : 2;            // chunk buffers of a key share
+  constexpr int PD = WK == 1 ? 4 : 8;            // operands read ahead (two workgroups a CU leave fewer registers)
+  constexpr int BU = 32 * (CL + CR);             // 16-byte units of a chunk
+  constexpr int Q = 16 * WQ;
   constexpr int TP = 64 / CL, RT = 64 / CR;      // tokens a load covers: latents, keys
-  constexpr int NLL = 32 / TP, NL = NLL + 32 / RT;
-  constexpr int LPW = (NL + WQ - 1) / WQ;        // a wave's of a chunk, at most
+  constexpr int NLL = 32 / TP, NL = NLL + 32 / RT;  // loads of a chunk: its latents', all
   constexpr int kEntry = (CL + CR) * 16;
-  static_assert(NLL % WQ == 0);
   constexpr int kJoin = WK > 1 ? WK * Q * (RANK + 4) * 4 / 16 : 0;
   constexpr int kUnits = WK * NB * BU > kJoin ? WK * NB * BU : kJoin;
-  static_assert(WQ * WK == 4 && (WK == 1 || NT == 1));
+  static_assert(WQ * WK == 4 && NLL % WQ == 0);
   __shared__ __attribute__((aligned(256))) uint4 buf[kUnits];
   __shared__ float s_ml[WK > 1 ? 2 * WK * Q : 1];
   __shared__ uint32_t s_flag[4];
@@ -446,73 +452,63 @@ __global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_b
   auto f = [](int t) { return (t & 7) << 1 | (t >> 2 & 1); };
   auto fr = [&](int t) { return CR == 8 ? (t & 3) << 1 | (t >> 2 & 1) : t >> 1 & 3; };
 
-  // lane offsets of the loads
-  const uint32_t ld_lat = (lane % CL ^ (TP == 2 ? (lane >> 5) * 2 : 0)) * 16;
-  const uint32_t ld_key = lane / CR * ((CL + CR) * 16) + (CL + (lane % CR ^ fr(lane / CR))) * 16;
   // page ids, 64 (of 32 chunks) in a wave's lanes, the next 64 asked for ahead; past the
   // item's last page it stands for the others
   int cp = c0;  // the chunk of lanes 0 and 1
   int32_t ids = list[min(2 * c0 + lane, np - 1)], ids_next = list[min(2 * c0 + 64 + lane, np - 1)];
-  // the wave's loads of chunk c into buffer b, one by one
-  size_t page[2];
-  auto take = [&](int c) {
+  // lane offsets of the loads
+  const uint32_t ld_lat = (lane % CL ^ (TP == 2 ? (lane >> 5) * 2 : 0)) * 16;
+  const uint32_t ld_key = lane / CR * kEntry + (CL + (lane % CR ^ fr(lane / CR))) * 16;
+  auto buffer = [&](int b) { return lds_addr(&buf[(wk * NB + b) * BU]); };  // (a multiple of 256)
+  // the wave's loads of chunk c into buffer b
+  auto issue = [&](int c, int b) {
     if (c >= cp + 32) {
       cp += 32;
       ids = ids_next;
       ids_next = list[min(2 * cp + 64 + lane, np - 1)];
     }
+    size_t page[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       page[i] = static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(ids, 2 * (c - cp) + i))) * (16 * kEntry);
-  };
-  auto load = [&](int j, uint32_t dst) {
-    const int i = WQ * j + wq;
-    if (NL % WQ != 0 && i >= NL) return;
-    const bool key = WQ * j >= NLL;
-    const int first = key ? (i - NLL) * RT : i * TP;
-    const char* base = pool + (first >> 4 ? page[1] : page[0]) + (first & 15) * kEntry;
-    // (f of a load's second token, first + 1, is f(first) ^ 2)
-    uint32_t at;
-    if (key) at = ld_key;
-    else if (TP == 1) at = xor_here(ld_lat, f(first) * 16);
-    else at = xor_here(ld_lat, f(first) * 16) + (lane >> 5) * kEntry;
-    load_lds16(base, at, dst + i * 1024);
-  };
-  auto buffer = [&](int b) { return lds_addr(&buf[(wk * NB + b) * BU]); };
-  auto issue = [&](int c, int b) {
-    take(c);
 #pragma unroll
-    for (int j = 0; j < LPW; ++j) load(j, buffer(b));
+    for (int j = 0; j < (NL + WQ - 1) / WQ; ++j) {
+      const int i = WQ * j + wq;
+      if (NL % WQ != 0 && i >= NL) break;
+      const bool key = WQ * j >= NLL;
+      const int first = key ? (i - NLL) * RT : i * TP;
+      const char* base = pool + (first >> 4 ? page[1] : page[0]) + (first & 15) * kEntry;
+      // (f of a load's second token, first + 1, is f(first) ^ 2)
+      uint32_t at;
+      if (key) at = ld_key;
+      else if (TP == 1) at = xor_here(ld_lat, f(first) * 16);
+      else at = xor_here(ld_lat, f(first) * 16) + (lane >> 5) * kEntry;
+      load_lds16(base, at, buffer(b) + i * 1024);
+    }
   };
 
-  // query vectors
-  uint4 qf[NT][DL + DR];
-  int klim[NT];  // the last key each sees (-1: none, a padding vector)
-  float mneg[NT], mlim[NT], lrun[NT][2];
-  f32x4 acc[DT][NT];
-  const int m0 = 16 * NT * wq;
-  auto pos_of = [&](int m) { return it.pos0 + (it.qv0 + m) / a.H - it.row0; };
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int m = m0 + 16 * nt + l16;
-    const bool ok = m < it.nqv;
-    klim[nt] = ok ? min(pos_of(m), it.t1 - 1) : -1;
+  // the lane's query vector
+  const int m = 16 * wq + l16;
+  const bool ok = m < it.nqv;
+  auto pos_of = [&](int i) { return it.pos0 + (it.qv0 + i) / a.H - it.row0; };
+  const int klim = ok ? min(pos_of(m), it.t1 - 1) : -1;  // the last key it sees (-1: none, padding)
+  const int pos_lo = pos_of(0);
+  uint4 qf[DL + DR];
+  {
     const size_t qv = static_cast<size_t>(it.qv0 + (ok ? m : 0));
     const bf16_t* ql = static_cast<const bf16_t*>(a.q_lat) + qv * RANK + 8 * g;
     const bf16_t* qr = static_cast<const bf16_t*>(a.q) + (qv + static_cast<size_t>(it.qoff) * a.H) * (a.nope + ROPE) + a.nope + 8 * g;
 #pragma unroll
     for (int s = 0; s < DL + DR; ++s)
-      qf[nt][s] = ok ? *reinterpret_cast<const uint4*>(s < DL ? ql + 32 * s : qr + 32 * (s - DL)) : make_uint4(0, 0, 0, 0);
-    mneg[nt] = FLT_MAX;
-    mlim[nt] = -INFINITY;
-    lrun[nt][0] = lrun[nt][1] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      acc[dt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-      asm volatile("" : "+a"(acc[dt][nt]));
-    }
+      qf[s] = ok ? *reinterpret_cast<const uint4*>(s < DL ? ql + 32 * s : qr + 32 * (s - DL)) : make_uint4(0, 0, 0, 0);
   }
-  const int pos_lo = pos_of(0);
+  float mneg = FLT_MAX, mlim = -INFINITY, lrun[2] = {0.f, 0.f};
+  f32x4 acc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    asm volatile("" : "+a"(acc[dt]));
+  }
 
   // lane constants of the reads
   // (of a k-step's or output tile's number, the bits that f changes are an exclusive or of the address)
@@ -523,277 +519,170 @@ __global__ __launch_bounds__(256, WK == 1 && NT == 1 ? 2 : 1) void attn_latent_b
   typedef __attribute__((address_space(3))) const u32x4* lds_units;
   auto unit_at = [](uint32_t lds) { return __builtin_bit_cast(uint4, *(lds_units)(uintptr_t)lds); };
 
-  uint32_t va[8];  // of the buffer that the sums are taken from: the addresses of tiles 0..7
-  auto read_v = [&](int dt) {
-    const uint32_t at = va[dt & 7] + (dt >> 3) * 256;
-    const uint2 x = read_tr(at), y = read_tr(at + 16 * RANK * 2);
-    return make_uint4(x.x, x.y, y.x, y.y);
-  };
   // Both products read their operands PD ahead: read earlier, as the compiler would,
   // they take registers that there are not.
   uint4 ring[PD];
-  f32x4 sc[NT][2];
-  // scores of the chunk in buffer b; also(i) after product i
-  auto scores = [&](int b, auto&& also) {
-    uint32_t ka[4] = {buffer(b) + k_off}, rb = buffer(b) + 32 * CL * 16 + r_off;
+  f32x4 sc[2];
+  // one chunk, c, in buffer b; masked: some row of the workgroup does not see some key of the step's chunks
+  auto chunk = [&](int c, int b, bool masked) {
+    {
+      uint32_t ka[4] = {buffer(b) + k_off}, rb = buffer(b) + 32 * CL * 16 + r_off;
 #pragma unroll
-    for (int i = 1; i < 4; ++i) ka[i] = xor_here(ka[0], i * 64);
-    auto read_k = [&](int u) {
-      const int s = u >> 1, hh = u & 1;
-      if (s < DL) return unit_at(ka[s & 3] + (s >> 2) * 256 + hh * (16 * CL * 16));
-      return unit_at((s > DL ? xor_here(rb, 64) : rb) + hh * (16 * CR * 16));
-    };
-    f32x4 x[NT][2];
+      for (int i = 1; i < 4; ++i) ka[i] = xor_here(ka[0], i * 64);
+      auto read_k = [&](int u) {  // k-step u / 2 of key tile u % 2
+        const int s = u >> 1, hh = u & 1;
+        if (s < DL) return unit_at(ka[s & 3] + (s >> 2) * 256 + hh * (16 * CL * 16));
+        return unit_at((s > DL ? xor_here(rb, 64) : rb) + hh * (16 * CR * 16));
+      };
+      f32x4 x[2];
 #pragma unroll
-    for (int u = 0; u < PD; ++u) ring[u] = read_k(u);
-    __builtin_amdgcn_sched_barrier(0);
+      for (int u = 0; u < PD; ++u) ring[u] = read_k(u);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int u = 0; u < 2 * (DL + DR); ++u) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        if (u < 2) x[nt][u & 1] = mfma_first_v(ring[u % PD], qf[nt][u >> 1]);
-        else mfma_in_place_v(ring[u % PD], qf[nt][u >> 1], x[nt][u & 1]);
-        if (nt == NT - 1 && u + PD < 2 * (DL + DR)) ring[u % PD] = read_k(u + PD);
-        also(u * NT + nt);
+      for (int u = 0; u < 2 * (DL + DR); ++u) {
+        if (u < 2) x[u] = mfma_first_v(ring[u % PD], qf[u >> 1]);
+        else mfma_in_place_v(ring[u % PD], qf[u >> 1], x[u & 1]);
+        if (u + PD < 2 * (DL + DR)) ring[u % PD] = read_k(u + PD);
         __builtin_amdgcn_sched_barrier(0);
       }
-    }
-    sums_ready();
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+      sums_ready();
 #pragma unroll
       for (int hh = 0; hh < 2; ++hh) {
-        asm volatile("" : "+v"(x[nt][hh]));  // (in its place until here)
-        sc[nt][hh] = x[nt][hh];
+        asm volatile("" : "+v"(x[hh]));  // (in its place until here)
+        sc[hh] = x[hh];
       }
-  };
-  // masks of chunk c in buffer b, some key of which some row of the workgroup does not see
-  auto mask = [&](int c, int b) {
-    asm volatile("");
-    uint4* lat = &buf[(wk * NB + b) * BU];
-    if (WQ > 1) {
-      SPEC_WAIT_VM_LDS(63);
-      block_sync();  // every wave of the share has its scores
     }
-    uint32_t flags = 0;
+    if (masked) {
+      asm volatile("");
+      uint4* lat = &buf[(wk * NB + b) * BU];
+      if (WQ > 1) {
+        SPEC_WAIT_VM_LDS(63);
+        block_sync();  // every wave of the share has its scores
+      }
+      uint32_t flags = 0;  // of the chunk's keys: a latent that is not finite
 #pragma unroll 1
-    for (int i = wq; i < NLL; i += WQ) {
-      const uint4 v = lat[64 * i + lane];
-      const uint64_t m = __ballot((nonfinite_bits(v.x) | nonfinite_bits(v.y) | nonfinite_bits(v.z) | nonfinite_bits(v.w)) != 0);
-      if (m == 0) continue;
-      lat[64 * i + lane] = drop_nonfinite(v);
-      if (TP == 1) flags |= 1u << i;
-      else flags |= (static_cast<uint32_t>(m) ? 1u : 0u) << (2 * i) | (m >> 32 ? 2u : 0u) << (2 * i);
-    }
-    if (WQ > 1) {
-      if (lane == 0) s_flag[wave] = flags;
-      SPEC_WAIT_VM_LDS(63);
-      block_sync();
+      for (int i = wq; i < NLL; i += WQ) {
+        const uint4 v = lat[64 * i + lane];
+        const uint64_t bad = __ballot((nonfinite_bits(v.x) | nonfinite_bits(v.y) | nonfinite_bits(v.z) | nonfinite_bits(v.w)) != 0);
+        if (bad == 0) continue;
+        lat[64 * i + lane] = drop_nonfinite(v);
+        if (TP == 1) flags |= 1u << i;
+        else flags |= (static_cast<uint32_t>(bad) ? 1u : 0u) << (2 * i) | (bad >> 32 ? 2u : 0u) << (2 * i);
+      }
+      if (WQ > 1) {
+        if (lane == 0) s_flag[wave] = flags;
+        SPEC_WAIT_VM_LDS(63);
+        block_sync();
 #pragma unroll
-      for (int i = 0; i < WQ; ++i) flags |= s_flag[wk * WQ + i];
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+        for (int i = 0; i < WQ; ++i) flags |= s_flag[wk * WQ + i];
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int k = 16 * (j / 4) + 4 * g + j % 4;
-        if (32 * c + k > klim[nt]) sc[nt][j / 4][j % 4] = -INFINITY;
-        else if (flags >> k & 1) sc[nt][j / 4][j % 4] = __builtin_nanf("");
-      }
-  };
-  // raises the maxima where a score asks for it; true: the sums of latents have to be scaled by alpha
-  float alpha[NT];
-  auto raise = [&] {
-    float mx[NT];
-    bool up = false;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      mx[nt] = sc[nt][0][0];
-#pragma unroll
-      for (int j = 1; j < 8; ++j) mx[nt] = fmaxf(mx[nt], sc[nt][j / 4][j % 4]);
-      up |= mx[nt] > mlim[nt];
-    }
-    up = __any(up);
-    if (up) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float m = mx[nt];
-        m = fmaxf(m, __shfl_xor(m, 16, kWave));
-        m = fmaxf(m, __shfl_xor(m, 32, kWave));
-        alpha[nt] = 1.f;
-        if (m > mlim[nt]) {
-          alpha[nt] = __builtin_amdgcn_exp2f((-mneg[nt] - m) * a.scale);
-          mneg[nt] = -m;
-          mlim[nt] = m + kLatentRescaleLog2 / a.scale;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) lrun[nt][i] *= alpha[nt];
+        if (32 * c + k > klim) sc[j / 4][j % 4] = -INFINITY;
+        else if (flags >> k & 1) sc[j / 4][j % 4] = __builtin_nanf("");
       }
     }
-    return up;
-  };
-  auto rescale = [&] {
-    sums_ready();
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) scale_in_place(acc[dt][nt], alpha[nt]);
-  };
-  // Probability of score e / 3 (of tile e / 24), in three pieces: the exponent, the power, and
-  // the sum with every second pair as bf16, as the values that they weight: the rounding
-  // stays below the output's.  A product takes the matrix unit 16 cycles and the wave's
-  // issue 4: about a piece fits behind each.
-  uint32_t pf[NT][4];
-  constexpr int E = 24 * NT;
-  auto prob = [&](int e, uint32_t (&to)[NT][4]) {
-    const int nt = e / 24, j = e / 3 % 8;
-    float x = sc[nt][j / 4][j % 4];
-    if (e % 3 == 0) x = (x + mneg[nt]) * a.scale;
-    else if (e % 3 == 1) x = __builtin_amdgcn_exp2f(x);
-    else lrun[nt][j % 2] += x;
-    if (e % 3 < 2) stay_here(x);
-    else stay_here(lrun[nt][j % 2]);
-    sc[nt][j / 4][j % 4] = x;
-    if (e % 3 == 2 && j % 2) to[nt][j / 2] = cvt_pk_bf16(sc[nt][j / 4][j % 4 - 1], x);
-  };
-  // sums of latents += the chunk whose first PD operands are read; also(i) after product i
-  auto first_v = [&](int b) {
-    va[0] = buffer(b) + v_off;
+    // the second product's first operands are on their way during the softmax
+    uint32_t va[8] = {buffer(b) + v_off};
 #pragma unroll
     for (int i = 1; i < 8; ++i) va[i] = xor_here(va[0], i * 32);
+    auto read_v = [&](int dt) {
+      const uint32_t at = va[dt & 7] + (dt >> 3) * 256;
+      const uint2 x = read_tr(at), y = read_tr(at + 16 * RANK * 2);
+      return make_uint4(x.x, x.y, y.x, y.y);
+    };
 #pragma unroll
     for (int u = 0; u < PD; ++u) ring[u] = read_v(u);
-  };
-  auto sums = [&](auto&& also) {
+    float top = sc[0][0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) top = fmaxf(top, sc[j / 4][j % 4]);
+    if (__any(top > mlim)) {
+      top = fmaxf(top, __shfl_xor(top, 16, kWave));
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      float alpha = 1.f;
+      if (top > mlim) {
+        alpha = __builtin_amdgcn_exp2f((-mneg - top) * a.scale);
+        mneg = -top;
+        mlim = top + kLatentRescaleLog2 / a.scale;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) lrun[i] *= alpha;
+      sums_ready();
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) scale_in_place(acc[dt], alpha);
+    }
+    float p[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f((sc[j / 4][j % 4] + mneg) * a.scale);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) lrun[j % 2] += p[j];
+    // bf16, as the values that they weight: the rounding stays below the output's
+    const uint4 pf = make_uint4(cvt_pk_bf16(p[0], p[1]), cvt_pk_bf16(p[2], p[3]), cvt_pk_bf16(p[4], p[5]), cvt_pk_bf16(p[6], p[7]));
     operands_ready();
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        mfma_in_place(ring[dt % PD], make_uint4(pf[nt][0], pf[nt][1], pf[nt][2], pf[nt][3]), acc[dt][nt]);
-        if (nt == NT - 1 && dt + PD < DT) ring[dt % PD] = read_v(dt + PD);
-        also(dt * NT + nt);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      mfma_in_place(ring[dt % PD], pf, acc[dt]);
+      if (dt + PD < DT) ring[dt % PD] = read_v(dt + PD);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
-  auto no_more = [](int) {};
 
-  if constexpr (PIPE) {
-    // A chunk's probabilities are taken between the products of the sums of the one
-    // before, and the loads are spread over the products of the scores: issued
-    // together, either holds a wave that has its SIMD to itself.
-    constexpr int LA = NB - 1;  // chunks that loads are ahead
-    constexpr int LQ = (LPW + 1) / 2, MS = 2 * (DL + DR) * NT, MV = DT * NT;  // products of the scores and of the sums
-    // (loads past the item's last chunk are of its last page: a branch around them would let
-    // the compiler gather up what is to be between the products)
-#pragma unroll
-    for (int i = 0; i < LA; ++i) issue(c0 + i, i);
-    SPEC_WAIT_VM_LDS((LA - 1) * (NL / WQ));
-    block_sync();
-    scores(0, no_more);
-    if (32 * c0 + 31 > pos_lo || 32 * c0 + 31 >= it.t1) mask(c0, 0);
-    raise();
-#pragma unroll
-    for (int e = 0; e < E; ++e) prob(e, pf);
-    for (int j = 0; j + 1 < nch; ++j) {
-      const int b = j % NB, bn = (j + 1) % NB, c = c0 + j + 1;
-      const uint32_t dst = buffer((j + LA) % NB);
-      // chunk j + 1 has landed (those behind it may be in flight), and every wave is done with chunk j - 1
-      SPEC_WAIT_VM_LDS((LA - 2) * (NL / WQ));
-      block_sync();
-      take(c0 + j + LA);
-      scores(bn, [&](int i) {
-        if (i % (MS / LQ) == 2 && i / (MS / LQ) < LQ) load(i / (MS / LQ), dst);
-      });
-      if (32 * c + 31 > pos_lo || 32 * c + 31 >= it.t1) mask(c, bn);
-      const bool up = raise();
-      first_v(b);
-      uint32_t next[NT][4];
-      sums([&](int i) {
-        constexpr int step = MV / (LPW - LQ);
-        if (i % step == 1 && i / step < LPW - LQ) load(LQ + i / step, dst);
-#pragma unroll
-        for (int e = i * E / MV; e < (i + 1) * E / MV; ++e) prob(e, next);
-      });
-      if (up) rescale();
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) pf[nt][i] = next[nt][i];
+  // (a share's chunk past the last is loaded from the last page, and masked)
+  if (NB == 2) issue(c0 + wk, 0);
+  for (int j = 0; j < nit; ++j) {
+    const int c = c0 + j * WK + wk, b = NB == 2 ? j & 1 : 0;
+    if (NB == 2) {
+      SPEC_WAIT_VM_LDS(0);
+      block_sync();  // chunk j has landed, and every wave is done with the one before
+      if (j + 1 < nit) issue(c + WK, (j + 1) & 1);
+    } else {  // a buffer of the wave's own
+      SPEC_WAIT_VM_LDS(0);
+      wave_fence();
+      issue(c, 0);
+      SPEC_WAIT_VM_LDS(0);
+      wave_fence();
     }
-    first_v((nch - 1) % NB);
-    sums(no_more);
-    SPEC_WAIT_VM_LDS(0);  // (no load outlives the buffers)
-  } else {
-    // (a share's chunk past the last is loaded from the last page, and masked)
-    if (NB == 2) issue(c0 + wk, 0);
-    for (int j = 0; j < nit; ++j) {
-      const int c = c0 + j * WK + wk, b = NB == 2 ? j & 1 : 0;
-      if (NB == 2) {
-        SPEC_WAIT_VM_LDS(0);
-        block_sync();  // chunk j has landed, and every wave is done with the one before
-        if (j + 1 < nit) issue(c + WK, (j + 1) & 1);
-      } else {  // a buffer of the wave's own
-        SPEC_WAIT_VM_LDS(0);
-        wave_fence();
-        issue(c, 0);
-        SPEC_WAIT_VM_LDS(0);
-        wave_fence();
-      }
-      scores(b, no_more);
-      const int last = 32 * (c0 + (j + 1) * WK) - 1;  // (the same for every share: mask has barriers)
-      if (last > pos_lo || last >= it.t1) mask(c, b);
-      first_v(b);
-      if (raise()) rescale();
-#pragma unroll
-      for (int e = 0; e < E; ++e) prob(e, pf);
-      sums(no_more);
-    }
+    const int last = 32 * (c0 + (j + 1) * WK) - 1;  // (the same for every share: a masked chunk has barriers)
+    chunk(c, b, last > pos_lo || last >= it.t1);
   }
 
   sums_ready();
+  float l = lrun[0] + lrun[1];
+  l += __shfl_xor(l, 16, kWave);
+  l += __shfl_xor(l, 32, kWave);
+  if constexpr (WK == 1) {
+    if (!ok) return;
+    if (it.part < 0) {
+      const float inv = 1.f / l;
+      bf16_t* o = static_cast<bf16_t*>(a.o_lat) + static_cast<size_t>(it.qv0 + m) * RANK + 4 * g;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    float l = lrun[nt][0] + lrun[nt][1];
-    l += __shfl_xor(l, 16, kWave);
-    l += __shfl_xor(l, 32, kWave);
-    const int m = m0 + 16 * nt + l16;
-    if constexpr (WK == 1) {
-      if (m >= it.nqv) continue;
-      if (it.part < 0) {
-        const float inv = 1.f / l;
-        bf16_t* o = static_cast<bf16_t*>(a.o_lat) + static_cast<size_t>(it.qv0 + m) * RANK + 4 * g;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const f32x4 v = acc[dt][nt] * inv;
-          put4(o + 16 * dt, v[0], v[1], v[2], v[3]);
-        }
-      } else {
-        const size_t pv = static_cast<size_t>(it.part) * Q + m;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(a.part_o + pv * RANK + 16 * dt + 4 * g) = acc[dt][nt];
-        if (g == 0) {
-          a.part_ml[2 * pv] = -mneg[nt];
-          a.part_ml[2 * pv + 1] = l;
-        }
+      for (int dt = 0; dt < DT; ++dt) {
+        const f32x4 v = acc[dt] * inv;
+        put4(o + 16 * dt, v[0], v[1], v[2], v[3]);
       }
     } else {
-      __syncthreads();  // every wave is done with its keys
-      float* so = reinterpret_cast<float*>(buf);
-      const int at = wk * Q + m;
+      const size_t pv = static_cast<size_t>(it.part) * Q + m;
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(so + at * (RANK + 4) + 16 * dt + 4 * g) = acc[dt][nt];
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(a.part_o + pv * RANK + 16 * dt + 4 * g) = acc[dt];
       if (g == 0) {
-        s_ml[2 * at] = -mneg[nt];
-        s_ml[2 * at + 1] = l;
+        a.part_ml[2 * pv] = -mneg;
+        a.part_ml[2 * pv + 1] = l;
       }
     }
-  }
-  if constexpr (WK > 1) {
+  } else {
+    __syncthreads();  // every wave is done with its keys
+    float* so = reinterpret_cast<float*>(buf);
+    const int at = wk * Q + m;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(so + at * (RANK + 4) + 16 * dt + 4 * g) = acc[dt];
+    if (g == 0) {
+      s_ml[2 * at] = -mneg;
+      s_ml[2 * at + 1] = l;
+    }
     __syncthreads();
-    join_waves<bf16_t, RANK, WK, Q>(a, it, reinterpret_cast<const float*>(buf), s_ml, Q);
+    join_waves<bf16_t, RANK, WK, Q>(a, it, so, s_ml, Q);
   }
 }
 
@@ -923,24 +812,25 @@ hipError_t launch_attention(const LatentArgs& a, const LatentItem* items, int n,
     if (tile != 16) return hipErrorInvalidValue;
     launch_kernel(attn_latent_f32_kernel<RANK, ROPE>, dim3(n), dim3(256), 0, st, a, items);
   } else if (tile == 16) {
-    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 1, 1, 4>, dim3(n), dim3(256), 0, st, a, items);
+    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 1, 4>, dim3(n), dim3(256), 0, st, a, items);
   } else if (tile == 32) {
-    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 1, 2, 2>, dim3(n), dim3(256), 0, st, a, items);
+    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 2, 2>, dim3(n), dim3(256), 0, st, a, items);
   } else if (tile == 64) {
-    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 1, 4, 1>, dim3(n), dim3(256), 0, st, a, items);
-  } else if (tile == 128) {
-    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 2, 4, 1>, dim3(n), dim3(256), 0, st, a, items);
+    launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 4, 1>, dim3(n), dim3(256), 0, st, a, items);
   } else {
     return hipErrorInvalidValue;
   }
   return hipGetLastError();
 }
 
-// Row blocks of the two products: at most about 1024 workgroups.
-unsigned row_blocks(int R, unsigned columns) {
-  const unsigned tiles = (static_cast<unsigned>(R) + 15) / 16;
-  return std::max(1u, std::min(tiles, 1024 / std::max(1u, columns)));
+// Row blocks of the two products: at most about `most` workgroups.
+unsigned row_blocks(int R, unsigned columns, int rows, unsigned most) {
+  const unsigned tiles = (static_cast<unsigned>(R) + rows - 1) / rows;
+  return std::max(1u, std::min(tiles, most / std::max(1u, columns)));
 }
+
+// Rows up to which the values' products are split over a workgroup's waves.
+constexpr int kSplitValueRows = 48;
 
 }  // namespace
 
@@ -965,7 +855,7 @@ hipError_t launch_rope_latent(int dtype, int R, int H, int nope, int rope, int r
 hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st) {
   if (a.R <= 0) return hipSuccess;
   const unsigned columns = static_cast<unsigned>(a.H) * (a.rank / 64);
-  const dim3 grid(columns, row_blocks(a.R, columns));
+  const dim3 grid(columns, row_blocks(a.R, columns, 16, 2048));
   if (a.nope == 64 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<64>, grid, dim3(256), 0, st, a);
   else if (a.nope == 128 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<128>, grid, dim3(256), 0, st, a);
   else if (a.nope == 64) launch_kernel(latent_absorb_bf16_kernel<64>, grid, dim3(256), 0, st, a);
@@ -977,11 +867,14 @@ hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st) {
 hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st) {
   if (a.R <= 0) return hipSuccess;
   const unsigned columns = static_cast<unsigned>(a.H) * (a.vdim / 16);
-  const dim3 grid(columns, row_blocks(a.R, columns));
+  const bool split = a.dtype == 0 || a.R <= kSplitValueRows;
+  const dim3 grid(columns, row_blocks(a.R, columns, split ? 16 : 64, 2048));
   if (a.rank == 256 && a.dtype == 0) launch_kernel(latent_values_f32_kernel<256>, grid, dim3(256), 0, st, a);
   else if (a.rank == 512 && a.dtype == 0) launch_kernel(latent_values_f32_kernel<512>, grid, dim3(256), 0, st, a);
-  else if (a.rank == 256) launch_kernel(latent_values_bf16_kernel<256>, grid, dim3(256), 0, st, a);
-  else if (a.rank == 512) launch_kernel(latent_values_bf16_kernel<512>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 256 && split) launch_kernel(latent_values_bf16_kernel<256, true>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 256) launch_kernel(latent_values_bf16_kernel<256, false>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 512 && split) launch_kernel(latent_values_bf16_kernel<512, true>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 512) launch_kernel(latent_values_bf16_kernel<512, false>, grid, dim3(256), 0, st, a);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }
@@ -999,7 +892,7 @@ hipError_t launch_latent_attention(const LatentArgs& a, const LatentItem* items,
 hipError_t launch_latent_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int tile, int max_parts,
                                  hipStream_t st) {
   if (n_groups <= 0) return hipSuccess;
-  if (static_cast<size_t>(n_groups) * tile > kMaxGrid256 || max_parts > kCombineMaxParts) return hipErrorInvalidValue;
+  if (static_cast<size_t>(n_groups) * tile > kMaxGrid256 || max_parts > kLatentMaxParts) return hipErrorInvalidValue;
   auto go = [&](auto t, auto rank) {
     using T = decltype(t);
     constexpr int RANK = decltype(rank)::value;

@@ -1,5 +1,5 @@
-// Device helpers of the latent attention's kernels, whose waves have a SIMD (and its 512
-// registers) to themselves: products in place, and the order they are issued in.
+// Device helpers of the absorbed latent attention: products in place, and the order they
+// are issued in.
 #pragma once
 
 #include "common.h"
@@ -36,8 +36,6 @@ __device__ __forceinline__ uint32_t xor_here(uint32_t x, uint32_t k) {
   asm volatile("v_xor_b32 %0, %1, %2" : "=v"(x) : "s"(k), "v"(x));
   return x;
 }
-// Has x computed before the products that follow: the compiler would sink it to its use.
-__device__ __forceinline__ void stay_here(float& x) { asm volatile("" : "+v"(x)); }
 // c *= x for such a sum, which stays where it is.
 __device__ __forceinline__ void scale_in_place(f32x4& c, float x) {
 #pragma unroll

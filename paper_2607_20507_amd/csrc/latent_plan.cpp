@@ -6,16 +6,40 @@
 
 namespace spec {
 
-LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_parts, bool fp32) {
+namespace {
+
+// The least split of at least `lo` that makes at most `target` items (hi makes as few as
+// there can be).
+template <typename F>
+int64_t least_split(int64_t lo, int64_t hi, int64_t target, F&& items) {
+  hi = std::max(lo, hi);
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    if (items(mid) <= target) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+constexpr int kCus = 256;
+
+}  // namespace
+
+LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, bool fp32) {
   LatentPlan p;
   int64_t most = 1;
   for (const LatentSegment& s : segs) most = std::max<int64_t>(most, static_cast<int64_t>(s.nrows) * H);
-  p.tile = fp32 || most <= 16 ? 16 : most <= 32 ? 32 : most <= 64 ? 64 : 128;
+  // The narrowest tile that holds a sequence's query vectors, at most 64 (32 heads of rank
+  // 512; tiles of 16 / 32 / 64, us a call): one token of 64 sequences 70 / 56 / 60, the same
+  // of 131000 keys 71 / 53 / 55, 4 to 8 rows of 64 sequences 201 / 172 / 128; 16 heads of rank
+  // 256, one token of 64 sequences 36 / 40 / 40.  (Tiles of 128, a wave with 32 query vectors
+  // and its SIMD to itself, took 131 for the second last.)
+  p.tile = fp32 || most <= 16 ? 16 : most <= 32 ? 32 : 64;
   struct Tile {
     int32_t qv0, nqv, row0, pos0, page0, kend, qoff;
   };
   std::vector<Tile> tiles;
-  int64_t most_keys = 0;
+  int64_t most_keys = 0, all_keys = 0;
   for (const LatentSegment& s : segs) {
     const int64_t first = static_cast<int64_t>(s.row0) * H, n = static_cast<int64_t>(s.nrows) * H;
     for (int64_t m = 0; m < n; m += p.tile) {
@@ -23,28 +47,24 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_pa
       const int kend = static_cast<int>(s.pos0 + (m + c - 1) / H + 1);  // keys 0 .. its last row's position
       tiles.push_back(Tile{static_cast<int32_t>(first + m), static_cast<int32_t>(c), s.row0, s.pos0, s.page0, kend, s.qoff});
       most_keys = std::max<int64_t>(most_keys, kend);
+      all_keys += kend;
     }
   }
-  const int target = 256, least = 4;
-  // the least split, in chunks of 32 keys, that makes at most `target` items (or one for each tile)
-  auto items = [&](int64_t sp) {
-    int64_t n = 0;
-    for (const Tile& t : tiles) n += (t.kend + sp - 1) / sp;
-    return n;
-  };
-  int64_t lo = least, hi = std::max<int64_t>(least, (most_keys + 31) / 32);
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (items(32 * mid) <= std::max<int64_t>(target, static_cast<int64_t>(tiles.size()))) hi = mid;
-    else lo = mid + 1;
-  }
-  int64_t split = 32 * lo;
-  auto parts = [&](int64_t sp) {
-    int64_t n = 0;
-    for (const Tile& t : tiles) n += t.kend > sp ? (t.kend + sp - 1) / sp : 0;
-    return n;
-  };
-  while (parts(split) > max_parts) split *= 2;
+  // Items that run at once, one a CU.  Two a CU (the 64-wide ones have the registers for it)
+  // hide each other's starts and ends, but halve the keys of an item, whose parts of 2 KB a
+  // query vector are written and read again: the better choice where an item has much to do
+  // (keys of all tiles a CU; 256 / 384 items, us): 187 keys 48.3 / 54.2, 312 keys 53.8 / 58.5, 940
+  // 83.6 / 86.4, 1300 155 / 128, 2344 158 / 145.
+  const int target = p.tile == 64 && all_keys / kCus >= 1200 ? kCus * 3 / 2 : kCus;
+  // At least a chunk for every wave that takes keys of its own; fp32 one page (133 keys of 2
+  // tiles in 2 parts each 24.1 us, in 3 22.9).
+  const int least = fp32 ? 2 : 4;
+  const int64_t split = 32 * least_split(least, (most_keys + 31) / 32, std::max<int64_t>(target, static_cast<int64_t>(tiles.size())),
+                                         [&](int64_t sp) {
+                                           int64_t n = 0;
+                                           for (const Tile& t : tiles) n += (t.kend + 32 * sp - 1) / (32 * sp);
+                                           return n;
+                                         });
   for (const Tile& t : tiles) {
     const int c = static_cast<int>((t.kend + split - 1) / split);
     if (c <= 1) {
@@ -65,21 +85,58 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int max_pa
 
 LatentPromptPlan plan_latent_prompt(const std::vector<LatentSegment>& segs, int H) {
   LatentPromptPlan p;
-  auto blocks = [&](int rows) {
-    int64_t n = 0;
-    for (const LatentSegment& s : segs) n += (static_cast<int64_t>(s.nrows) + rows - 1) / rows;
-    return n * H;
+  // Blocks of 128 rows take 0.7 of the time of 256.  Where the CUs have much to do (300 keys of
+  // 128-row blocks each, or more) the form with less work in all is the faster one, else
+  // the smaller blocks, which share it out (32 heads of 128, 256 / 128 rows, us): 300 rows behind 8000
+  // keys 181 / 195, 4 x 300 rows 46.6 / 48.5, 512 behind 2000 78.3 / 80.8; 130 behind 500 42.6 / 39.6,
+  // 4 x 200 39.6 / 35.0, 512 41.7 / 35.7; 96 behind 8000 135 / 123.
+  int64_t wide = 0, narrow = 0, keys = 0;
+  for (const LatentSegment& s : segs) {
+    wide += (static_cast<int64_t>(s.nrows) + 255) / 256;
+    narrow += (static_cast<int64_t>(s.nrows) + 127) / 128;
+    for (int64_t r = 0; r < s.nrows; r += 128) keys += s.pos0 + std::min<int64_t>(r + 128, s.nrows);
+  }
+  p.rows = keys * H / kCus >= 300 && wide * 100 <= narrow * 70 ? 256 : 128;
+  struct Block {
+    int32_t row, nrows, pos, page0, kend;
   };
-  if (blocks(256) < 256) p.rows = 128;
+  std::vector<Block> tiles;
+  int64_t most_keys = 0;
   for (const LatentSegment& s : segs)
     for (int64_t r = 0; r < s.nrows; r += p.rows) {
       const int n = static_cast<int>(std::min<int64_t>(p.rows, s.nrows - r)), first = static_cast<int>(r);
-      p.items.push_back(LatentItem{s.row0 + s.qoff + first, n, 0, s.pos0 + first, s.page0, 0, s.pos0 + first + n, -1, 0});
+      tiles.push_back(Block{s.row0 + s.qoff + first, n, s.pos0 + first, s.page0, s.pos0 + first + n});
+      most_keys = std::max<int64_t>(most_keys, tiles.back().kend);
     }
-  std::stable_sort(p.items.begin(), p.items.end(), [](const LatentItem& x, const LatentItem& y) { return x.t1 > y.t1; });
+  // the least range of keys, in 64s and at least 256, with which the workgroups run at once
+  const int64_t split = 64 * least_split(4, (most_keys + 63) / 64, std::max<int64_t>(kCus / H, static_cast<int64_t>(tiles.size())),
+                                         [&](int64_t sp) {
+                                           int64_t n = 0;
+                                           for (const Block& t : tiles) n += (t.kend + 64 * sp - 1) / (64 * sp);
+                                           return n;
+                                         });
+  for (const Block& t : tiles) {
+    const int c = static_cast<int>((t.kend + split - 1) / split);
+    if (c > 1) p.groups.push_back(LatentGroup{t.row, t.nrows, p.n_parts, c});
+    for (int i = 0; i < c; ++i)
+      p.items.push_back(LatentItem{t.row, t.nrows, 0, t.pos, t.page0, static_cast<int32_t>(i * split),
+                                   static_cast<int32_t>(std::min<int64_t>(t.kend, (i + 1) * split)), c > 1 ? p.n_parts + i : -1, 0});
+    if (c > 1) p.n_parts += c;
+  }
+  std::stable_sort(p.items.begin(), p.items.end(),
+                   [](const LatentItem& x, const LatentItem& y) { return x.t1 - x.t0 > y.t1 - y.t0; });
   return p;
 }
 
-bool latent_expands(int nrows, int pos0) { return nrows >= 256; }
+// The expanded form makes every head's keys and values of all pos0 + nrows tokens, whatever
+// the rows, and then has a third of the absorbed form's work a row and key.  The border
+// in rows grows with what is made for the keys before them (absorbed / expanded, us; 32
+// heads, 8M weights): 24 rows 29.6 / 19.3, 24 behind 500 39.6 / 30.8, 48 behind 2000 54 / 50, 96
+// behind 2000 64.5 / 53.2, 130 behind 8000 121 / 138, 200 behind 8000 150 / 144; 8 heads, 130
+// behind 8000 70.9 / 61.8, 48 52.7 / 58.1; 16 heads of 64 dims and rank 256, 48 behind 8000 45.3 / 41.2,
+// 24 40.9 / 41.0.
+bool latent_expands(int nrows, int pos0, int64_t weights) {
+  return nrows >= 24 + static_cast<double>(pos0) * static_cast<double>(weights) / 1.9e8;
+}
 
 }  // namespace spec

@@ -144,7 +144,8 @@ __global__ __launch_bounds__(256, 3) void latent_expand_kernel(LatentArgs a, con
 
 // ---------------------------------------------------------------------------
 // Attention to the expanded pages: one workgroup of 8 waves (two per SIMD) per (block
-// of 128 NT consecutive rows, head).  The structure is the K / V cache's prompt kernel's
+// of 128 NT consecutive rows, head, range of keys: all, or a part where blocks and
+// heads leave CUs idle).  The structure is the K / V cache's prompt kernel's
 // (attention.hip): 64 keys at a time in LDS, three buffers; each wave both products for
 // its own 16 NT rows; a 32-key chunk is a matrix phase and a vector phase, and waves 4..7
 // run one phase behind waves 0..3, with which they share the SIMDs.  A key's score has
@@ -167,7 +168,9 @@ template <int NOPE, int ROPE, int VD, int NT>
 __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a, const LatentItem* __restrict__ items,
                                                                     const bf16_t* __restrict__ kx,
                                                                     const bf16_t* __restrict__ vx,
-                                                                    const bf16_t* __restrict__ rx) {
+                                                                    const bf16_t* __restrict__ rx,
+                                                                    float* __restrict__ part_o,
+                                                                    float* __restrict__ part_ml) {
   constexpr int DN = NOPE / 32, DS = DN + ROPE / 32;  // k-steps of the scores: own dims, all
   constexpr int DT = VD / 16;
   constexpr int NW = 8, NB = 3;
@@ -184,13 +187,14 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, l16 = lane & 15;
-  const int t1 = it.t1, ns = (t1 + 63) >> 6;
+  const int t0 = it.t0, t1 = it.t1, ns = (t1 - t0 + 63) >> 6;
 
   // the next stage into buffer b.  Pages past the sequence's last are other pages, or what
   // the workspace has behind them (their keys are masked, and their values not used)
-  const char* next_k = reinterpret_cast<const char*>(kx) + (static_cast<size_t>(it.page0) * a.H + h) * (32 * NOPE);
-  const char* next_v = reinterpret_cast<const char*>(vx) + (static_cast<size_t>(it.page0) * a.H + h) * (32 * VD);
-  const char* next_r = reinterpret_cast<const char*>(rx) + static_cast<size_t>(it.page0) * (32 * ROPE);
+  const int page0 = it.page0 + (t0 >> 4);
+  const char* next_k = reinterpret_cast<const char*>(kx) + (static_cast<size_t>(page0) * a.H + h) * (32 * NOPE);
+  const char* next_v = reinterpret_cast<const char*>(vx) + (static_cast<size_t>(page0) * a.H + h) * (32 * VD);
+  const char* next_r = reinterpret_cast<const char*>(rx) + static_cast<size_t>(page0) * (32 * ROPE);
   const size_t page_k = static_cast<size_t>(a.H) * (32 * NOPE), page_v = static_cast<size_t>(a.H) * (32 * VD);
   size_t of_k[WK], of_v[WV];
 #pragma unroll
@@ -224,7 +228,7 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
     }
   }
   const int pos_lo = it.pos0 + 16 * NT * wave;
-  const int pos_hi = it.pos0 + min(16 * NT * (wave + 1), it.nqv) - 1;
+  const int pos_hi = min(it.pos0 + min(16 * NT * (wave + 1), it.nqv), t1) - 1;
   const float scale = a.scale;
   // minus the running maximum, minus its logit (-inf: no key yet, every p is 0; 0 where logits
   // are large), the score above which it is raised (-inf: no key yet), two partial sums of p
@@ -396,10 +400,10 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
     const int b = j % NB, bn = (j + 1) % NB;
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
-      const int c0 = 64 * j + 32 * hf;
+      const int c0 = t0 + 64 * j + 32 * hf;
       // matrix phase (chunks above every row of this wave are left out); the sums come
       // first, so that their operands are gone when the scores' need registers
-      if (c0 >= 32 && c0 - 32 <= pos_hi) output(c0 - 32);
+      if (c0 > t0 && c0 - 32 <= pos_hi) output(c0 - 32);
       __builtin_amdgcn_sched_barrier(0);
       if (c0 <= pos_hi) {
         read_r(b, hf);
@@ -419,10 +423,10 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
       phase_end();
     }
   }
-  if (64 * ns - 32 <= pos_hi) output(64 * ns - 32);
+  if (t0 + 64 * ns - 32 <= pos_hi) output(t0 + 64 * ns - 32);
   if (wave < 4) phase_end();
   if (dropped)
-    for (int c0 = max(pos_lo - 31, 0) / 32 * 32; c0 <= pos_hi; c0 += 32) {
+    for (int c0 = max(max(pos_lo - 31, 0) / 32 * 32, t0); c0 <= pos_hi; c0 += 32) {
       if (c0 + 31 <= pos_lo) continue;
       const uint4* vb = reinterpret_cast<const uint4*>(
           vx + ((static_cast<size_t>(it.page0) + min((c0 + 8 * g) >> 4, (t1 - 1) >> 4)) * a.H + h) * (16 * VD));
@@ -442,21 +446,74 @@ __global__ __launch_bounds__(512, 1) void attn_latent_prompt_kernel(LatentArgs a
     l += __shfl_xor(l, 32, kWave);
     const int m = 16 * (NT * wave + nt) + l16;
     if (m >= it.nqv) continue;
-    const float inv = 1.f / l;
-    bf16_t* o = static_cast<bf16_t*>(a.out) + (static_cast<size_t>(it.qv0 + m) * a.H + h) * VD + 4 * g;
+    if (it.part < 0) {
+      const float inv = 1.f / l;
+      bf16_t* o = static_cast<bf16_t*>(a.out) + (static_cast<size_t>(it.qv0 + m) * a.H + h) * VD + 4 * g;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const f32x4 v = acc[dt][nt] * inv;
-      *reinterpret_cast<uint2*>(o + 16 * dt) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
+      for (int dt = 0; dt < DT; ++dt) {
+        const f32x4 v = acc[dt][nt] * inv;
+        *reinterpret_cast<uint2*>(o + 16 * dt) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
+      }
+    } else {
+      // a part's reference is its maximum itself, without the rounding of its logit
+      const bool none = mlim[nt] == -INFINITY;
+      const float fix = none || add[nt] == 0.f ? 1.f : __builtin_amdgcn_exp2f(-fmaf(-mneg[nt], scale, add[nt]));
+      const size_t pv = (static_cast<size_t>(it.part) * (16 * NT * NW) + m) * a.H + h;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(part_o + pv * VD + 16 * dt + 4 * g) = acc[dt][nt] * fix;
+      if (g == 0) *reinterpret_cast<float2*>(part_ml + 2 * pv) = make_float2(none ? -FLT_MAX : -mneg[nt], l * fix);
     }
   }
+}
+
+// The parts of a block's rows to its output: a thread has four dims of one row and head.
+template <int VD>
+__global__ __launch_bounds__(256) void latent_prompt_combine_kernel(LatentArgs a, const LatentGroup* __restrict__ groups, int rows,
+                                                                    const float* __restrict__ part_o,
+                                                                    const float* __restrict__ part_ml) {
+  constexpr int U = VD / 4, HB = 256 / U;  // threads of a head, heads of a workgroup
+  const LatentGroup gr = groups[blockIdx.x / rows];
+  const int r = blockIdx.x % rows, h = blockIdx.y * HB + threadIdx.x / U, d = 4 * (threadIdx.x % U);
+  if (r >= gr.nqv || h >= a.H) return;
+  const size_t first = (static_cast<size_t>(gr.part0) * rows + r) * a.H + h, step = static_cast<size_t>(rows) * a.H;
+  constexpr int B = 8;
+  float top = -FLT_MAX;
+  for (int p0 = 0; p0 < gr.nparts; p0 += B) {
+    float m[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) m[b] = part_ml[2 * (first + min(p0 + b, gr.nparts - 1) * step)];
+#pragma unroll
+    for (int b = 0; b < B; ++b) top = fmaxf(top, m[b]);
+  }
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  for (int p0 = 0; p0 < gr.nparts; p0 += B) {
+    f32x4 v[B];
+    float2 ml[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const size_t at = first + min(p0 + b, gr.nparts - 1) * step;
+      v[b] = *reinterpret_cast<const f32x4*>(part_o + at * VD + d);
+      ml[b] = *reinterpret_cast<const float2*>(part_ml + 2 * at);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+      if (p0 + b < gr.nparts) {
+        const float w = __builtin_amdgcn_exp2f((ml[b].x - top) * a.scale);
+        l += w * ml[b].y;
+        o += w * v[b];
+      }
+  }
+  o *= 1.f / l;
+  *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + (static_cast<size_t>(gr.qv0 + r) * a.H + h) * VD + d) =
+      make_uint2(cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]));
 }
 
 template <int NOPE, int ROPE, int VD>
 hipError_t launch_prompt(const LatentArgs& a, const LatentItem* items, unsigned n, int rows, const LatentExpanded& x, hipStream_t st) {
   const bf16_t *k = static_cast<const bf16_t*>(x.k), *v = static_cast<const bf16_t*>(x.v), *key = static_cast<const bf16_t*>(x.key);
-  if (rows == 256) launch_kernel(attn_latent_prompt_kernel<NOPE, ROPE, VD, 2>, dim3(n), dim3(512), 0, st, a, items, k, v, key);
-  else launch_kernel(attn_latent_prompt_kernel<NOPE, ROPE, VD, 1>, dim3(n), dim3(512), 0, st, a, items, k, v, key);
+  if (rows == 256) launch_kernel(attn_latent_prompt_kernel<NOPE, ROPE, VD, 2>, dim3(n), dim3(512), 0, st, a, items, k, v, key, x.part_o, x.part_ml);
+  else launch_kernel(attn_latent_prompt_kernel<NOPE, ROPE, VD, 1>, dim3(n), dim3(512), 0, st, a, items, k, v, key, x.part_o, x.part_ml);
   return hipGetLastError();
 }
 
@@ -489,6 +546,18 @@ hipError_t launch_latent_prompt(const LatentArgs& a, const LatentItem* items, in
     case 6: return launch_prompt<128, 64, 64>(a, items, g, rows, x, st);
     default: return launch_prompt<128, 64, 128>(a, items, g, rows, x, st);
   }
+}
+
+hipError_t launch_latent_prompt_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int rows,
+                                        const LatentExpanded& x, hipStream_t st) {
+  if (n_groups <= 0) return hipSuccess;
+  const int hb = 1024 / a.vdim;
+  const size_t n = static_cast<size_t>(n_groups) * rows;
+  const dim3 grid(static_cast<unsigned>(n), (a.H + hb - 1) / hb);
+  if (n * grid.y > kMaxGrid256) return hipErrorInvalidValue;
+  if (a.vdim == 128) launch_kernel(latent_prompt_combine_kernel<128>, grid, dim3(256), 0, st, a, groups, rows, x.part_o, x.part_ml);
+  else launch_kernel(latent_prompt_combine_kernel<64>, grid, dim3(256), 0, st, a, groups, rows, x.part_o, x.part_ml);
+  return hipGetLastError();
 }
 
 }  // namespace spec

@@ -658,7 +658,7 @@ struct LatentCall {
   int R = 0;                       // their number
   LatentPlan plan;
   LatentPromptPlan x;
-  size_t o_q = 0, o_o = 0, o_part = 0, o_ml = 0, o_k = 0, o_v = 0, o_key = 0, bytes = 0;
+  size_t o_q = 0, o_o = 0, o_part = 0, o_ml = 0, o_k = 0, o_v = 0, o_key = 0, o_xpart = 0, o_xml = 0, bytes = 0;
 };
 
 // Most bytes of expanded keys and values: beyond it (131072 keys of 32 heads of 128
@@ -680,6 +680,7 @@ LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const
                 "spec_op_attention_latent: nope_dim and v_dim must be 64 or 128, rope_dim 32 or 64, rank 256 or 512");
   if (n_seqs > 0 && (!rows || !pos0)) return fail(SPEC_E_INVALID, "spec_op_attention_latent: null pointer");
   const int64_t x_page = int64_t{32} * (static_cast<int64_t>(n_heads) * (nope_dim + v_dim) + rope_dim);  // bytes
+  const int64_t weights = static_cast<int64_t>(n_heads) * (nope_dim + v_dim) * rank;
   std::vector<LatentSegment> segs, x_segs;
   for (int i = 0; i < n_seqs; ++i) {
     const int64_t len = static_cast<int64_t>(pos0[i]) + rows[i], pages = (len + 15) / 16;
@@ -690,7 +691,7 @@ LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const
     if (rows[i] == 0) continue;
     if (c.pages + pages > kMaxExtent) return fail(SPEC_E_INVALID, "spec_op_attention_latent: too many pages");
     const int32_t row = static_cast<int32_t>(c.rows);
-    if (dtype == SPEC_BF16 && latent_expands(rows[i], pos0[i]) && (c.x_pages + pages) * x_page <= kLatentMaxExpanded) {
+    if (dtype == SPEC_BF16 && latent_expands(rows[i], pos0[i], weights) && (c.x_pages + pages) * x_page <= kLatentMaxExpanded) {
       x_segs.push_back(LatentSegment{0, rows[i], pos0[i], static_cast<int32_t>(c.x_pages), row});
       c.second.push_back(i);
       c.x_pages += pages;
@@ -704,7 +705,7 @@ LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const
   }
   c.status = SPEC_OK;
   if (c.rows == 0) return c;
-  if (c.R) c.plan = plan_latent(segs, n_heads, kOpMaxParts, dtype == SPEC_F32);
+  if (c.R) c.plan = plan_latent(segs, n_heads, dtype == SPEC_F32);
   c.x = plan_latent_prompt(x_segs, n_heads);
   if (c.R && c.R < c.rows)
     for (const LatentSegment& s : segs)
@@ -712,7 +713,7 @@ LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const
   const size_t elem = dtype == SPEC_F32 ? 4 : 2, lat = align_up(elem * c.R * n_heads * rank);
   c.o_q = align_up(sizeof(int32_t) * (c.pages + c.x_pages)) + align_up(sizeof(LatentItem) * c.plan.items.size()) +
           align_up(sizeof(LatentGroup) * c.plan.groups.size()) + align_up(sizeof(LatentItem) * c.x.items.size()) +
-          align_up(sizeof(int32_t) * c.row_list.size());
+          align_up(sizeof(LatentGroup) * c.x.groups.size()) + align_up(sizeof(int32_t) * c.row_list.size());
   c.o_o = c.o_q + lat;
   c.o_part = c.o_o + lat;
   c.o_ml = c.o_part + align_up(sizeof(float) * static_cast<size_t>(c.plan.n_parts) * c.plan.tile * rank);
@@ -720,7 +721,10 @@ LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const
   c.o_v = c.o_k + align_up(size_t{32} * c.x_pages * n_heads * nope_dim);
   c.o_key = c.o_v + align_up(size_t{32} * c.x_pages * n_heads * v_dim);
   // (the prompt kernel loads four pages at a time: up to three past the last)
-  c.bytes = c.o_key + align_up(size_t{32} * c.x_pages * rope_dim) + (c.x_pages ? size_t{96} * n_heads * std::max(nope_dim, v_dim) : 0);
+  c.o_xpart = c.o_key + align_up(size_t{32} * c.x_pages * rope_dim) + (c.x_pages ? align_up(size_t{96} * n_heads * std::max(nope_dim, v_dim)) : 0);
+  const size_t x_rows = static_cast<size_t>(c.x.n_parts) * c.x.rows * n_heads;
+  c.o_xml = c.o_xpart + align_up(sizeof(float) * x_rows * v_dim);
+  c.bytes = c.o_xml + align_up(sizeof(float) * x_rows * 2);
   return c;
 }
 
@@ -771,7 +775,7 @@ spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_
     }
   MetaBlock mb;
   const size_t opt = mb.add(table), oit = mb.add(c.plan.items), ogr = mb.add(c.plan.groups), oxi = mb.add(c.x.items),
-               orl = mb.add(c.row_list);
+               oxg = mb.add(c.x.groups), orl = mb.add(c.row_list);
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const spec_status up = upload_tables(ws, mb, "spec_op_attention_latent: larger tables than a captured call takes", st);
@@ -800,10 +804,13 @@ spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_
   a.part_ml = reinterpret_cast<float*>(ws + c.o_ml);
   hipError_t e = hipSuccess;
   if (!c.x.items.empty()) {
-    const LatentExpanded x{ws + c.o_k, ws + c.o_v, ws + c.o_key};
+    const LatentExpanded x{ws + c.o_k, ws + c.o_v, ws + c.o_key, reinterpret_cast<float*>(ws + c.o_xpart),
+                           reinterpret_cast<float*>(ws + c.o_xml)};
     e = launch_latent_expand(a, a.page_list + c.pages, static_cast<int>(c.x_pages), x, st);
     if (e == hipSuccess)
       e = launch_latent_prompt(a, reinterpret_cast<const LatentItem*>(ws + oxi), static_cast<int>(c.x.items.size()), c.x.rows, x, st);
+    if (e == hipSuccess)
+      e = launch_latent_prompt_combine(a, reinterpret_cast<const LatentGroup*>(ws + oxg), static_cast<int>(c.x.groups.size()), c.x.rows, x, st);
   }
   if (c.R) {
     int max_parts = 0;
