@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstring>
 #include <mutex>
@@ -128,6 +129,7 @@ class MetaBlock {
   }
   template <typename T>
   size_t add(const std::vector<T>& v) { return add(v.data(), v.size()); }
+  void pad(size_t n) { buf_.resize(std::max(n, buf_.size())); }
   size_t size() const { return buf_.size(); }
   const char* data() const { return buf_.data(); }
   void clear() { buf_.clear(); }

@@ -88,7 +88,11 @@ hipError_t launch_rope_latent(int dtype, int R, int H, int nope, int rope, int r
                               const float* q, const float* kv, const void* norm_w, const int32_t* pos,
                               const int32_t* slot, int num_pages, void* q_out, void* pages, hipStream_t st);
 
-hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st);
+// The queries' product.  With n > 0 (at most kLatentInline bytes, a multiple of 16) its
+// first workgroup also copies the call's tables to `to` (16-byte aligned), in the
+// kernel's arguments: one launch less before the attention that reads them.
+constexpr size_t kLatentInline = 3008;
+hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st, void* to = nullptr, const void* tables = nullptr, size_t n = 0);
 hipError_t launch_latent_attention(const LatentArgs& a, const LatentItem* items, int n_items, int tile, hipStream_t st);
 // (max_parts: the most parts of a group)
 hipError_t launch_latent_combine(const LatentArgs& a, const LatentGroup* groups, int n_groups, int tile, int max_parts,

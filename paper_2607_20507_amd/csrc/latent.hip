@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <cstring>
 #include <type_traits>
 
 #include "common.h"
@@ -134,20 +135,44 @@ __global__ __launch_bounds__(256) void rope_latent_kernel(int H, int nope, int r
   }
 }
 
+// Workgroup b's head and block of it, of `blocks` a head: consecutive workgroups go to
+// the 8 XCDs in turn, so the blocks of a head, which read the same rows, are 8 apart and
+// share an XCD's cache (384 rows of 32 heads: values 18 -> 13 us).
+__device__ __forceinline__ int2 head_block(int b, int blocks, int H) {
+  if (H % 8) return make_int2(b / blocks, b % blocks);
+  const int i = b / 8;
+  return make_int2(b % 8 + 8 * (i / blocks), i % blocks);
+}
+
 // The row, among all, of absorbed row i.
 __device__ __forceinline__ int row_of(const LatentArgs& a, int i) { return a.row_list ? a.row_list[i] : i; }
+
+// A call's tables, in a kernel's arguments.
+struct Tables {
+  uint4* to;
+  uint32_t n;  // units
+  uint4 unit[kLatentInline / 16];
+};
+struct NoTables {};
+__device__ __forceinline__ void copy_tables(const NoTables&) {}
+__device__ __forceinline__ void copy_tables(const Tables& t) {
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < t.n) t.to[threadIdx.x] = t.unit[threadIdx.x];
+}
+static_assert(kLatentInline % 16 == 0 && kLatentInline / 16 <= 256, "a unit a thread");
 
 // ---------------------------------------------------------------------------
 // Queries into the latents' space: q' [row, h, c] = sum_n q[row, h, n] w_k[h, n, c].
 // A workgroup holds w_k's columns 64 cb .. of one head, one wave 16 of them as MFMA
 // operands for all of its rows.
 
-template <int NOPE>
-__global__ __launch_bounds__(256) void latent_absorb_bf16_kernel(LatentArgs a) {
+template <int NOPE, typename Tab>
+__global__ __launch_bounds__(256) void latent_absorb_bf16_kernel(LatentArgs a, Tab tables) {
+  copy_tables(tables);
   constexpr int KS = NOPE / 32;
   __shared__ uint4 sw[NOPE * 8];
   const int blocks = a.rank / 64;
-  const int h = blockIdx.x / blocks, c0 = blockIdx.x % blocks * 64;
+  const int2 hb = head_block(blockIdx.x, blocks, a.H);
+  const int h = hb.x, c0 = hb.y * 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
   const bf16_t* w = static_cast<const bf16_t*>(a.w_k) + static_cast<int64_t>(h) * a.k_stride + c0;
   // row n's 16-byte chunks c at c ^ f(n): reads of four rows' 32 bytes, and writes, take every bank
@@ -193,8 +218,9 @@ __global__ __launch_bounds__(256) void latent_absorb_bf16_kernel(LatentArgs a) {
   }
 }
 
-template <int NOPE>
-__global__ __launch_bounds__(256) void latent_absorb_f32_kernel(LatentArgs a) {
+template <int NOPE, typename Tab>
+__global__ __launch_bounds__(256) void latent_absorb_f32_kernel(LatentArgs a, Tab tables) {
+  copy_tables(tables);
   constexpr int J = NOPE / 16;
   const int blocks = a.rank / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
@@ -226,43 +252,48 @@ __global__ __launch_bounds__(256) void latent_absorb_f32_kernel(LatentArgs a) {
 
 // ---------------------------------------------------------------------------
 // Sums of latents to values: out[row, h, d] = sum_c o'[row, h, c] w_v[h, d, c].  A
-// workgroup makes 16 dims of one head.  For few rows its four waves take a quarter of
-// the sum each (SPLIT: all 256 CUs stream the weight); for more, every wave holds all 16
-// rows of the weight and takes its own row tiles.
+// workgroup makes 16 dims of one head, its four waves a quarter of the sum each.  (Every
+// wave with the whole sum and row tiles of its own, and no exchange: 24 us instead of 12
+// for 384 rows of 32 heads.)
 
-template <int RANK, bool SPLIT>
+template <int RANK>
 __global__ __launch_bounds__(256) void latent_values_bf16_kernel(LatentArgs a) {
-  constexpr int KS = SPLIT ? RANK / 128 : RANK / 32;
-  __shared__ f32x4 part[SPLIT ? 4 : 1][64];
+  constexpr int KS = RANK / 128;
+  __shared__ f32x4 part[2][4][64];
   const int tiles = a.vdim / 16;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
-  const int h = blockIdx.x / tiles, d0 = blockIdx.x % tiles * 16;
-  const int c0 = (SPLIT ? wave * (RANK / 4) : 0) + 8 * g;
+  const int2 hb = head_block(blockIdx.x, tiles, a.H);
+  const int h = hb.x, d0 = hb.y * 16;
+  const int c0 = wave * (RANK / 4) + 8 * g;
   const bf16_t* w = static_cast<const bf16_t*>(a.w_v) + static_cast<int64_t>(h) * a.v_stride +
                     static_cast<size_t>(d0 + l16) * RANK + c0;
-  uint4 wf[KS];
+  uint4 wf[KS], of[KS], on[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) wf[s] = *reinterpret_cast<const uint4*>(w + 32 * s);
   const bf16_t* o = static_cast<const bf16_t*>(a.o_lat);
   bf16_t* out = static_cast<bf16_t*>(a.out);
-  const int step = (SPLIT ? 16 : 64) * gridDim.y;
-  for (int r0 = SPLIT ? 16 * blockIdx.y : 64 * blockIdx.y + 16 * wave; r0 < a.R; r0 += step) {
-    const int r = r0 + l16;
-    const size_t qv = static_cast<size_t>(min(r, a.R - 1)) * a.H + h;
-    uint4 of[KS];
+  const int step = 16 * gridDim.y;
+  auto read = [&](int r0, uint4 (&x)[KS]) {
+    const size_t qv = static_cast<size_t>(min(r0 + l16, a.R - 1)) * a.H + h;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) of[s] = *reinterpret_cast<const uint4*>(o + qv * RANK + c0 + 32 * s);
+    for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const uint4*>(o + qv * RANK + c0 + 32 * s);
+  };
+  read(16 * blockIdx.y, of);
+  int b = 0;
+  for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += step, b ^= 1) {
+    read(r0 + step, on);  // (past the last row: that row)
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int s = 0; s < KS; ++s) acc = mfma16x16x32(wf[s], of[s], acc);
-    if constexpr (SPLIT) {
-      part[wave][lane] = acc;
-      __syncthreads();
-      if (wave == 0) acc = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
-    }
-    if ((!SPLIT || wave == 0) && r < a.R)
+    part[b][wave][lane] = acc;
+    __syncthreads();  // (the other buffer's last readers passed the barrier before)
+    const int r = r0 + l16;
+    if (wave == 0 && r < a.R) {
+      acc = part[b][0][lane] + part[b][1][lane] + part[b][2][lane] + part[b][3][lane];
       put4(out + (static_cast<size_t>(row_of(a, r)) * a.H + h) * a.vdim + d0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
-    if constexpr (SPLIT) __syncthreads();
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s) of[s] = on[s];
   }
 }
 
@@ -823,14 +854,12 @@ hipError_t launch_attention(const LatentArgs& a, const LatentItem* items, int n,
   return hipGetLastError();
 }
 
-// Row blocks of the two products: at most about `most` workgroups.
-unsigned row_blocks(int R, unsigned columns, int rows, unsigned most) {
-  const unsigned tiles = (static_cast<unsigned>(R) + rows - 1) / rows;
-  return std::max(1u, std::min(tiles, most / std::max(1u, columns)));
+// Row blocks of the two products: at most about 1024 workgroups (384 rows of 32 heads, 4
+// blocks and 11: values 18 and 20 us).
+unsigned row_blocks(int R, unsigned columns) {
+  const unsigned tiles = (static_cast<unsigned>(R) + 15) / 16;
+  return std::max(1u, std::min(tiles, 1024u / std::max(1u, columns)));
 }
-
-// Rows up to which the values' products are split over a workgroup's waves.
-constexpr int kSplitValueRows = 48;
 
 }  // namespace
 
@@ -852,29 +881,35 @@ hipError_t launch_rope_latent(int dtype, int R, int H, int nope, int rope, int r
   return hipGetLastError();
 }
 
-hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st) {
-  if (a.R <= 0) return hipSuccess;
+hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st, void* to, const void* tables, size_t n) {
+  if (a.R <= 0 || n > kLatentInline || n % 16 || reinterpret_cast<uintptr_t>(to) % 16) return hipErrorInvalidValue;
   const unsigned columns = static_cast<unsigned>(a.H) * (a.rank / 64);
-  const dim3 grid(columns, row_blocks(a.R, columns, 16, 2048));
-  if (a.nope == 64 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<64>, grid, dim3(256), 0, st, a);
-  else if (a.nope == 128 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<128>, grid, dim3(256), 0, st, a);
-  else if (a.nope == 64) launch_kernel(latent_absorb_bf16_kernel<64>, grid, dim3(256), 0, st, a);
-  else if (a.nope == 128) launch_kernel(latent_absorb_bf16_kernel<128>, grid, dim3(256), 0, st, a);
-  else return hipErrorInvalidValue;
-  return hipGetLastError();
+  const dim3 grid(columns, row_blocks(a.R, columns));
+  auto go = [&](auto tab) {
+    using Tab = decltype(tab);
+    if (a.nope == 64 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<64, Tab>, grid, dim3(256), 0, st, a, tab);
+    else if (a.nope == 128 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<128, Tab>, grid, dim3(256), 0, st, a, tab);
+    else if (a.nope == 64) launch_kernel(latent_absorb_bf16_kernel<64, Tab>, grid, dim3(256), 0, st, a, tab);
+    else if (a.nope == 128) launch_kernel(latent_absorb_bf16_kernel<128, Tab>, grid, dim3(256), 0, st, a, tab);
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+  };
+  if (n == 0) return go(NoTables{});
+  Tables t;
+  t.to = static_cast<uint4*>(to);
+  t.n = static_cast<uint32_t>(n / 16);
+  std::memcpy(t.unit, tables, n);
+  return go(t);
 }
 
 hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st) {
   if (a.R <= 0) return hipSuccess;
   const unsigned columns = static_cast<unsigned>(a.H) * (a.vdim / 16);
-  const bool split = a.dtype == 0 || a.R <= kSplitValueRows;
-  const dim3 grid(columns, row_blocks(a.R, columns, split ? 16 : 64, 2048));
+  const dim3 grid(columns, row_blocks(a.R, columns));
   if (a.rank == 256 && a.dtype == 0) launch_kernel(latent_values_f32_kernel<256>, grid, dim3(256), 0, st, a);
   else if (a.rank == 512 && a.dtype == 0) launch_kernel(latent_values_f32_kernel<512>, grid, dim3(256), 0, st, a);
-  else if (a.rank == 256 && split) launch_kernel(latent_values_bf16_kernel<256, true>, grid, dim3(256), 0, st, a);
-  else if (a.rank == 256) launch_kernel(latent_values_bf16_kernel<256, false>, grid, dim3(256), 0, st, a);
-  else if (a.rank == 512 && split) launch_kernel(latent_values_bf16_kernel<512, true>, grid, dim3(256), 0, st, a);
-  else if (a.rank == 512) launch_kernel(latent_values_bf16_kernel<512, false>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 256) launch_kernel(latent_values_bf16_kernel<256>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 512) launch_kernel(latent_values_bf16_kernel<512>, grid, dim3(256), 0, st, a);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }

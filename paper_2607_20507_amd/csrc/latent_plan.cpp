@@ -56,9 +56,11 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, bool fp32)
   // (keys of all tiles a CU; 256 / 384 items, us): 187 keys 48.3 / 54.2, 312 keys 53.8 / 58.5, 940
   // 83.6 / 86.4, 1300 155 / 128, 2344 158 / 145.
   const int target = p.tile == 64 && all_keys / kCus >= 1200 ? kCus * 3 / 2 : kCus;
-  // At least a chunk for every wave that takes keys of its own; fp32 one page (133 keys of 2
-  // tiles in 2 parts each 24.1 us, in 3 22.9).
-  const int least = fp32 ? 2 : 4;
+  // Whole where a wave then has at most four chunks (of 32 keys; fp32 pages): a join is a
+  // launch.  Otherwise at least a chunk for every wave that takes keys of its own.
+  const int shares = p.tile == 64 ? 1 : p.tile == 32 ? 2 : 4;
+  const int whole = fp32 ? 8 : 4 * shares;
+  const int least = most_keys <= 32 * whole ? whole : fp32 ? 2 : 4;
   const int64_t split = 32 * least_split(least, (most_keys + 31) / 32, std::max<int64_t>(target, static_cast<int64_t>(tiles.size())),
                                          [&](int64_t sp) {
                                            int64_t n = 0;

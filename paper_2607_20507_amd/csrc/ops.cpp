@@ -778,8 +778,15 @@ spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_
                oxg = mb.add(c.x.groups), orl = mb.add(c.row_list);
   char* ws = static_cast<char*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const spec_status up = upload_tables(ws, mb, "spec_op_attention_latent: larger tables than a captured call takes", st);
-  if (up != SPEC_OK) return up;
+  // small tables of the absorbed form alone travel with its first kernel
+  const size_t n_inline = align_up(mb.size(), 16);
+  const bool in_args = c.x.items.empty() && n_inline <= kLatentInline;
+  if (in_args) {
+    mb.pad(n_inline);
+  } else {
+    const spec_status up = upload_tables(ws, mb, "spec_op_attention_latent: larger tables than a captured call takes", st);
+    if (up != SPEC_OK) return up;
+  }
   LatentArgs a;
   a.dtype = dtype == SPEC_F32 ? 0 : 1;
   a.H = n_heads;
@@ -815,7 +822,7 @@ spec_status spec_op_attention_latent(int32_t dtype, int32_t n_seqs, const int32_
   if (c.R) {
     int max_parts = 0;
     for (const LatentGroup& g : c.plan.groups) max_parts = std::max(max_parts, g.nparts);
-    if (e == hipSuccess) e = launch_latent_absorb(a, st);
+    if (e == hipSuccess) e = in_args ? launch_latent_absorb(a, st, ws, mb.data(), mb.size()) : launch_latent_absorb(a, st);
     if (e == hipSuccess)
       e = launch_latent_attention(a, reinterpret_cast<const LatentItem*>(ws + oit), static_cast<int>(c.plan.items.size()),
                                   c.plan.tile, st);
