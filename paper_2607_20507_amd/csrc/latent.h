@@ -46,7 +46,9 @@ struct LatentPlan {
 
 // Tiles and key splits of the absorbed form (at most kLatentMaxParts parts in all).
 constexpr int kLatentMaxParts = 512;
-LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, bool fp32);
+// fp32_waves: 0 for bf16, else the waves that share an fp32 item's pages.
+LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int fp32_waves);
+constexpr int latent_f32_waves(int rank) { return rank == 256 ? 8 : 4; }
 
 // Items of the expanded form (below): blocks of `rows` (256 or 128) rows, those with
 // most keys first.
@@ -91,7 +93,7 @@ hipError_t launch_rope_latent(int dtype, int R, int H, int nope, int rope, int r
 // The queries' product.  With n > 0 (at most kLatentInline bytes, a multiple of 16) its
 // first workgroup also copies the call's tables to `to` (16-byte aligned), in the
 // kernel's arguments: one launch less before the attention that reads them.
-constexpr size_t kLatentInline = 3008;
+constexpr size_t kLatentInline = 3584;
 hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st, void* to = nullptr, const void* tables = nullptr, size_t n = 0);
 hipError_t launch_latent_attention(const LatentArgs& a, const LatentItem* items, int n_items, int tile, hipStream_t st);
 // (max_parts: the most parts of a group)

@@ -344,11 +344,11 @@ __device__ __forceinline__ float join_weight(float m, float top, float scale) {
 }
 
 // The waves' states, in LDS as [WK][Q][RANK + 4] and [WK][Q][2], to the item's output.
-template <typename T, int RANK, int WK, int Q>
+template <typename T, int RANK, int WK, int Q, int THREADS>
 __device__ __forceinline__ void join_waves(const LatentArgs& a, const LatentItem& it, const float* so, const float* sml,
                                            int tile) {
   constexpr int U = RANK / 4;
-  for (int u = threadIdx.x; u < Q * U; u += 256) {
+  for (int u = threadIdx.x; u < Q * U; u += THREADS) {
     const int m = u / U, c = u % U * 4;
     if (m >= it.nqv) break;
     float top = sml[2 * m];
@@ -713,21 +713,22 @@ __global__ __launch_bounds__(256, WK == 1 ? 2 : 1) void attn_latent_bf16_kernel(
       s_ml[2 * at + 1] = l;
     }
     __syncthreads();
-    join_waves<bf16_t, RANK, WK, Q>(a, it, so, s_ml, Q);
+    join_waves<bf16_t, RANK, WK, Q, 256>(a, it, so, s_ml, Q);
   }
 }
 
 // ---------------------------------------------------------------------------
-// Absorbed attention, fp32: 16 query vectors a workgroup, whose four waves take its
-// pages in turn.  fp32 MFMA throughout (16 x 16 x 4), operands straight from the
+// Absorbed attention, fp32: 16 query vectors a workgroup, whose waves take its pages in
+// turn.  A page is (rank 256) 136 MFMAs of 32 cycles in one wave, the bound of a short
+// context: eight waves there, four where registers allow no more.  fp32 MFMA throughout (16 x 16 x 4), operands straight from the
 // cache: k-step (j, i) of the scores takes dim 16 j + 4 g + i in lane group g, and
 // output tile (j, t) holds dims 64 j + 4 row + t, so that every load is 16 bytes a
 // lane and a lane's scores are the probabilities it supplies.
 
 template <int RANK, int ROPE>
-__global__ __launch_bounds__(256, 1) void attn_latent_f32_kernel(LatentArgs a, const LatentItem* __restrict__ items) {
+__global__ __launch_bounds__(64 * latent_f32_waves(RANK), 1) void attn_latent_f32_kernel(LatentArgs a, const LatentItem* __restrict__ items) {
   constexpr int D = RANK + ROPE, J = D / 16, JV = RANK / 64;
-  constexpr int WK = 4, Q = 16;
+  constexpr int WK = latent_f32_waves(RANK), Q = 16;
   __shared__ float so[WK * Q * (RANK + 4)];
   __shared__ float s_ml[2 * WK * Q];
   const LatentItem it = items[blockIdx.x];
@@ -834,14 +835,14 @@ __global__ __launch_bounds__(256, 1) void attn_latent_f32_kernel(LatentArgs a, c
     s_ml[2 * at + 1] = lrun;
   }
   __syncthreads();
-  join_waves<float, RANK, WK, Q>(a, it, so, s_ml, Q);
+  join_waves<float, RANK, WK, Q, 64 * WK>(a, it, so, s_ml, Q);
 }
 
 template <int RANK, int ROPE>
 hipError_t launch_attention(const LatentArgs& a, const LatentItem* items, int n, int tile, hipStream_t st) {
   if (a.dtype == 0) {
     if (tile != 16) return hipErrorInvalidValue;
-    launch_kernel(attn_latent_f32_kernel<RANK, ROPE>, dim3(n), dim3(256), 0, st, a, items);
+    launch_kernel(attn_latent_f32_kernel<RANK, ROPE>, dim3(n), dim3(64 * latent_f32_waves(RANK)), 0, st, a, items);
   } else if (tile == 16) {
     launch_kernel(attn_latent_bf16_kernel<RANK, ROPE, 1, 4>, dim3(n), dim3(256), 0, st, a, items);
   } else if (tile == 32) {

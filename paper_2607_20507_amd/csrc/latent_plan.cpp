@@ -25,7 +25,8 @@ constexpr int kCus = 256;
 
 }  // namespace
 
-LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, bool fp32) {
+LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int fp32_waves) {
+  const bool fp32 = fp32_waves > 0;
   LatentPlan p;
   int64_t most = 1;
   for (const LatentSegment& s : segs) most = std::max<int64_t>(most, static_cast<int64_t>(s.nrows) * H);
@@ -56,11 +57,12 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, bool fp32)
   // (keys of all tiles a CU; 256 / 384 items, us): 187 keys 48.3 / 54.2, 312 keys 53.8 / 58.5, 940
   // 83.6 / 86.4, 1300 155 / 128, 2344 158 / 145.
   const int target = p.tile == 64 && all_keys / kCus >= 1200 ? kCus * 3 / 2 : kCus;
-  // Whole where a wave then has at most four chunks (of 32 keys; fp32 pages): a join is a
-  // launch.  Otherwise at least a chunk for every wave that takes keys of its own.
+  // Whole where a wave then has at most four chunks of 32 keys, or two fp32 pages (a join is
+  // a launch): 8 sequences of 256 to 512 keys, 16 heads of rank 256, 24.8 us in parts, 17.3
+  // whole.  Otherwise at least a chunk, or page, for every wave that takes keys of its own.
   const int shares = p.tile == 64 ? 1 : p.tile == 32 ? 2 : 4;
-  const int whole = fp32 ? 8 : 4 * shares;
-  const int least = most_keys <= 32 * whole ? whole : fp32 ? 2 : 4;
+  const int whole = fp32 ? fp32_waves : 4 * shares;
+  const int least = most_keys <= 32 * whole ? whole : fp32 ? fp32_waves / 2 : 4;
   const int64_t split = 32 * least_split(least, (most_keys + 31) / 32, std::max<int64_t>(target, static_cast<int64_t>(tiles.size())),
                                          [&](int64_t sp) {
                                            int64_t n = 0;

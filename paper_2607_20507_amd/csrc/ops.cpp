@@ -705,7 +705,7 @@ LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const
   }
   c.status = SPEC_OK;
   if (c.rows == 0) return c;
-  if (c.R) c.plan = plan_latent(segs, n_heads, dtype == SPEC_F32);
+  if (c.R) c.plan = plan_latent(segs, n_heads, dtype == SPEC_F32 ? latent_f32_waves(rank) : 0);
   c.x = plan_latent_prompt(x_segs, n_heads);
   if (c.R && c.R < c.rows)
     for (const LatentSegment& s : segs)
