@@ -95,6 +95,54 @@ def test_one_key_far_above_the_others(dtype, rows, H):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("power", [7, 14, 22])
+@pytest.mark.parametrize("rows, pos0", [(3, 500), (3, 5000), (200, 3), (40, 3000)])
+def test_large_logits_keep_small_differences(dtype, power, rows, pos0):
+    """Logits of 2^power + 0 .. 3, whose products and sums 24 bits hold exactly: e^0 .. e^-3 once the maximum is taken away."""
+    device()
+    say("large", dtype, power, rows, pos0)
+    c = L.Case(dtype, [rows], [pos0], 4, seed=19, **SMALL)
+    flat = c.pages.view(-1, 288)
+    n = rows + pos0
+    g = torch.Generator(device="cuda")
+    g.manual_seed(20)
+    level = torch.randint(0, 4, (n,), generator=g, device="cuda")
+    flat[c.slots(0), 256:] = 0
+    flat[c.slots(0), 256] = 1
+    flat[c.slots(0), 257] = level.to(dtype)
+    c.q.zero_()
+    c.q[:, :, 64] = 2.0 ** power
+    c.q[:, :, 65] = 1
+    c.scale = 1.0
+    got, ref = c.run(B), c.ref()
+    assert torch.isfinite(got).all() and L.row_error(got, ref) <= L.TOL[dtype]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows, pos0", [(3, 500), (200, 3)])
+def test_a_scale_that_makes_logits_huge(dtype, rows, pos0):
+    """Logits to 2^30 and beyond: a row is its best key's value, at differences of thousands and more."""
+    device()
+    say("huge", dtype, rows, pos0)
+    c = L.Case(dtype, [rows], [pos0], 4, seed=21, **SMALL)
+    c.scale = 1e9
+    got, ref = c.run(B), c.ref()
+    assert torch.isfinite(got).all()
+    flat, r = c.pages.view(-1, 288), torch.arange(rows, device="cuda")
+    held = flat[c.slots(0)].double()
+    for h in range(4):
+        k = torch.cat([held[:, :256] @ c.w_k[h].double().t().contiguous(), held[:, 256:]], 1)
+        s = c.q[:, h].double() @ k.t().contiguous()
+        s.masked_fill_(torch.arange(len(held), device="cuda") > pos0 + r[:, None], -math.inf)
+        # one rounding to bf16 of queries or keys moves a score by 0.0017 sqrt(64) in the root mean square, two scores' difference
+        # by 0.02: 0.3 is 15 times that
+        top = s.topk(min(2, s.shape[1]), 1)[0]
+        lead = top[:, 0] - top[:, -1] > 0.3
+        assert int(lead.sum()) >= min(rows, 50) // 3
+        assert L.row_error(got[lead, h], ref[lead, h]) <= L.TOL[dtype]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("H", [4, 16, 32])
 @pytest.mark.parametrize("where, value", [("latent", math.nan), ("latent", -math.inf), ("key", math.nan), ("key", math.inf)])
 @pytest.mark.parametrize("rows, bad", [(6, 3), (300, 3), (300, 150), (300, 290)])
