@@ -137,7 +137,7 @@ __global__ __launch_bounds__(256) void rope_latent_kernel(int H, int nope, int r
 
 // Workgroup b's head and block of it, of `blocks` a head: consecutive workgroups go to
 // the 8 XCDs in turn, so the blocks of a head, which read the same rows, are 8 apart and
-// share an XCD's cache (384 rows of 32 heads: values 18 -> 13 us).
+// share an XCD's cache (384 rows of 32 heads, CT = 1: values 18 -> 13 us).
 __device__ __forceinline__ int2 head_block(int b, int blocks, int H) {
   if (H % 8) return make_int2(b / blocks, b % blocks);
   const int i = b / 8;
@@ -162,10 +162,11 @@ static_assert(kLatentInline % 16 == 0 && kLatentInline / 16 <= 256, "a unit a th
 
 // ---------------------------------------------------------------------------
 // Queries into the latents' space: q' [row, h, c] = sum_n q[row, h, n] w_k[h, n, c].
-// A workgroup holds w_k's columns 64 cb .. of one head, one wave 16 of them as MFMA
-// operands for all of its rows.
+// A workgroup holds w_k's columns 64 cb .. of one head, a wave 16 CT of them as MFMA
+// operands for its share of the rows: every fourth tile of 16 (CT = 4) or all (CT = 1,
+// where there are too few tiles to share).
 
-template <int NOPE, typename Tab>
+template <int NOPE, int CT, typename Tab>
 __global__ __launch_bounds__(256) void latent_absorb_bf16_kernel(LatentArgs a, Tab tables) {
   copy_tables(tables);
   constexpr int KS = NOPE / 32;
@@ -175,6 +176,16 @@ __global__ __launch_bounds__(256) void latent_absorb_bf16_kernel(LatentArgs a, T
   const int h = hb.x, c0 = hb.y * 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
   const bf16_t* w = static_cast<const bf16_t*>(a.w_k) + static_cast<int64_t>(h) * a.k_stride + c0;
+  const bf16_t* q = static_cast<const bf16_t*>(a.q);
+  bf16_t* to = static_cast<bf16_t*>(a.q_lat);
+  const int hq = NOPE + a.rope, step = 16 * CT * gridDim.y;
+  uint4 qf[KS], qn[KS];
+  auto read = [&](int r0, uint4 (&x)[KS]) {
+    const size_t from = (static_cast<size_t>(row_of(a, min(r0 + l16, a.R - 1))) * a.H + h) * hq;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const uint4*>(q + from + 32 * s + 8 * g);
+  };
+  const int first = 16 * (CT * blockIdx.y + (CT == 4 ? wave : 0)), t0 = CT == 4 ? 0 : wave;  // rows, column tiles
   // row n's 16-byte chunks c at c ^ f(n): reads of four rows' 32 bytes, and writes, take every bank
   auto f = [](int n) { return (n & 3) << 1 | (n >> 2 & 1); };
 #pragma unroll
@@ -182,37 +193,34 @@ __global__ __launch_bounds__(256) void latent_absorb_bf16_kernel(LatentArgs a, T
     const int u = i * 256 + threadIdx.x, n = u >> 3, c = u & 7;
     sw[n * 8 + (c ^ f(n))] = *reinterpret_cast<const uint4*>(w + static_cast<size_t>(n) * a.rank + 8 * c);
   }
+  read(first, qf);
   __syncthreads();
-  uint4 wf[KS];
+  uint4 wf[CT][KS];
   const uint32_t base = lds_addr(sw);
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    uint2 p[2];
+  for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int n = 32 * s + 8 * g + 4 * t + (l16 >> 2), c = 2 * wave + (l16 >> 1 & 1);
-      p[t] = read_tr(base + (n * 8 + (c ^ f(n))) * 16 + (l16 & 1) * 8);
+    for (int s = 0; s < KS; ++s) {
+      uint2 p[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int n = 32 * s + 8 * g + 4 * t + (l16 >> 2), c = 2 * (t0 + ct) + (l16 >> 1 & 1);
+        p[t] = read_tr(base + (n * 8 + (c ^ f(n))) * 16 + (l16 & 1) * 8);
+      }
+      wf[ct][s] = make_uint4(p[0].x, p[0].y, p[1].x, p[1].y);
     }
-    wf[s] = make_uint4(p[0].x, p[0].y, p[1].x, p[1].y);
-  }
-  const bf16_t* q = static_cast<const bf16_t*>(a.q);
-  bf16_t* to = static_cast<bf16_t*>(a.q_lat);
-  const int hq = NOPE + a.rope, step = 16 * gridDim.y;
-  uint4 qf[KS], qn[KS];
-  auto read = [&](int r0, uint4 (&x)[KS]) {
-    const size_t from = (static_cast<size_t>(row_of(a, min(r0 + l16, a.R - 1))) * a.H + h) * hq;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const uint4*>(q + from + 32 * s + 8 * g);
-  };
-  read(16 * blockIdx.y, qf);
-  for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += step) {
+  for (int r0 = first; r0 < a.R; r0 += step) {
     read(r0 + step, qn);  // (past the last row: that row)
     const int r = r0 + l16;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < KS; ++s) acc = mfma16x16x32(wf[s], qf[s], acc);
-    if (r < a.R)
-      put4(to + (static_cast<size_t>(r) * a.H + h) * a.rank + c0 + 16 * wave + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+    for (int ct = 0; ct < CT; ++ct) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) acc = mfma16x16x32(wf[ct][s], qf[s], acc);
+      // (bf16: what the scores' products take)
+      if (r < a.R)
+        put4(to + (static_cast<size_t>(r) * a.H + h) * a.rank + c0 + 16 * (t0 + ct) + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+    }
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = qn[s];
   }
@@ -252,24 +260,20 @@ __global__ __launch_bounds__(256) void latent_absorb_f32_kernel(LatentArgs a, Ta
 
 // ---------------------------------------------------------------------------
 // Sums of latents to values: out[row, h, d] = sum_c o'[row, h, c] w_v[h, d, c].  A
-// workgroup makes 16 dims of one head, its four waves a quarter of the sum each.  (Every
-// wave with the whole sum and row tiles of its own, and no exchange: 24 us instead of 12
-// for 384 rows of 32 heads.)
+// workgroup makes 16 CT dims of one head, its four waves a quarter of the sum each.
 
-template <int RANK>
+template <int RANK, int CT>
 __global__ __launch_bounds__(256) void latent_values_bf16_kernel(LatentArgs a) {
   constexpr int KS = RANK / 128;
-  __shared__ f32x4 part[2][4][64];
-  const int tiles = a.vdim / 16;
+  __shared__ f32x4 part[2][4][CT][64];
+  const int tiles = a.vdim / (16 * CT);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
   const int2 hb = head_block(blockIdx.x, tiles, a.H);
-  const int h = hb.x, d0 = hb.y * 16;
+  const int h = hb.x, d0 = hb.y * (16 * CT);
   const int c0 = wave * (RANK / 4) + 8 * g;
   const bf16_t* w = static_cast<const bf16_t*>(a.w_v) + static_cast<int64_t>(h) * a.v_stride +
                     static_cast<size_t>(d0 + l16) * RANK + c0;
-  uint4 wf[KS], of[KS], on[KS];
-#pragma unroll
-  for (int s = 0; s < KS; ++s) wf[s] = *reinterpret_cast<const uint4*>(w + 32 * s);
+  uint4 wf[CT][KS], of[KS], on[KS];
   const bf16_t* o = static_cast<const bf16_t*>(a.o_lat);
   bf16_t* out = static_cast<bf16_t*>(a.out);
   const int step = 16 * gridDim.y;
@@ -279,18 +283,25 @@ __global__ __launch_bounds__(256) void latent_values_bf16_kernel(LatentArgs a) {
     for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const uint4*>(o + qv * RANK + c0 + 32 * s);
   };
   read(16 * blockIdx.y, of);
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) wf[ct][s] = *reinterpret_cast<const uint4*>(w + 16 * ct * RANK + 32 * s);
   int b = 0;
   for (int r0 = 16 * blockIdx.y; r0 < a.R; r0 += step, b ^= 1) {
     read(r0 + step, on);  // (past the last row: that row)
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int s = 0; s < KS; ++s) acc = mfma16x16x32(wf[s], of[s], acc);
-    part[b][wave][lane] = acc;
+    for (int ct = 0; ct < CT; ++ct) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) acc = mfma16x16x32(wf[ct][s], of[s], acc);
+      part[b][wave][ct][lane] = acc;
+    }
     __syncthreads();  // (the other buffer's last readers passed the barrier before)
     const int r = r0 + l16;
-    if (wave == 0 && r < a.R) {
-      acc = part[b][0][lane] + part[b][1][lane] + part[b][2][lane] + part[b][3][lane];
-      put4(out + (static_cast<size_t>(row_of(a, r)) * a.H + h) * a.vdim + d0 + 4 * g, acc[0], acc[1], acc[2], acc[3]);
+    if (wave < CT && r < a.R) {
+      const f32x4 acc = part[b][0][wave][lane] + part[b][1][wave][lane] + part[b][2][wave][lane] + part[b][3][wave][lane];
+      put4(out + (static_cast<size_t>(row_of(a, r)) * a.H + h) * a.vdim + d0 + 16 * wave + 4 * g, acc[0], acc[1], acc[2], acc[3]);
     }
 #pragma unroll
     for (int s = 0; s < KS; ++s) of[s] = on[s];
@@ -855,11 +866,17 @@ hipError_t launch_attention(const LatentArgs& a, const LatentItem* items, int n,
   return hipGetLastError();
 }
 
-// Row blocks of the two products: at most about 1024 workgroups (384 rows of 32 heads, 4
-// blocks and 11: values 18 and 20 us).
-unsigned row_blocks(int R, unsigned columns) {
-  const unsigned tiles = (static_cast<unsigned>(R) + 15) / 16;
-  return std::max(1u, std::min(tiles, 1024u / std::max(1u, columns)));
+// Whether the two bf16 products take 64 columns a wave (CT = 4), which reads the rows a
+// quarter as often, rather than 16, which shares few rows out better.  32 heads of rank
+// 512, CT = 1 / 4, us: absorb of 32 rows 4.1 / 3.6, 64 rows 5.0 / 3.9, 384 rows 16 / 9.3; values
+// 3.9 / 4.1, 6.0 / 4.5, 16 / 9.2.
+bool wide_columns(const LatentArgs& a) { return a.dtype == 1 && a.R >= 48; }
+
+// Row blocks of the two products, of at most about `groups` workgroups.  Each brings
+// its weights again: 384 rows of 32 heads, values (CT = 4) in 256 / 512 / 1024 / 1536
+// workgroups 9.2 / 9.8 / 12.7 / 16.6 us, absorb in 256 / 512 / 1024 12 / 9.3 / 10.9.
+unsigned row_blocks(unsigned row_tiles, unsigned columns, unsigned groups) {
+  return std::max(1u, std::min(row_tiles, groups / std::max(1u, columns)));
 }
 
 }  // namespace
@@ -885,13 +902,17 @@ hipError_t launch_rope_latent(int dtype, int R, int H, int nope, int rope, int r
 hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st, void* to, const void* tables, size_t n) {
   if (a.R <= 0 || n > kLatentInline || n % 16 || reinterpret_cast<uintptr_t>(to) % 16) return hipErrorInvalidValue;
   const unsigned columns = static_cast<unsigned>(a.H) * (a.rank / 64);
-  const dim3 grid(columns, row_blocks(a.R, columns));
+  const bool wide = wide_columns(a);
+  const unsigned rows = wide ? 64 : 16;  // of a workgroup at a time
+  const dim3 grid(columns, row_blocks((a.R + rows - 1) / rows, columns, wide ? 512 : 1024));
   auto go = [&](auto tab) {
     using Tab = decltype(tab);
     if (a.nope == 64 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<64, Tab>, grid, dim3(256), 0, st, a, tab);
     else if (a.nope == 128 && a.dtype == 0) launch_kernel(latent_absorb_f32_kernel<128, Tab>, grid, dim3(256), 0, st, a, tab);
-    else if (a.nope == 64) launch_kernel(latent_absorb_bf16_kernel<64, Tab>, grid, dim3(256), 0, st, a, tab);
-    else if (a.nope == 128) launch_kernel(latent_absorb_bf16_kernel<128, Tab>, grid, dim3(256), 0, st, a, tab);
+    else if (a.nope == 64 && wide) launch_kernel(latent_absorb_bf16_kernel<64, 4, Tab>, grid, dim3(256), 0, st, a, tab);
+    else if (a.nope == 64) launch_kernel(latent_absorb_bf16_kernel<64, 1, Tab>, grid, dim3(256), 0, st, a, tab);
+    else if (a.nope == 128 && wide) launch_kernel(latent_absorb_bf16_kernel<128, 4, Tab>, grid, dim3(256), 0, st, a, tab);
+    else if (a.nope == 128) launch_kernel(latent_absorb_bf16_kernel<128, 1, Tab>, grid, dim3(256), 0, st, a, tab);
     else return hipErrorInvalidValue;
     return hipGetLastError();
   };
@@ -905,12 +926,15 @@ hipError_t launch_latent_absorb(const LatentArgs& a, hipStream_t st, void* to, c
 
 hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st) {
   if (a.R <= 0) return hipSuccess;
-  const unsigned columns = static_cast<unsigned>(a.H) * (a.vdim / 16);
-  const dim3 grid(columns, row_blocks(a.R, columns));
+  const bool wide = wide_columns(a);
+  const unsigned columns = static_cast<unsigned>(a.H) * (a.vdim / (wide ? 64 : 16));
+  const dim3 grid(columns, row_blocks((static_cast<unsigned>(a.R) + 15) / 16, columns, wide ? 256 : 1024));
   if (a.rank == 256 && a.dtype == 0) launch_kernel(latent_values_f32_kernel<256>, grid, dim3(256), 0, st, a);
   else if (a.rank == 512 && a.dtype == 0) launch_kernel(latent_values_f32_kernel<512>, grid, dim3(256), 0, st, a);
-  else if (a.rank == 256) launch_kernel(latent_values_bf16_kernel<256>, grid, dim3(256), 0, st, a);
-  else if (a.rank == 512) launch_kernel(latent_values_bf16_kernel<512>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 256 && wide) launch_kernel(latent_values_bf16_kernel<256, 4>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 256) launch_kernel(latent_values_bf16_kernel<256, 1>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 512 && wide) launch_kernel(latent_values_bf16_kernel<512, 4>, grid, dim3(256), 0, st, a);
+  else if (a.rank == 512) launch_kernel(latent_values_bf16_kernel<512, 1>, grid, dim3(256), 0, st, a);
   else return hipErrorInvalidValue;
   return hipGetLastError();
 }

@@ -50,6 +50,17 @@ def test_sizes(dtype, nope, rope, rank, v):
         check(L.Case(dtype, rows, pos0, H, nope, rope, rank, v, seed=5))
 
 
+# many sequences of few rows: products of 47 rows and more at a time, with last blocks of one row, of 16 and of others
+@pytest.mark.parametrize("sizes", [BIG, SMALL, dict(nope=64, rope=64, rank=512, v=64)], ids=["512", "256", "mixed"])
+@pytest.mark.parametrize("seqs, most, H", [(47, 1, 8), (48, 1, 3), (49, 1, 16), (20, 8, 5), (70, 6, 16), (40, 23, 1), (130, 8, 1)])
+def test_many_sequences(sizes, seqs, most, H):
+    device()
+    say("many", sizes, seqs, most, H)
+    rng = np.random.default_rng(seqs)
+    rows = rng.integers(most if most == 1 else 0, most + 1, seqs).tolist()
+    check(L.Case(BF, rows, rng.integers(0, 200, seqs).tolist(), H, seed=seqs, **sizes))
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_long_context(dtype):
     device()
