@@ -173,10 +173,17 @@ SPEC_API spec_status spec_op_rope_latent(int32_t dtype, int32_t R, int32_t n_hea
  * rope_dim) for most models).  A page id outside 0 .. num_pages - 1 is refused
  * (SPEC_E_INVALID), as are more than 2^30 positions a sequence or rows x heads.
  * Buffers 16-byte aligned (head strides too).
- * Scores and sums are fp32.  bf16 rounds the queries in the latents' space, the
- * probabilities and the sums of latents to bf16; probabilities below 2^-126 of a
- * row's largest count as 0.  A cache entry that is not finite reaches the rows that
- * see its key only.
+ * Two forms of the same sums, chosen for each sequence: few rows take their queries
+ * to the latents' space and attend to the cache itself; bf16 runs of 24 rows and more
+ * (more behind a long context) make every head's keys and values of their
+ * sequence in the workspace first, which then has 2 Hq (nope_dim + v_dim) bytes a token,
+ * up to 4 GiB in all; sequences beyond that take the first form.
+ * Scores and sums are fp32.  bf16 rounds once each, to bf16, the queries in the latents'
+ * space (second form: the keys), the probabilities, the sums of latents (the
+ * values) and the output; probabilities below 2^-126 of a row's largest count as 0.
+ * How keys are shared out among workgroups goes by all sequences of the call, so a
+ * row's last bits can differ between batches; equal calls give equal bits.  A cache
+ * entry that is not finite reaches the rows that see its key only.
  * workspace: device, 256-byte aligned, >= spec_op_attention_latent_workspace_bytes
  * of the same rows and positions (0 for arguments the call refuses), not shared by
  * calls that overlap in time.  Captured calls and host arrays as

@@ -156,6 +156,10 @@ __global__ __launch_bounds__(256, 3) void latent_expand_kernel(LatentArgs a, con
 // the maximum first.  Values that are not finite are
 // dropped from chunks in which some row does not see their key, and added after the
 // walk for the rows that do.
+// 8192 rows of 32 heads (687 GFLOP of attention) take 690 to 750 us, 0.92 to 1.0 PFLOP/s, 1000 rows
+// behind 6000 others 147: MFMA (busy 48% of the cycles) and the softmax's vector instructions
+// (43%) of a SIMD's two waves add up more than they overlap.  Four waves of 64 rows, a
+// wave's own two chunks interleaved instead, 788 us.
 
 constexpr float kPromptRescaleLog2 = 8.f;
 constexpr float kPromptLargeLogit = 65536.f;
