@@ -214,6 +214,53 @@ def test_page_ids_beyond_32_bit_offsets():
     assert L.row_error(c.run(B), ref) <= L.TOL[BF]
 
 
+def test_expanded_pages_up_to_their_limit():
+    """Keys and values of 60500 tokens of 128 heads, 3.96 GB beyond 32-bit offsets; a second prompt's would pass 4 GiB, and it is
+    attended to in the cache itself."""
+    device()
+    say("4 GiB")
+    H, rows, pos0 = 128, [5500, 5200], [55000, 0]
+    c = L.Case(BF, rows, pos0, H, seed=23)
+    one = B.spec_op_attention_latent_workspace_bytes(B.SPEC_BF16, rows[:1], pos0[:1], c.table.shape[1], H, 128, 64, 512, 128)
+    both = B.spec_op_attention_latent_workspace_bytes(*c.args(B), c.table.shape[1], H, 128, 64, 512, 128)
+    say("workspace", one, both)
+    assert one > 60500 * H * 512 and both - one >= 2 * 5200 * H * 1024  # the second: queries and sums in the latents' space
+    got = c.run(B)
+    flat, first = c.pages.view(-1, 576), 0
+    for i in range(2):
+        held = flat[c.slots(i)]
+        for r in (0, 127, 2700, rows[i] - 2):  # two rows from each
+            n = pos0[i] + r + 2
+            ref = L.attend(c.q[first + r:first + r + 2], held[:n], pos0[i] + r, c.w_k, c.w_v, c.scale, 512)
+            err = L.row_error(got[first + r:first + r + 2], ref)
+            say("error", i, r, err)
+            assert err <= L.TOL[BF]
+        first += rows[i]
+    assert torch.isfinite(got).all() and (c.out[len(c.q):] == 7).all()
+
+
+def test_two_calls_at_once():
+    """Two streams, each with a workspace of its own, a verify beside a prompt, again and again."""
+    device()
+    say("two calls")
+    cases = [L.Case(BF, [6, 5], [2047, 300], 32, seed=24), L.Case(BF, [700], [100], 8, seed=25)]
+    spaces, refs = [c.workspace(B) for c in cases], [c.run(B).clone() for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        for c, ws, st in zip(cases, spaces, streams):
+            c.out.fill_(7)
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for c, ws, st in zip(cases, spaces, streams):
+                c.run(B, ws, st)
+        torch.cuda.synchronize()
+        for c, ref in zip(cases, refs):
+            assert torch.equal(c.out[:len(c.q)].view_as(ref), ref)
+    for c, ref in zip(cases, refs):
+        assert L.row_error(ref, c.ref()) <= L.TOL[BF]
+
+
 @pytest.mark.parametrize("case", [([6], [2047]), ([2, 300], [40, 100])], ids=["verify", "mixed"])
 def test_another_stream_and_a_captured_call(case):
     device()
