@@ -172,7 +172,9 @@ SPEC_API spec_status spec_op_rope_latent(int32_t dtype, int32_t R, int32_t n_hea
  * device dtype [sum rows, Hq * v_dim]; scale multiplies the scores (1 / sqrt(nope_dim +
  * rope_dim) for most models).  A page id outside 0 .. num_pages - 1 is refused
  * (SPEC_E_INVALID), as are more than 2^30 positions a sequence or rows x heads.
- * Buffers 16-byte aligned (head strides too).
+ * Calls of more workgroups than a launch holds (2^24 - 1, fp32 of rank 256 2^23 - 1;
+ * the first form's take 16 to 64 rows x heads of one sequence, fp32's 16) are
+ * SPEC_E_UNSUPPORTED.  Buffers 16-byte aligned (head strides too).
  * Two forms of the same sums, chosen for each sequence: few rows take their queries
  * to the latents' space and attend to the cache itself; bf16 runs of 24 rows and more
  * (more behind a long context) make every head's keys and values of their

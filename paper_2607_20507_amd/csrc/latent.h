@@ -50,6 +50,12 @@ constexpr int kLatentMaxParts = 512;
 LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int fp32_waves);
 constexpr int latent_f32_waves(int rank) { return rank == 256 ? 8 : 4; }
 
+// Tiles of those segments (there are at most that many items, or a few hundred), and the
+// most items that a launch takes: one workgroup each of 256 threads, or of an fp32 item's
+// waves, and a launch counts its threads in 32 bits.
+int64_t latent_tiles(const std::vector<LatentSegment>& segs, int H, int fp32_waves);
+constexpr int64_t latent_max_items(int fp32_waves) { return ((int64_t{1} << 32) - 1) / (fp32_waves > 4 ? 64 * fp32_waves : 256); }
+
 // Items of the expanded form (below): blocks of `rows` (256 or 128) rows, those with
 // most keys first.
 struct LatentPromptPlan {

@@ -954,7 +954,7 @@ hipError_t launch_latent_values(const LatentArgs& a, hipStream_t st) {
 
 hipError_t launch_latent_attention(const LatentArgs& a, const LatentItem* items, int n_items, int tile, hipStream_t st) {
   if (n_items <= 0) return hipSuccess;
-  if (static_cast<size_t>(n_items) > kMaxGrid256) return hipErrorInvalidValue;
+  if (n_items > latent_max_items(a.dtype == 0 ? latent_f32_waves(a.rank) : 0)) return hipErrorInvalidValue;
   if (a.rank == 512 && a.rope == 64) return launch_attention<512, 64>(a, items, n_items, tile, st);
   if (a.rank == 512 && a.rope == 32) return launch_attention<512, 32>(a, items, n_items, tile, st);
   if (a.rank == 256 && a.rope == 64) return launch_attention<256, 64>(a, items, n_items, tile, st);

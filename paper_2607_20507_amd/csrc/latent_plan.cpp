@@ -23,19 +23,30 @@ int64_t least_split(int64_t lo, int64_t hi, int64_t target, F&& items) {
 
 constexpr int kCus = 256;
 
+// Query vectors of a tile: the narrowest that holds a sequence's, at most 64 (32 heads of rank
+// 512; tiles of 16 / 32 / 64, us a call): one token of 64 sequences 70 / 56 / 60, the same
+// of 131000 keys 71 / 53 / 55, 4 to 8 rows of 64 sequences 201 / 172 / 128; 16 heads of rank
+// 256, one token of 64 sequences 36 / 40 / 40.  (Tiles of 128, a wave with 32 query vectors
+// and its SIMD to itself, took 131 for the second last.)
+int tile_of(const std::vector<LatentSegment>& segs, int H, bool fp32) {
+  int64_t most = 1;
+  for (const LatentSegment& s : segs) most = std::max<int64_t>(most, static_cast<int64_t>(s.nrows) * H);
+  return fp32 || most <= 16 ? 16 : most <= 32 ? 32 : 64;
+}
+
 }  // namespace
+
+int64_t latent_tiles(const std::vector<LatentSegment>& segs, int H, int fp32_waves) {
+  const int tile = tile_of(segs, H, fp32_waves > 0);
+  int64_t n = 0;
+  for (const LatentSegment& s : segs) n += (static_cast<int64_t>(s.nrows) * H + tile - 1) / tile;
+  return n;
+}
 
 LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int fp32_waves) {
   const bool fp32 = fp32_waves > 0;
   LatentPlan p;
-  int64_t most = 1;
-  for (const LatentSegment& s : segs) most = std::max<int64_t>(most, static_cast<int64_t>(s.nrows) * H);
-  // The narrowest tile that holds a sequence's query vectors, at most 64 (32 heads of rank
-  // 512; tiles of 16 / 32 / 64, us a call): one token of 64 sequences 70 / 56 / 60, the same
-  // of 131000 keys 71 / 53 / 55, 4 to 8 rows of 64 sequences 201 / 172 / 128; 16 heads of rank
-  // 256, one token of 64 sequences 36 / 40 / 40.  (Tiles of 128, a wave with 32 query vectors
-  // and its SIMD to itself, took 131 for the second last.)
-  p.tile = fp32 || most <= 16 ? 16 : most <= 32 ? 32 : 64;
+  p.tile = tile_of(segs, H, fp32);
   struct Tile {
     int32_t qv0, nqv, row0, pos0, page0, kend, qoff;
   };

@@ -705,7 +705,11 @@ LatentCall latent_call(int32_t dtype, int32_t n_seqs, const int32_t* rows, const
   }
   c.status = SPEC_OK;
   if (c.rows == 0) return c;
-  if (c.R) c.plan = plan_latent(segs, n_heads, dtype == SPEC_F32 ? latent_f32_waves(rank) : 0);
+  const int waves = dtype == SPEC_F32 ? latent_f32_waves(rank) : 0;
+  // (the expanded form's launches stay far below: 4 GiB of keys and values hold under 2^20 blocks x heads)
+  if (latent_tiles(segs, n_heads, waves) > latent_max_items(waves))
+    return fail(SPEC_E_UNSUPPORTED, "spec_op_attention_latent: more workgroups than a launch holds");
+  if (c.R) c.plan = plan_latent(segs, n_heads, waves);
   c.x = plan_latent_prompt(x_segs, n_heads);
   if (c.R && c.R < c.rows)
     for (const LatentSegment& s : segs)
