@@ -1,5 +1,7 @@
-"""Attention over a latent cache: workspaces that held other calls' values, and sequences alone and among
-others."""
+"""Attention over a latent cache: workspaces that held other calls' values, sequences alone and among others, and entries that
+are not finite in every tile."""
+
+import math
 
 import numpy as np
 import pytest
@@ -59,3 +61,27 @@ def test_a_sequence_alone_and_among_others(dtype, sizes):
         c, want = part(seqs)
         got = c.run(B)
         assert torch.isfinite(got).all() and L.row_error(got, want) <= L.TOL[dtype]
+
+
+# heads and rows of one sequence: in bf16 tiles of 16 (whole rows of it, or a row's heads), 32 and 64, and the second form; whole
+# contexts and parts; a context that ends inside a chunk of 32 keys, where a single row's own key is in a chunk that is cleaned
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("sizes", [BIG, SMALL], ids=["512", "256"])
+@pytest.mark.parametrize("rows, H", [(4, 4), (16, 1), (1, 16), (2, 16), (8, 4), (5, 12), (30, 3)])
+@pytest.mark.parametrize("pos0", [70, 2500])
+def test_entries_that_are_not_finite(dtype, sizes, rows, H, pos0):
+    device()
+    rank = sizes["rank"]
+    c = L.Case(dtype, [rows, 1], [pos0, 31], H, seed=50, **sizes)
+    flat, slots = c.pages.view(-1, rank + sizes["rope"]), c.slots(0)
+    whole = flat.clone()
+    for bad in sorted({0, rows // 2, rows - 1}):
+        for dim, value in [(0, math.nan), (rank - 1, math.inf), (rank // 2 + 5, -math.inf), (rank + 3, math.nan)]:
+            say("not finite", dtype, sizes, rows, H, pos0, bad, dim, value)
+            flat.copy_(whole)
+            flat[slots[pos0 + bad], dim] = value  # the key of row `bad`
+            got, ref = c.run(B), c.ref()
+            fine = torch.isfinite(ref).all(-1)
+            assert fine[:bad].all() and not fine[bad:rows].any() and fine[rows:].all()
+            assert torch.isfinite(got[fine]).all() and L.row_error(got[fine], ref[fine]) <= L.TOL[dtype]
+            assert not torch.isfinite(got[~fine]).all(-1).any()
