@@ -701,7 +701,7 @@ __global__ __launch_bounds__(256, WK == 1 ? 2 : 1) void attn_latent_bf16_kernel(
     chunk(c, b, last > pos_lo || last >= it.t1);
   }
 
-  sums_ready();
+  sums_ready(acc);
   float l = lrun[0] + lrun[1];
   l += __shfl_xor(l, 16, kWave);
   l += __shfl_xor(l, 32, kWave);

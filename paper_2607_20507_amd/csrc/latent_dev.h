@@ -48,7 +48,15 @@ __device__ __forceinline__ void scale_in_place(f32x4& c, float x) {
   }
 }
 __device__ __forceinline__ void operands_ready() { asm volatile("s_nop 1"); }
+// (Keeps its place among the statements of asm only: what else reads a sum takes it from one behind this wait, or is
+// moved ahead of it.)
 __device__ __forceinline__ void sums_ready() { asm volatile("s_nop 15\n\ts_nop 7"); }
+template <int N>
+__device__ __forceinline__ void sums_ready(f32x4 (&acc)[N]) {
+  sums_ready();
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+a"(acc[i]));
+}
 
 __device__ __forceinline__ void wave_fence() {
   __atomic_signal_fence(__ATOMIC_SEQ_CST);
