@@ -184,7 +184,9 @@ SPEC_API spec_status spec_op_rope_latent(int32_t dtype, int32_t R, int32_t n_hea
  * space (second form: the keys), the probabilities, the sums of latents (the
  * values) and the output; probabilities below 2^-126 of a row's largest count as 0.
  * How keys are shared out among workgroups goes by all sequences of the call, so a
- * row's last bits can differ between batches; equal calls give equal bits.  A cache
+ * row's last bits can differ between batches; equal calls give equal bits.  A call of
+ * few sequences splits long contexts; one of hundreds does not, and then takes as long as
+ * its longest (131000 keys: 3.6 ms), which is better given a call of its own.  A cache
  * entry that is not finite reaches the rows that see its key only.
  * workspace: device, 256-byte aligned, >= spec_op_attention_latent_workspace_bytes
  * of the same rows and positions (0 for arguments the call refuses), not shared by

@@ -63,7 +63,8 @@ __device__ __forceinline__ void get8(const bf16_t* p, float (&v)[8]) {
 // Append: one workgroup per row and share of the heads.  A thread's unit is 8
 // consecutive values (or 8 rotary pairs, whose halves are 8 consecutive values
 // each).  The first share's first wave norms the latent: 8 values a lane.  Bound by
-// HBM: 8192 rows of 32 heads move 330 MB in 54 to 56 us, 6 TB/s.
+// HBM: 8192 rows of 32 heads move 330 MB in 54 to 56 us, 6 TB/s, more than a copy's 4.9: two
+// bytes are read for each written.
 
 template <typename T>
 __global__ __launch_bounds__(256) void rope_latent_kernel(int H, int nope, int rope, int rank, float theta, float eps,
@@ -465,10 +466,16 @@ __global__ __launch_bounds__(256) void latent_combine_kernel(LatentArgs a, const
 // nothing wider, and a second bf16 part of the sums alone would double what the values'
 // kernel reads to take a row's error from 0.0031 to 0.0026.
 // What bounds it: tiles of 64 (64 sequences, 384 rows of 32 heads over 512 .. 4096 keys,
-// 73 us) the second product's LDS reads, each feeding one 16-row product, and MFMA
-// (pipe busy 35% of the cycles in which a CU holds waves); tiles of 32 (one row over
-// 131001 keys, 33 us) HBM, 151 MB at 4.6 TB/s; short contexts the chain of a chunk's
-// two products and softmax, about 2 us.
+// 73 us) that a chunk's scores, softmax and sums take turns: of the cycles in which a CU
+// holds waves LDS is in use 38% (the second product's reads feed one 16-row product each),
+// MFMA 36%, vector instructions 24%; tiles of 32 (one row over 131001 keys, 33 us) HBM, 151 MB
+// at 4.6 TB/s; short contexts the chain of a chunk's loads, two products and softmax, about 2 us,
+// and that few CUs have one: 6 rows of 32 heads over 2053 keys (17 us) are 51 workgroups of four
+// chunks in turn, MFMA busy 13% and waves waiting 36% of their time.  A tile of 16 has one buffer a
+// key share, whose next loads leave when its chunk is done: 8 sequences of 256 .. 512 keys (rank
+// 256, 12 us) wait half of the time.
+// Two workgroups a CU (WK = 1) leave 256 registers a wave: rank 512 spills 12 to 15, one of them
+// read again in the keys' loop.
 // A key that some row does not see may hold a value that is not finite (a slot past the
 // sequence anything at all), whose product with the row's probability 0 would be NaN.
 // So chunks with such keys are cleaned in LDS between the two products: values that
@@ -741,9 +748,13 @@ __global__ __launch_bounds__(256, WK == 1 ? 2 : 1) void attn_latent_bf16_kernel(
 
 // ---------------------------------------------------------------------------
 // Absorbed attention, fp32: 16 query vectors a workgroup, whose waves take its pages in
-// turn.  A page is (rank 256) 136 MFMAs of 32 cycles in one wave, the bound of a short
-// context: eight waves there, four where registers allow no more (5 rows of 4 heads over
-// 133 keys, eight waves 17 us; asking for a page's values before its softmax 17.4).
+// turn: eight, four where registers allow no more.  What bounds it is waiting for the cache: a
+// page's 34 loads (rank 256) are asked for one ahead of their use, a chain of some 17 answers, and
+// the next page's id behind them.  5 rows of 4 heads over 133 keys take 17 us in two workgroups
+// whose waves have one page or two: they wait 62% of their time, and their pages' MFMAs, 136 of 32
+// cycles each, are 13% of it (asking for a page's values before its softmax 17.4).  One row of 4 heads
+// over 30000 keys is 34 us a call where the bytes take 7, 1024 rows of 16 heads behind 3000 keys 742
+// where the flops take 146.
 // fp32 MFMA throughout (16 x 16 x 4), operands straight from the cache: k-step (j, i)
 // of the scores takes dim 16 j + 4 g + i in lane group g, and output tile (j, t) holds
 // dims 64 j + 4 row + t, so that every load is 16 bytes a lane and a lane's scores are

@@ -70,7 +70,14 @@ LatentPlan plan_latent(const std::vector<LatentSegment>& segs, int H, int fp32_w
   const int target = p.tile == 64 && all_keys / kCus >= 1200 ? kCus * 3 / 2 : kCus;
   // Whole where a wave then has at most four chunks of 32 keys, or two fp32 pages (a join is
   // a launch): 8 sequences of 256 to 512 keys, 16 heads of rank 256, 24.8 us in parts, 17.3
-  // whole.  Otherwise at least a chunk, or page, for every wave that takes keys of its own.
+  // whole.  Otherwise an item has at least four chunks, or a page for every fp32 wave.  Four
+  // chunks are one for each key share of a tile of 16, but two in turn of a tile of 32, and of
+  // a tile of 64 four: 6 rows of 32 heads behind 505 / 1005 / 2047 / 4000 keys are 12 / 24 / 51 /
+  // 96 items on 256 CUs (25.5 / 25.3 / 28.5 / 36.4 us a call).
+  // The split is one for all tiles, and makes as many items as there are tiles, or the target:
+  // with that many tiles every context stays whole, however long one is.  32 heads, one row of
+  // 199 sequences of 512 to 4096 keys 132 us, and of one more of 131001, in parts, 175; of 255
+  // such sequences 185, and of one more of 131001, which one workgroup walks, 3629.
   const int shares = p.tile == 64 ? 1 : p.tile == 32 ? 2 : 4;
   const int whole = fp32 ? fp32_waves : 4 * shares;
   const int least = most_keys <= 32 * whole ? whole : fp32 ? fp32_waves / 2 : 4;
@@ -123,7 +130,10 @@ LatentPromptPlan plan_latent_prompt(const std::vector<LatentSegment>& segs, int 
       tiles.push_back(Block{s.row0 + s.qoff + first, n, s.pos0 + first, s.page0, s.pos0 + first + n});
       most_keys = std::max<int64_t>(most_keys, tiles.back().kend);
     }
-  // the least range of keys, in 64s and at least 256, with which the workgroups run at once
+  // The least range of keys, in 64s and at least 256, with which the workgroups run at once.  As
+  // above it is one for all blocks, and does not even them out: of 32 heads, 1024 rows behind 6000
+  // keys are 4 blocks in two parts of up to 3520 keys (217 us a call); of 1025 to 1280 rows' five
+  // blocks the last ones are cut at 6528, into a long and a very short part (300 to 305).
   const int64_t split = 64 * least_split(4, (most_keys + 63) / 64, std::max<int64_t>(kCus / H, static_cast<int64_t>(tiles.size())),
                                          [&](int64_t sp) {
                                            int64_t n = 0;
@@ -144,12 +154,18 @@ LatentPromptPlan plan_latent_prompt(const std::vector<LatentSegment>& segs, int 
 }
 
 // The expanded form makes every head's keys and values of all pos0 + nrows tokens, whatever
-// the rows, and then has a third of the absorbed form's work a row and key.  The border
-// in rows grows with what is made for the keys before them (absorbed / expanded, us; 32
-// heads, 8M weights): 24 rows 29.6 / 19.3, 24 behind 500 39.6 / 30.8, 48 behind 2000 54 / 50, 96
-// behind 2000 64.5 / 53.2, 130 behind 8000 121 / 138, 200 behind 8000 150 / 144; 8 heads, 130
-// behind 8000 70.9 / 61.8, 48 52.7 / 58.1; 16 heads of 64 dims and rank 256, 48 behind 8000 45.3 / 41.2,
-// 24 40.9 / 41.0.
+// the rows, and then has a third of the absorbed form's work a row and key.  The border in
+// rows grows with what is made for the keys before them.  One sequence, absorbed / expanded, us:
+//   32 heads of 128 dims, rank 512 (4.2M weights): 16 rows 22 / 19, 24 21 / 17; behind 500 keys
+//   (border 35) 32 rows 33 / 30, 48 41 / 32; behind 2000 (68) 48 45 / 48, 64 47 / 50, 96 54 / 51; behind
+//   4000 (112) 96 66 / 73, 130 87 / 83; behind 8000 (201) 130 129 / 136, 200 184 / 142, 260 248 / 175.
+//   8 of them: behind 2000 (35) 32 29 / 31, 48 40 / 31; behind 8000 (68) 64 47 / 55, 130 54 / 61, 200 65 / 65.
+//   16 heads of 64 dims, rank 256 (0.5M): behind 2000 (30) 24 29 / 24, 32 30 / 24; behind 8000 (46)
+//   32 34 / 39, 48 40 / 39.  32 of them: behind 2000 (35) 24 34 / 26, 48 36 / 26.
+// Near the border the form that is taken is the slower one by up to 30% in places.  And it is
+// the border of one sequence: several fill the chip with fewer rows each, and the absorbed form's
+// range grows.  16 sequences of the first kind, 48 rows behind 500 83 / 134, 96 behind 2000 271 / 518,
+// 130 behind 4000 701 / 1076, four of 96 behind 2000 117 / 130: there the expanded form is taken.
 bool latent_expands(int nrows, int pos0, int64_t weights) {
   return nrows >= 24 + static_cast<double>(pos0) * static_cast<double>(weights) / 1.9e8;
 }
