@@ -153,10 +153,11 @@ SPEC_API spec_status spec_op_attention_kv4(int32_t dtype, int32_t n_seqs, const 
  * first) to q_out (the same in dtype) with its last rope_dim dims rotated; kv
  * (device fp32 [R, rank + rope_dim]) into slot[r]: the first rank values as
  * c = x / sqrt(mean(x^2) + eps) * norm_w (norm_w: device, dtype [rank]), the rest
- * rotated.  Pairs (i, i + rope_dim / 2) turn by pos[r] theta^(-2i / rope_dim).  pos
- * and slot device int32 [R] (slot = page * 16 + offset); a row with a slot outside
- * 0 .. 16 num_pages - 1 (padding: -1) has its q written and no entry.  Two rows of
- * one call must not have one slot.  Buffers 16-byte aligned, pos and slot 4. */
+ * rotated.  Pairs (i, i + rope_dim / 2) turn by pos[r] theta^(-2i / rope_dim), theta
+ * positive and finite.  pos and slot device int32 [R] (slot = page * 16 + offset); a
+ * row with a slot outside 0 .. 16 num_pages - 1 (padding: -1) has its q written and no
+ * entry.  Two rows of one call must not have one slot.  Buffers 16-byte aligned, pos
+ * and slot 4. */
 SPEC_API spec_status spec_op_rope_latent(int32_t dtype, int32_t R, int32_t n_heads, int32_t nope_dim,
                                          int32_t rope_dim, int32_t rank, float theta, float eps, const float* q,
                                          const float* kv, const void* norm_w, const int32_t* pos,

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <exception>
 #include <mutex>
 #include <string>
@@ -631,7 +632,7 @@ spec_status spec_op_rope_latent(int32_t dtype, int32_t R, int32_t n_heads, int32
                                 const void* norm_w, const int32_t* pos, const int32_t* slot, int32_t num_pages,
                                 void* q_out, void* pages, void* stream) {
   if ((dtype != SPEC_F32 && dtype != SPEC_BF16) || R < 0 || n_heads <= 0 || n_heads > kMaxHeads || !(theta > 0.f) ||
-      !(eps >= 0.f) || num_pages < 0 || num_pages > kMaxSlotPages)
+      !(theta <= FLT_MAX) || !(eps >= 0.f) || num_pages < 0 || num_pages > kMaxSlotPages)
     return refuse(SPEC_E_INVALID, "spec_op_rope_latent: bad dtype or size");
   if (!latent_sizes(nope_dim, rope_dim, rank))
     return refuse(SPEC_E_UNSUPPORTED, "spec_op_rope_latent: nope_dim must be 64 or 128, rope_dim 32 or 64, rank 256 or 512");
