@@ -474,8 +474,8 @@ __global__ __launch_bounds__(256) void latent_combine_kernel(LatentArgs a, const
 // chunks in turn, MFMA busy 13% and waves waiting 36% of their time.  A tile of 16 has one buffer a
 // key share, whose next loads leave when its chunk is done: 8 sequences of 256 .. 512 keys (rank
 // 256, 12 us) wait half of the time.
-// Two workgroups a CU (WK = 1) leave 256 registers a wave: rank 512 spills 12 to 15, one of them
-// read again in the keys' loop.
+// Two workgroups a CU (WK = 1) leave 256 registers a wave: rank 512 spills 12 (32 rotated dims)
+// or 15, of which the second kind reads one again in the keys' loop.
 // A key that some row does not see may hold a value that is not finite (a slot past the
 // sequence anything at all), whose product with the row's probability 0 would be NaN.
 // So chunks with such keys are cleaned in LDS between the two products: values that
